@@ -1,0 +1,128 @@
+// Declarations shared by the host layer and the kernels of the paged cache
+// (include/stlite_paged.h).
+#pragma once
+
+#include "stlite_internal.h"
+
+namespace stlite {
+
+// The cache and the batch of new tokens, as the kernels see them.
+struct PagedDev {
+  uint16_t* k;  // [units][n_pages][page][d]
+  uint16_t* v;
+  const int32_t* page_table;  // [n_seqs][max_pages]
+  int32_t* seq_lens;          // [n_seqs], new tokens included
+  const int32_t* cu_new;      // [n_seqs + 1]
+  int32_t n_layers, n_q_heads, n_kv_heads, n_units, group;
+  int32_t n_seqs, n_pages, max_pages, max_len;
+  int32_t page_shift;  // log2(page_size), >= 4
+  int64_t total_new;
+};
+
+struct PagedCompactArgs {
+  PagedDev c;
+  const int32_t* cu_budget;
+  int64_t total_tokens, total_budget;
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* kept;
+  int32_t kept_per_layer;
+};
+
+struct RowsIn {
+  const uint16_t* data;  // nullable (no queries)
+  int64_t token_stride, layer_stride;
+};
+
+struct PagedAppendArgs {
+  PagedDev c;
+  RowsIn q, k, v;
+  uint16_t* q_out;
+  const uint16_t* q_norm;  // [layers][d], nullable
+  const uint16_t* k_norm;
+  float eps;
+  const int32_t* positions;  // [axes][total_new], nullable: no rotation
+  int32_t interleaved;
+  int32_t axis1, axis2;  // pairs >= axis1 go by the second position, >= axis2 by the third
+  double turns[64];      // theta^(-i/64) / (2 pi): turns of pair i per position
+};
+
+// Attention runs as a flat range of keys, cut into equal shares.  The queries of
+// a (unit, sequence) are cut into items of `tokens` new tokens (all heads of the
+// kv head: tokens * group rows; decode: one token, at most 16 heads); item i of a
+// sequence with n new tokens behind c cached ones counts c + min((i + 1) tokens,
+// n) keys, what its last token sees.  Items lie one after another, units
+// outermost; work-group w takes the keys [w share, (w + 1) share) of that range.
+// A share that holds a whole item writes its output; the parts of an item that
+// several shares cut leave (max, sum, O) in the workspace and are joined by a
+// second launch.  The lengths are read on the device only, so the grid does not
+// depend on them.
+struct PagedAttnArgs {
+  PagedDev c;
+  const uint16_t* q;  // [layers][total_new][q_heads][d]
+  uint16_t* out;
+  float scale2;       // scale * log2(e)
+  int32_t parts;      // head groups of a kv head (decode: 16 heads each; else 1)
+  int32_t tokens;     // new tokens per item
+  int32_t rows;       // rows of an item's partial (decode 16, else 32 per wave)
+  int32_t shares;     // work-groups
+  int32_t min_share;  // keys
+  float* pm;          // workspace [shares][2][rows]: max (log2 units)
+  float* pl;          // workspace [shares][2][rows]: sum
+  float* po;          // workspace [shares][2][rows][d]: O, unnormalised
+};
+
+hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream);
+hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t stream);
+hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
+hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, int32_t waves, hipStream_t stream);
+
+// ---------------------------------------------------------------------------
+// Device helpers
+// ---------------------------------------------------------------------------
+
+// 16-bit element types: bf16 or IEEE half.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__bf16> {
+  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+  __device__ static f32x16_t mfma32(x8 a, x8 b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  __device__ static f32x4_t mfma16(x8 a, x8 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  // Pairs of a dword whose exponent is all ones (bits 15 and 31).
+  __device__ static uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+  // Weights are at most 2^8 of their running maximum's (kLazy): any exponent fits.
+  static constexpr float kBias = 0.0f;
+};
+template <>
+struct Elem<_Float16> {
+  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+  __device__ static f32x16_t mfma32(x8 a, x8 b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  __device__ static f32x4_t mfma16(x8 a, x8 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  __device__ static uint32_t not_finite(uint32_t w) { return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+  // Half weights lose bits below 2^-14: they are formed 2^7 times as large, at
+  // most 2^15 with kLazy.
+  static constexpr float kBias = 7.0f;
+};
+
+template <typename T>
+__device__ inline float elem_lo(uint32_t w) {
+  return float(__builtin_bit_cast(T, uint16_t(w)));
+}
+template <typename T>
+__device__ inline float elem_hi(uint32_t w) {
+  return float(__builtin_bit_cast(T, uint16_t(w >> 16)));
+}
+template <typename T>
+__device__ inline uint32_t elem_pack(float lo, float hi) {  // each rounded to nearest
+  return uint32_t(__builtin_bit_cast(uint16_t, T(lo))) | (uint32_t(__builtin_bit_cast(uint16_t, T(hi))) << 16);
+}
+
+__device__ inline int32_t paged_len(const PagedDev& c, int32_t s) { return min(max(c.seq_lens[s], 0), c.max_len); }
+
+// First row of page `page` of a unit, in rows of the pool.
+__device__ inline int64_t page_row(const PagedDev& c, int32_t unit, int32_t page) {
+  return ((int64_t(unit) * c.n_pages + page) << c.page_shift);
+}
+
+}  // namespace stlite

@@ -29,6 +29,8 @@ EXPORTS = (
     "stlite_css_saliency_nbhd", "stlite_kept_overlap", "stlite_probe_mfma", "stlite_probe_read",
     "stlite_layer_mean", "stlite_tsg_rho_concat", "stlite_css_saliency_concat", "stlite_compact_kv_layer",
     "stlite_select_topk_noalloc", "stlite_mean_attention",
+    "stlite_paged_validate", "stlite_paged_workspace_size", "stlite_paged_compact", "stlite_paged_append",
+    "stlite_paged_attention",
 )
 
 
@@ -52,6 +54,26 @@ class _CProblem(ctypes.Structure):
     ]
 
 
+class _CPaged(ctypes.Structure):
+    _fields_ = [
+        ("n_layers", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("max_len", ctypes.c_int32), ("total_new", ctypes.c_int64),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("seq_lens", ctypes.c_void_p), ("cu_new", ctypes.c_void_p), ("h_cu_new", ctypes.c_void_p),
+    ]
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
+
+
+class _CRope(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 3), ("reserved", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -63,7 +85,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_2603_00188_amd.build`")
     lib = ctypes.CDLL(path)
-    P = ctypes.POINTER(_CProblem)
+    P, C, R = ctypes.POINTER(_CProblem), ctypes.POINTER(_CPaged), ctypes.POINTER(_CRows)
     vp, sz, i64, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
     st = ctypes.c_int
     sig = {
@@ -93,6 +115,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "stlite_css_saliency_concat": (st, [P, vp, vp, vp]),
         "stlite_compact_kv_layer": (st, [P, vp, vp, vp, vp, vp, vp]),
         "stlite_select_topk_noalloc": (st, [P, vp, vp, vp, f32, vp, vp, vp]),
+        "stlite_paged_validate": (st, [C, vp, vp]),
+        "stlite_paged_workspace_size": (st, [C, ctypes.POINTER(sz)]),
+        "stlite_paged_compact": (st, [P, C, vp, vp, vp, ctypes.c_int32, vp]),
+        "stlite_paged_append": (st, [C, ctypes.POINTER(_CRope), vp, R, R, R, vp, vp, f32, vp, vp]),
+        "stlite_paged_attention": (st, [C, vp, f32, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -413,8 +440,11 @@ def kept_overlap(p: Problem, kept_a, kept_b, hits=None, stream=None):
 
 
 def compress(p: Problem, q_win, k, v, out: Buffers, alpha: float = 1.0, css: bool = True,
-             tsg: bool = True, stream=None, overlap: bool = False, mean_width: int = 0) -> Buffers:
+             tsg: bool = True, stream=None, overlap: bool = False, mean_width: int = 0, cache=None) -> Buffers:
     """The whole pass: score, gate, saliency, select, compact (five C calls).
+
+    With ``cache`` (a paged.PagedCache) the kept rows go into its pages, which
+    serving goes on from, instead of out.k_out and out.v_out.
 
     mean_width > 0 ranks on the Mean-Attention prior (stlite_mean_attention of
     that width, written to out.a_mean) instead of A_base.
@@ -456,7 +486,11 @@ def compress(p: Problem, q_win, k, v, out: Buffers, alpha: float = 1.0, css: boo
         prior = out.a_mean
     stlite_select_topk(p, prior, out.phi if css else None, out.gate if tsg else None, alpha,
                        out.kept, out.score, out.ws, main)
-    stlite_compact_kv(p, k, v, out.kept, out.k_out, out.v_out, main)
+    if cache is not None:
+        from . import paged
+        paged.paged_compact(cache, p, k, v, out.kept, stream=main)
+    else:
+        stlite_compact_kv(p, k, v, out.kept, out.k_out, out.v_out, main)
     return out
 
 

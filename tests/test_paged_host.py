@@ -1,0 +1,466 @@
+"""CPU tests of the paged cache: the cuts of an attention call, the refusals of
+every entry point and of the binding, validation of tables and lengths, and the
+64-bit oracle against closed forms."""
+import ctypes
+import os
+import random
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as OP
+from paper_2603_00188_amd import paged as P
+from paper_2603_00188_amd import stlite as S
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2603_00188_amd", "csrc")
+FAKE = 0x100000  # never dereferenced: validation reads only the host mirror
+
+needs_lib = pytest.mark.skipif(not os.path.exists(S.LIB_PATH), reason="libstlite.so not built")
+
+# ---------------------------------------------------------------------------
+# Cuts (csrc/paged_cuts.h, the code that the kernels compile)
+# ---------------------------------------------------------------------------
+
+# argv: units tokens shares min_share, then n and cached of each sequence.  Walks
+# every share as the attention kernels do and every boundary as the joining launch
+# does; prints the number of joined items, fails on a tile, an item or a slot out
+# of place.
+PROGRAM = r"""
+#include <stdio.h>
+#include <stdlib.h>
+#include <map>
+#include <vector>
+#include "paged_cuts.h"
+using namespace stlite;
+struct Item { int64_t start, keys; int32_t tiles; };
+int main(int argc, char** argv) {
+  const int64_t units = atoll(argv[1]);
+  const int32_t tokens = atoi(argv[2]), shares = atoi(argv[3]), min_share = atoi(argv[4]);
+  std::vector<Item> items;
+  int64_t at = 0;
+  for (int64_t u = 0; u < units; ++u)
+    for (int i = 5; i + 1 < argc; i += 2) {
+      const int32_t n = atoi(argv[i]), cached = atoi(argv[i + 1]);
+      int64_t base = at;
+      for (int32_t k = 0; k < paged_items(n, tokens); ++k) {
+        if (at != base + paged_prefix(k, cached, tokens)) { printf("prefix of item %d\n", k); return 1; }
+        const int64_t keys = paged_item_keys(k, n, cached, tokens);
+        const int64_t seen = cached + (int64_t(k) * tokens + tokens < n ? int64_t(k) * tokens + tokens : n);
+        if (keys < seen || keys < 1) { printf("item %d counts %lld keys, sees %lld\n", k, (long long)keys, (long long)seen); return 1; }
+        if (paged_item_of(at - base, n, cached, tokens) != k || paged_item_of(at - base + keys - 1, n, cached, tokens) != k) { printf("item_of %d\n", k); return 1; }
+        items.push_back({at, keys, int32_t((keys + kPagedTile - 1) / kPagedTile)});
+        at += keys;
+      }
+      if (at - base != paged_keys(n, cached, tokens)) { printf("keys of a sequence\n"); return 1; }
+    }
+  const int64_t total = at, share = paged_share(total, shares, min_share);
+  if (share * shares < total) { printf("shares do not cover the range\n"); return 1; }
+  std::map<int64_t, size_t> slots;                 // slot -> item
+  std::vector<int32_t> next(items.size(), 0);      // tiles covered so far
+  std::vector<int> parts(items.size(), 0), whole(items.size(), 0);
+  for (int64_t w = 0; w < shares; ++w) {
+    int64_t x = w * share;
+    const int64_t y = x + share < total ? x + share : total;
+    size_t i = 0;
+    if (x < y) while (items[i].start + items[i].keys <= x) ++i;
+    for (; x < y; ++i) {
+      const PagedPart p = paged_part(x, y, items[i].start, items[i].keys);
+      if (p.t0 != next[i] || p.t1 < p.t0) { printf("share %lld item %zu: tiles %d .. %d, %d covered\n", (long long)w, i, p.t0, p.t1, next[i]); return 1; }
+      next[i] = p.t1;
+      ++parts[i];
+      if (p.whole) ++whole[i];
+      else {
+        const int64_t slot = paged_slot(w, share, items[i].start);
+        if (slot < 0 || slot >= 2 * int64_t(shares) || slots.count(slot)) { printf("slot %lld twice\n", (long long)slot); return 1; }
+        slots[slot] = i;
+      }
+      x = p.end;
+    }
+  }
+  std::vector<int> joined(items.size(), 0);
+  for (int64_t w = 0; w + 1 < shares; ++w) {
+    const int64_t cut = (w + 1) * share;
+    if (cut >= total) continue;
+    size_t i = 0;
+    while (items[i].start + items[i].keys <= cut) ++i;
+    if (items[i].start == cut || items[i].start / share != w) continue;
+    ++joined[i];
+    const int64_t w1 = (items[i].start + items[i].keys - 1) / share;
+    for (int64_t k = w; k <= w1; ++k) {
+      const auto at = slots.find(paged_slot(k, share, items[i].start));
+      if (at == slots.end() || at->second != i) { printf("item %zu: share %lld left no part\n", i, (long long)k); return 1; }
+    }
+    if (w1 - w + 1 != parts[i]) { printf("item %zu: %d parts\n", i, parts[i]); return 1; }
+  }
+  int n_joined = 0;
+  for (size_t i = 0; i < items.size(); ++i) {
+    if (next[i] != items[i].tiles) { printf("item %zu: %d of %d tiles\n", i, next[i], items[i].tiles); return 1; }
+    if (whole[i] + joined[i] != 1 || (whole[i] && parts[i] != 1)) { printf("item %zu: written %d times\n", i, whole[i] + joined[i]); return 1; }
+    n_joined += joined[i];
+  }
+  printf("%d\n", n_joined);
+  return 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def cuts(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("no host compiler")
+    d = tmp_path_factory.mktemp("paged_cuts")
+    src, exe = str(d / "cuts.cpp"), str(d / "cuts")
+    with open(src, "w") as f:
+        f.write(PROGRAM)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", f"-I{CSRC}", src, "-o", exe], check=True)
+
+    def run(units, tokens, shares, min_share, seqs):
+        args = [str(x) for s in seqs for x in s]
+        r = subprocess.run([exe, str(units), str(tokens), str(shares), str(min_share), *args], capture_output=True, text=True)
+        assert r.returncode == 0, (units, tokens, shares, min_share, seqs, r.stdout)
+        return int(r.stdout)
+    return run
+
+
+@pytest.mark.parametrize("units,tokens,shares,min_share,seqs", [
+    (1, 1, 512, 64, [(1, 0)]), (1, 1, 512, 64, [(1, 677)]), (4, 1, 512, 64, [(1, 677)]), (112, 1, 512, 64, [(1, 30104)]),
+    (3, 1, 512, 64, [(1, -1), (0, 50), (1, 0), (1, 63), (1, 64), (0, 0)]), (1, 1, 1, 64, [(1, 5)]),
+    (4, 36, 256, 256, [(3136, 30105)]), (2, 32, 256, 256, [(131, 0), (2999, 0), (1, 0), (32, 0), (33, 0)]),
+    (5, 18, 512, 256, [(5, -3), (5, 2), (5, 4000), (0, 9)]), (2, 1, 512, 256, [(7, 100)]), (1, 128, 512, 256, [(129, 1)]),
+])
+def test_every_tile_and_output_once(cuts, units, tokens, shares, min_share, seqs):
+    cuts(units, tokens, shares, min_share, seqs)
+
+
+def test_cuts_of_random_batches(cuts):
+    r = random.Random(11)
+    joined = 0
+    for _ in range(150):
+        tokens = r.choice([1, 1, 2, 18, 32, 36, 128, 256])
+        most = 1 if tokens == 1 else r.choice([3, 40, 700])
+        seqs = [(r.randint(0, most), r.choice([-1, 0, 0, 1, 63, r.randint(0, 3000)])) for _ in range(r.randint(1, 9))]
+        if not any(n for n, _ in seqs):
+            seqs[0] = (1, 10)
+        joined += cuts(r.randint(1, 6), tokens, r.choice([1, 2, 3, 17, 256, 512]), r.choice([1, 63, 64, 256]), seqs)
+    assert joined > 100
+
+
+# ---------------------------------------------------------------------------
+# Refusals
+# ---------------------------------------------------------------------------
+
+
+class Fake:
+    """A _CPaged whose host mirror is real and whose device pointers are fake."""
+
+    def __init__(self, counts=(0, 1, 3), **kw):
+        self.cu = np.asarray(counts, np.int32)
+        f = dict(n_layers=2, n_q_heads=28, n_kv_heads=4, head_dim=128, dtype=0, page_size=16, n_pages=20,
+                 n_seqs=len(self.cu) - 1, max_pages=5, max_len=80, total_new=int(self.cu[-1]), k=FAKE, v=FAKE,
+                 page_table=FAKE, seq_lens=FAKE, cu_new=FAKE, h_cu_new=self.cu.ctypes.data)
+        f.update(kw)
+        self.c = S._CPaged(**f)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _err():
+    return S.load().stlite_last_error().decode()
+
+
+BAD = [
+    (dict(head_dim=64), S.ERR_UNSUPPORTED, "head_dim"), (dict(n_q_heads=30), S.ERR_INVALID_ARG, "multiple"),
+    (dict(n_q_heads=0), S.ERR_INVALID_ARG, ">= 1"), (dict(n_layers=0), S.ERR_INVALID_ARG, ">= 1"),
+    (dict(n_q_heads=129 * 4), S.ERR_UNSUPPORTED, "per kv head"), (dict(dtype=2), S.ERR_INVALID_ARG, "dtype"),
+    (dict(page_size=8), S.ERR_UNSUPPORTED, "page_size"), (dict(page_size=48), S.ERR_UNSUPPORTED, "page_size"),
+    (dict(page_size=512), S.ERR_UNSUPPORTED, "page_size"), (dict(n_pages=0), S.ERR_INVALID_ARG, "n_pages"),
+    (dict(n_pages=2 ** 27), S.ERR_UNSUPPORTED, "2^31"), (dict(n_seqs=0), S.ERR_INVALID_ARG, "n_seqs"),
+    (dict(n_seqs=65536), S.ERR_UNSUPPORTED, "65535"), (dict(n_layers=20000), S.ERR_UNSUPPORTED, "65535"),
+    (dict(max_pages=0), S.ERR_INVALID_ARG, "max_pages"), (dict(max_len=0), S.ERR_INVALID_ARG, "max_len"),
+    (dict(max_len=81), S.ERR_INVALID_ARG, "max_len"),
+    (dict(max_pages=2 ** 25, max_len=2 ** 28 + 1), S.ERR_UNSUPPORTED, "2^28"),
+    (dict(k=None), S.ERR_INVALID_ARG, "non-NULL"), (dict(v=None), S.ERR_INVALID_ARG, "non-NULL"),
+    (dict(page_table=None), S.ERR_INVALID_ARG, "non-NULL"), (dict(k=FAKE + 8), S.ERR_INVALID_ARG, "aligned"),
+]
+BAD_BATCH = [
+    (dict(seq_lens=None), S.ERR_INVALID_ARG, "non-NULL"), (dict(cu_new=None), S.ERR_INVALID_ARG, "non-NULL"),
+    (dict(h_cu_new=None), S.ERR_INVALID_ARG, "non-NULL"), (dict(total_new=4), S.ERR_INVALID_ARG, "total_new"),
+    (dict(max_len=1), S.ERR_INVALID_ARG, "new tokens"),
+]
+
+
+@needs_lib
+@pytest.mark.parametrize("change, status, text", BAD + BAD_BATCH)
+def test_cache_rejections(change, status, text):
+    """Every call refuses a malformed cache with nothing enqueued."""
+    lib, f = S.load(), Fake(**change)
+    n = ctypes.c_size_t(7)
+    row = ctypes.byref(S._CRows(FAKE, 36 * 128, 3 * 36 * 128))
+    calls = [lambda: lib.stlite_paged_validate(f.ref, None, None),
+             lambda: lib.stlite_paged_workspace_size(f.ref, ctypes.byref(n)),
+             lambda: lib.stlite_paged_append(f.ref, None, None, row, row, row, None, None, 0.0, FAKE + 4096, None),
+             lambda: lib.stlite_paged_attention(f.ref, FAKE, 1.0, FAKE + 4096, FAKE, 1 << 40, None)]
+    for call in calls:
+        assert call() == status
+        assert text in _err()
+    assert n.value == 0
+
+
+@needs_lib
+@pytest.mark.parametrize("cu", [(1, 2, 3), (0, 2, 1), (0, 81, 82)])
+def test_new_token_counts_rejected(cu):
+    f = Fake(counts=cu)
+    assert S.load().stlite_paged_validate(f.ref, None, None) == S.ERR_INVALID_ARG
+
+
+@needs_lib
+def test_null_arguments_rejected():
+    lib, f = S.load(), Fake()
+    n = ctypes.c_size_t(0)
+    assert lib.stlite_paged_validate(None, None, None) == S.ERR_INVALID_ARG
+    assert lib.stlite_paged_workspace_size(f.ref, None) == S.ERR_INVALID_ARG
+    assert lib.stlite_paged_workspace_size(None, ctypes.byref(n)) == S.ERR_INVALID_ARG
+    assert lib.stlite_paged_attention(None, FAKE, 1.0, FAKE, FAKE, 1, None) == S.ERR_INVALID_ARG
+    assert lib.stlite_paged_append(None, None, None, None, None, None, None, None, 0.0, None, None) == S.ERR_INVALID_ARG
+
+
+@needs_lib
+def test_attention_rejections():
+    lib, f = S.load(), Fake()
+    n = ctypes.c_size_t(0)
+    assert lib.stlite_paged_workspace_size(f.ref, ctypes.byref(n)) == S.OK and n.value > 0 and n.value % 256 == 0
+    call = lambda q=FAKE, scale=1.0, out=FAKE + 4096, ws=FAKE, nb=n.value: lib.stlite_paged_attention(  # noqa: E731
+        f.ref, q, scale, out, ws, nb, None)
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(scale=scale) == S.ERR_INVALID_ARG and "scale" in _err()
+    assert call(ws=None) == S.ERR_WORKSPACE
+    assert call(nb=n.value - 1) == S.ERR_WORKSPACE
+    assert call(ws=FAKE + 16) == S.ERR_WORKSPACE
+    assert call(q=None) == S.ERR_INVALID_ARG and call(out=None) == S.ERR_INVALID_ARG
+    assert call(out=FAKE) == S.ERR_INVALID_ARG and "alias" in _err()
+    assert call(q=FAKE + 8) == S.ERR_INVALID_ARG and call(out=FAKE + 4104) == S.ERR_INVALID_ARG
+    # no new token: nothing to do, whatever the buffers
+    none = Fake(counts=(0, 0, 0))
+    assert lib.stlite_paged_attention(none.ref, None, 1.0, None, None, 0, None) == S.OK
+    assert lib.stlite_paged_workspace_size(none.ref, ctypes.byref(n)) == S.OK and n.value == 0
+
+
+@needs_lib
+def test_append_rejections():
+    lib, f = S.load(), Fake()
+
+    def call(rope=None, positions=None, q=(FAKE, 28 * 128), k=(FAKE, 4 * 128), v=(FAKE, 4 * 128), q_norm=None, k_norm=None,
+             eps=1e-6, q_out=FAKE + 8192):
+        rows = [None if r is None else ctypes.byref(S._CRows(r[0], r[1], r[2] if len(r) > 2 else 3 * r[1])) for r in (q, k, v)]
+        return lib.stlite_paged_append(f.ref, None if rope is None else ctypes.byref(rope), positions, *rows, q_norm, k_norm,
+                                       eps, q_out, None)
+
+    def rope(theta=1e6, interleaved=0, n_axes=1, sections=(0, 0, 0), reserved=0):
+        return S._CRope(theta, interleaved, n_axes, (ctypes.c_int32 * 3)(*sections), reserved)
+
+    bad = S.ERR_INVALID_ARG
+    assert call(rope=rope()) == bad and call(positions=FAKE) == bad
+    for theta in (0.5, 0.0, -1.0, float("nan"), float("inf")):
+        assert call(rope=rope(theta=theta), positions=FAKE) == bad and "theta" in _err()
+    assert call(rope=rope(interleaved=2), positions=FAKE) == bad
+    assert call(rope=rope(reserved=1), positions=FAKE) == bad
+    assert call(rope=rope(n_axes=2), positions=FAKE) == bad and "n_axes" in _err()
+    for sections in ((16, 24, 23), (16, 24, 25), (-1, 33, 32), (2 ** 31 - 1, 1, 0)):
+        assert call(rope=rope(n_axes=3, sections=sections), positions=FAKE) == bad and "sections" in _err()
+    assert call(k=None) == bad and call(v=None) == bad and call(k=(None, 512)) == bad
+    assert call(q=None) == bad and call(q_out=None) == bad and call(q=(None, 28 * 128)) == bad
+    assert call(k=(FAKE + 8, 512)) == bad and call(k=(FAKE, 516)) == bad and call(k=(FAKE, 504)) == bad
+    assert call(q=(FAKE, 27 * 128)) == bad and call(v=(FAKE, 512, 4)) == bad and call(v=(FAKE, 512, -512)) == bad
+    assert call(q_out=FAKE) == bad and "alias" in _err()
+    assert call(q_out=FAKE + 8192 + 2) == bad and call(q_norm=FAKE + 2) == bad and call(k_norm=FAKE + 2) == bad
+    for eps in (-1e-6, float("nan"), float("inf")):
+        assert call(q_norm=FAKE, eps=eps) == bad and call(k_norm=FAKE, eps=eps) == bad and "eps" in _err()
+
+
+@needs_lib
+def test_compact_rejections():
+    lib = S.load()
+
+    def problem(n_layers=2, n_kv=4, lens=(50, 60)):
+        cu = np.concatenate([[0], np.cumsum(lens)])
+        return S.Problem(n_layers, 7 * n_kv, n_kv, 1, cu, np.zeros(len(lens) + 1), np.zeros((0, 3)), S.budgets(cu, 4, 5),
+                         device="cpu")
+
+    def call(p, f, k=FAKE, v=FAKE, kept=FAKE):
+        return lib.stlite_paged_compact(p.ref, f.ref, k, v, kept, 0, None)
+
+    bad = S.ERR_INVALID_ARG
+    for change, status, text in BAD:
+        assert call(problem(), Fake(**change)) == status and text in _err()
+    assert call(problem(n_layers=3), Fake()) == bad and "layers" in _err()
+    assert call(problem(n_kv=2), Fake()) == bad
+    assert call(problem(lens=(50,)), Fake()) == bad
+    assert call(problem(), Fake(max_len=47)) == bad and "keeps 48 rows" in _err()
+    for name in ("k", "v", "kept"):
+        assert call(problem(), Fake(), **{name: None}) == bad
+    assert call(problem(), Fake(), k=FAKE + 2) == bad
+    assert call(problem(), Fake(seq_lens=None)) == bad
+    p = problem()
+    p.c.window = 0
+    assert call(p, Fake()) == bad and "window" in _err()
+
+
+@needs_lib
+def test_validate_tables_and_lengths():
+    lib = S.load()
+    f = Fake(counts=(0, 1, 3), page_size=16, n_pages=6, max_pages=3, max_len=40)
+
+    def check(table, lens):
+        t, n = np.asarray(table, np.int32), np.asarray(lens, np.int32)
+        return lib.stlite_paged_validate(f.ref, t.ctypes.data, n.ctypes.data)
+
+    good = [[0, 1, 2], [5, 4, -1]]
+    assert check(good, [40, 32]) == S.OK
+    assert check(good, [40, 33]) == S.ERR_INVALID_ARG and "entry 2 is -1" in _err()
+    assert check([[0, 6, 2], [5, 4, 3]], [17, 2]) == S.ERR_INVALID_ARG and "outside [0, 6)" in _err()
+    assert check([[0, 6, 2], [5, 4, 3]], [16, 2]) == S.OK  # entries behind the end are not looked at
+    assert check(good, [41, 32]) == S.ERR_INVALID_ARG and check(good, [0, 32]) == S.ERR_INVALID_ARG
+    assert check(good, [1, 1]) == S.ERR_INVALID_ARG and "2 new tokens" in _err()
+    # a shared first page is fine, a shared page that is written to is not
+    assert check([[0, 1, 2], [0, 4, 3]], [40, 32]) == S.OK
+    assert check([[0, 1, 2], [0, 4, 3]], [16, 32]) == S.ERR_INVALID_ARG and "holds twice" in _err()
+    assert check([[0, 1, 1], [3, 4, 3]], [40, 32]) == S.ERR_INVALID_ARG
+    assert lib.stlite_paged_validate(f.ref, None, np.asarray([40, 32], np.int32).ctypes.data) == S.OK
+
+
+@needs_lib
+def test_workspace_does_not_depend_on_lengths_and_is_bounded():
+    """One new token per sequence, any batch: at most 512 shares x two parts of 16
+    heads; more: two parts of an item's rows for each share."""
+    lib = S.load()
+    n = ctypes.c_size_t(0)
+    per = 130 * 4  # a row's maximum, sum and 128 sums
+    for cu, rows, shares in (((0, 1, 2), 16, 512), ((0, 0, 1), 16, 512), ((0, 5, 6), 128, 512), ((0, 70, 71), 256, 256)):
+        f = Fake(counts=cu, n_layers=28, max_pages=10000, n_pages=10000, max_len=150000)
+        assert lib.stlite_paged_workspace_size(f.ref, ctypes.byref(n)) == S.OK
+        assert 0 < n.value <= shares * 2 * rows * per + 3 * 256, cu
+    tiny = Fake(counts=(0, 1), n_layers=1, n_q_heads=1, n_kv_heads=1, max_pages=1, max_len=16)
+    assert lib.stlite_paged_workspace_size(tiny.ref, ctypes.byref(n)) == S.OK and n.value == 0
+
+
+# ---------------------------------------------------------------------------
+# The binding
+# ---------------------------------------------------------------------------
+
+
+def _cache(**kw):
+    return P.PagedCache.alloc(2, 8, 2, 3, 40, page_size=16, device="cpu", **kw)
+
+
+def test_cache_layout():
+    c = _cache(dtype=torch.float16)
+    assert c.k.shape == (2, 2, 9, 16, 128) and c.max_pages == 3 and c.max_len == 40
+    assert c.page_table.tolist() == [[0, 1, 2], [3, 4, 5], [6, 7, 8]]
+    one = c.layer(1)
+    assert one.n_layers == 1 and one.k.data_ptr() == c.k[1].data_ptr() and one.seq_lens is c.seq_lens
+    with pytest.raises(ValueError):
+        c.layer(2)
+
+
+def test_binding_rejects_tensors():
+    c = _cache()
+    table, lens = c.page_table, c.seq_lens
+    for k, v, t, n in ((c.k.float(), c.v, table, lens), (c.k, c.v.half(), table, lens), (c.k, c.v[:1], table, lens),
+                       (c.k[..., :64], c.v[..., :64], table, lens), (c.k.transpose(0, 1), c.v.transpose(0, 1), table, lens),
+                       (c.k, c.v, table.long(), lens), (c.k, c.v, table[0], lens), (c.k, c.v, table.t(), lens),
+                       (c.k, c.v, table, lens[:2]), (c.k, c.v, table, lens.long())):
+        with pytest.raises(ValueError):
+            P.PagedCache(k, v, t, n, 8)
+    b = P.NewTokens([0, 1, 1, 4], device="cpu")
+    q = torch.zeros((2, 4, 8, 128), dtype=torch.bfloat16)
+    kn = torch.zeros((2, 4, 2, 128), dtype=torch.bfloat16)
+    for bad in (q.half(), q[:1], q[:, :3], q.transpose(1, 2), q.view(2, 4, 128, 8)):
+        with pytest.raises(ValueError):
+            P.paged_attention(c, b, bad)
+    with pytest.raises(ValueError):
+        P.paged_attention(c, b, q, out=q.float())
+    for bad in (kn.half(), kn[:, :3], kn[..., :64], torch.zeros((2, 4, 128, 2), dtype=torch.bfloat16).transpose(2, 3)):
+        with pytest.raises(ValueError):
+            P.paged_append(c, b, q, bad, kn)
+    pos = torch.zeros((1, 4), dtype=torch.int32)
+    for kw in (dict(positions=pos), dict(rope=P.Rope()), dict(positions=pos.long(), rope=P.Rope()),
+               dict(positions=pos, rope=P.Rope(sections=(16, 24, 24))), dict(q_norm=torch.zeros((2, 128))),
+               dict(k_norm=torch.zeros(128, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            P.paged_append(c, b, q, kn, kn, **kw)
+    for sections in ((64, 0), (16, 24, 23), (63,)):
+        with pytest.raises(ValueError):
+            P.Rope(sections=sections)
+    with pytest.raises(ValueError):
+        P.NewTokens([0], device="cpu")
+    with pytest.raises(ValueError):  # nothing runs on the CPU
+        P.paged_attention(c, b, q)
+
+
+@needs_lib
+def test_binding_raises_the_library_errors():
+    c = _cache()
+    with pytest.raises(ValueError):
+        c.workspace_size(P.NewTokens([0, 1, 1], device="cpu"))  # another number of sequences
+    with pytest.raises(S.StliteError) as e:
+        c.workspace_size(P.NewTokens([0, 1, 0, 4], device="cpu"))
+    assert e.value.status == S.ERR_INVALID_ARG
+    b = P.NewTokens([0, 1, 1, 4], device="cpu")
+    assert c.workspace_size(b) > 0
+    c.validate(b, c.page_table.numpy(), [1, 0, 3])
+    with pytest.raises(S.StliteError):
+        c.validate(b, c.page_table.numpy(), [1, 0, 2])
+    with pytest.raises(ValueError):
+        c.validate(b, c.page_table.numpy()[:, :2], [1, 0, 3])
+
+
+# ---------------------------------------------------------------------------
+# The oracle
+# ---------------------------------------------------------------------------
+
+
+def test_oracle_rotation_closed_forms():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((3, 2, 128))
+    assert np.array_equal(OP.rotate(x, [[0, 0, 0]], 1e4), x)
+    for inter in (False, True):
+        y = OP.rotate(x, [[5, 70000, -3]], 1e6, interleaved=inter)
+        assert np.allclose((y * y).sum(-1), (x * x).sum(-1))
+        a, b = (0, 1) if inter else (0, 64)  # pair 0 turns by the position itself
+        want = (x[1, 0, a] + 1j * x[1, 0, b]) * np.exp(1j * 70000)
+        assert np.allclose([y[1, 0, a], y[1, 0, b]], [want.real, want.imag])
+        # relative positions: a dot product depends on the difference alone
+        p, q = OP.rotate(x, [[7, 7, 7]], 1e4, interleaved=inter), OP.rotate(x[::-1], [[3, 3, 3]], 1e4, interleaved=inter)
+        r, s = OP.rotate(x, [[107] * 3], 1e4, interleaved=inter), OP.rotate(x[::-1], [[103] * 3], 1e4, interleaved=inter)
+        assert np.allclose((p * q).sum(-1), (r * s).sum(-1))
+    # three axes: equal positions are one axis; each section goes by its own
+    one = OP.rotate(x, [[4, 5, 6]], 1e4)
+    assert np.allclose(OP.rotate(x, [[4, 5, 6]] * 3, 1e4, (16, 24, 24)), one)
+    y = OP.rotate(x, [[4, 5, 6], [0, 0, 0], [0, 0, 0]], 1e4, (16, 24, 24))
+    assert np.allclose(y[..., :16], one[..., :16]) and np.array_equal(y[..., 16:64], x[..., 16:64])
+
+
+def test_oracle_norm_and_attention_closed_forms():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((4, 128))
+    y = OP.norm(x, np.ones(128), 0.0)
+    assert np.allclose((y * y).mean(-1), 1) and np.allclose(OP.norm(3 * x, 2 * np.ones(128), 0.0), 2 * y)
+    # zero queries: the mean of the visible rows, page by page; a bad page holds nothing
+    k = rng.standard_normal((1, 4, 16, 128))
+    v = rng.standard_normal((1, 4, 16, 128))
+    table = np.array([[2, 0], [3, -1]], np.int32)
+    q = np.zeros((3, 2, 128))
+    out, weight, keys, _ = OP.attention(q, k, v, table, [18, 20], [0, 2, 3], 32, 1.0, 2)
+    assert np.allclose(out[1, 0], np.concatenate([v[0, 2], v[0, 0, :2]]).mean(0))
+    assert np.allclose(out[0, 1], np.concatenate([v[0, 2], v[0, 0, :1]]).mean(0))
+    assert np.allclose(out[2, 0], v[0, 3].mean(0)) and keys[:, 0].tolist() == [17, 18, 16]
+    # a sequence shorter than its new tokens: the first see nothing; a length past max_len is cut
+    out, _, keys, _ = OP.attention(np.zeros((3, 1, 128)), k, v, table, [1, 99], [0, 2, 3], 16, 1.0, 1)
+    assert not out[0].any() and np.allclose(out[1, 0], v[0, 2, 0]) and keys[:, 0].tolist() == [0, 1, 16]
+    assert OP.new_places(table, [1, 99], [0, 2, 3], 16, 4, 16) == [None, 32, 63]
