@@ -64,7 +64,7 @@ struct PagedAttnArgs {
   float scale2;       // scale * log2(e)
   int32_t parts;      // head groups of a kv head (decode: 16 heads each; else 1)
   int32_t tokens;     // new tokens per item
-  int32_t rows;       // rows of an item's partial (decode 16, else 32 per wave)
+  int32_t rows;       // rows of an item's partial (decode 16, else 128 or 256)
   int32_t shares;     // work-groups
   int32_t min_share;  // keys
   float* pm;          // workspace [shares][2][rows]: max (log2 units)
@@ -75,7 +75,7 @@ struct PagedAttnArgs {
 hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream);
 hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
-hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, int32_t waves, hipStream_t stream);
+hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t stream);
 
 // ---------------------------------------------------------------------------
 // Device helpers
@@ -115,7 +115,9 @@ __device__ inline float elem_hi(uint32_t w) {
 }
 template <typename T>
 __device__ inline uint32_t elem_pack(float lo, float hi) {  // each rounded to nearest
-  return uint32_t(__builtin_bit_cast(uint16_t, T(lo))) | (uint32_t(__builtin_bit_cast(uint16_t, T(hi))) << 16);
+  typedef T pair_t __attribute__((ext_vector_type(2)));
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, pair_t));
 }
 
 __device__ inline int32_t paged_len(const PagedDev& c, int32_t s) { return min(max(c.seq_lens[s], 0), c.max_len); }

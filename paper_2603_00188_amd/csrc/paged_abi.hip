@@ -117,7 +117,7 @@ PagedDev device_view(const stlite_paged* c) {
 // How an attention call runs, from what the host knows (not the lengths).
 struct AttnPlan {
   bool decode;
-  int32_t waves, parts, tokens, rows, shares, min_share;
+  int32_t parts, tokens, rows, shares, min_share;
   size_t bytes;
 };
 
@@ -133,7 +133,6 @@ AttnPlan attn_plan(const stlite_paged* c) {
   p.decode = most <= 1;
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
   if (p.decode) {
-    p.waves = 4;
     p.parts = int32_t(ceil_div(group, 16));
     p.tokens = 1;
     p.rows = 16;
@@ -141,11 +140,10 @@ AttnPlan attn_plan(const stlite_paged* c) {
     p.min_share = 64;
     items *= p.parts * live;
   } else {
-    p.waves = most * group <= 128 ? 4 : 8;
     p.parts = 1;
-    p.rows = 32 * p.waves;
+    p.rows = most * group <= 128 ? 128 : 256;
     p.tokens = int32_t(p.rows / group);
-    p.shares = p.waves == 8 ? 256 : 512;
+    p.shares = 256;
     p.min_share = 256;
     int64_t blocks = 0;
     for (int32_t s = 0; s < c->n_seqs; ++s) blocks += ceil_div(int64_t(c->h_cu_new[s + 1]) - c->h_cu_new[s], p.tokens);
@@ -336,7 +334,7 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.po = a.pl + align_up(slots * sizeof(float)) / sizeof(float);
   const bool half = c->dtype == STLITE_FP16;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return hip_status(p.decode ? launch_paged_decode(a, half, s) : launch_paged_extend(a, half, p.waves, s),
+  return hip_status(p.decode ? launch_paged_decode(a, half, s) : launch_paged_extend(a, half, s),
                     "paged_attention launch");
 }
 

@@ -2,7 +2,7 @@
 //   out_t = sum_{j <= m_t} softmax_j(scale q_t . k_j) v_j,   m_t = len - n + t,
 // in two forms, by the number of new tokens per sequence, and the launch that
 // joins the parts of items that several work-groups share.
-#include <type_traits>
+#include <float.h>
 
 #include "paged_plan.h"
 #include "tile_lds.h"
@@ -35,6 +35,33 @@ struct PageWindow {
     bad = __ballot(!ok);
   }
   __device__ int32_t page(int32_t entry) const { return __builtin_amdgcn_readlane(held, entry & 63); }
+  __device__ bool is_bad(int32_t entry) const { return (bad >> (entry & 63)) & 1; }
+};
+
+// The same with the entries in LDS, 64 words of this wave's own: a register held
+// through a long loop is dear in the several-token kernel.
+struct LdsPageWindow {
+  const int32_t* row;
+  int32_t n_pages, last, base;
+  uint64_t bad;
+  uint32_t at;
+
+  __device__ LdsPageWindow(const PagedDev& c, int32_t seq, uint32_t lds)
+      : row(c.page_table + int64_t(seq) * c.max_pages), n_pages(c.n_pages), last(c.max_pages - 1), base(-1), bad(0), at(lds) {}
+
+  __device__ void seek(int32_t entry) {
+    if ((entry & ~63) == base) return;
+    base = entry & ~63;
+    const int32_t lane = threadIdx.x & 63;
+    const int32_t e = row[min(base + lane, last)];
+    const bool ok = e >= 0 && e < n_pages;
+    *reinterpret_cast<volatile __attribute__((address_space(3))) int32_t*>((uintptr_t)(at + lane * 4)) = ok ? e : 0;
+    bad = __ballot(!ok);
+  }
+  __device__ int32_t page(int32_t entry) const {
+    return __builtin_amdgcn_readfirstlane(
+        *reinterpret_cast<const volatile __attribute__((address_space(3))) int32_t*>((uintptr_t)(at + (entry & 63) * 4)));
+  }
   __device__ bool is_bad(int32_t entry) const { return (bad >> (entry & 63)) & 1; }
 };
 
@@ -218,10 +245,12 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // ---------------------------------------------------------------------------
 //
 // An item's rows (token-major, all query heads of the kv head) are cut into
-// blocks of 32, one per wave; the work-group streams 64-key tiles of K and V
-// through a ring in LDS (direct DMA).  Everything is transposed, so that a lane
-// owns one query (column lane & 31; two lanes share it, each with half the keys)
-// and the softmax needs no exchange but one swap:
+// blocks of 32; eight waves stream 64-key tiles of K and V through rings in LDS
+// (direct DMA).  KB = 2: eight blocks, a wave takes all 64 keys of a tile for its
+// block; KB = 1, for at most 128 rows: four blocks, two waves take 32 keys each and
+// are merged behind the last tile.  Everything is transposed, so that a lane owns
+// one query (column lane & 31; two lanes share it, each with half the keys) and the
+// softmax needs no exchange but one swap:
 //   S^T = K Q^T      32x32x16, A: K rows from LDS, B: queries in registers;
 //   P^T              exp2 of the accumulators, packed where they are: register
 //                    order is a permutation of the keys within 16, which the V
@@ -229,12 +258,22 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 //   O^T += V^T P^T   A: V read transposed from LDS (ds_read_b64_tr_b16).
 // The running maximum moves only when a tile exceeds it by 2^kLazy, so that the
 // output is rescaled rarely.
+//
+// A step of a wave has two halves: its products (the logits of tile t + 1, the
+// values of tile t) and its vector work (the weights of tile t + 1, the DMA).  The
+// two waves of a SIMD, w and w + 4, are half a step apart, so that one's products
+// run under the other's vector work; a barrier ends each half.  At the end of its
+// products in step t a wave waits for its part of K(t+2) and V(t+1), so both have
+// landed for everybody when anyone's step t + 1 begins; K(t) and V(t-1) are free
+// once both waves are through their products of step t - 1, which is when the
+// vector half of step t fetches K(t+4) and V(t+3) into their places.
 
 constexpr float kLazy = 8.0f;
-constexpr int kExtTile = kPagedTile;
-constexpr int kTileBytes = kExtTile * kHeadDim * 2;
-
-typedef __attribute__((address_space(3))) u32x2_t* lds_u32x2_t;
+constexpr int kExtWaves = 8;
+constexpr int kRing = 4;
+constexpr int kTileBytes = kPagedTile * kHeadDim * 2;
+constexpr int kTileLoads = 16 / kExtWaves;         // DMA instructions of a wave per tile of K or V
+constexpr int kWaveKeys = kPagedTile / kExtWaves;  // keys of a tile that a wave fetches: they lie in one page
 
 // Four keys of one dimension per lane: each group of 16 lanes reads 4 rows of 16
 // elements (lane i: row i >> 2, elements 4 (i & 3) ..) and gets them transposed.
@@ -244,41 +283,59 @@ __device__ inline u32x2_t read_transposed(uint32_t lds) {
   return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr_t)(uintptr_t)lds));
 }
 
-template <typename T, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void paged_extend_kernel(PagedAttnArgs a) {
+// 16 bytes per lane from offset `at` + `from` of a buffer to LDS address `to` + 16
+// lane.  In assembly because the compiler, which cannot tell the tiles apart, would
+// wait for every load in flight before each transposed read; it has no output
+// register, and wait_vmcnt counts it.  (The nops: M0 is read one wait state after
+// it is written, a scalar that the vector unit wrote, as a page read from LDS is,
+// five.)
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+__device__ inline void dma16(i32x4_t rsrc, uint32_t to, uint32_t at, uint32_t from) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(at), "s"(rsrc), "s"(from), "s"(to)
+               : "memory");
+}
+
+template <typename T, int KB>
+__global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
-  constexpr int NT = NW * 64;
-  constexpr int kStages = NW == 8 ? 3 : 2;
-  constexpr int kRows = NW * 32;
-  constexpr int kLoads = 2 * 16 / NW;  // DMA instructions of a wave per tile
-  __shared__ __align__(1024) uint16_t sm_tiles[kStages * 2 * kTileBytes / 2];  // [stage][K, V][64][128]
+  constexpr int NT = kExtWaves * 64;
+  constexpr int kBlocks = 4 * KB, kRows = kBlocks * 32;
+  __shared__ __align__(1024) uint16_t sm_tiles[2 * kRing * kTileBytes / 2];  // K, then V: [slot][64][128]
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
+  __shared__ int32_t sm_pages[kExtWaves][64];
+  __shared__ float sm_ml[KB == 1 ? kBlocks : 1][2][32];  // a merged wave's maxima and sums
   const PagedDev& c = a.c;
   PagedPlan<NT> plan(a, sm_plan);
   int64_t x = int64_t(blockIdx.x) * plan.share;
   const int64_t y = min(x + plan.share, plan.total);
   if (x >= y) return;
   PagedItem it = plan.find(x);
+  const int64_t share = plan.share;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = wave >> 2;                      // half a step apart
+  const int block = KB == 2 ? wave : wave & 3;      // of 32 rows
+  const int first_key = KB == 2 ? 0 : 32 * group;   // of a tile
   const int col = lane & 31, h = lane >> 5;
   const int32_t in_page = (1 << c.page_shift) - 1;
   const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>(sm_tiles));
   // K: chunk (16 bytes) q of key k lies at slot q ^ (k & 15): 16 keys' reads of
   // one chunk take 16 slots.  V: at slot q ^ (4 (k & 3) + (k >> 2 & 3)): a
-  // transposed read of 4 keys x 32 dimensions takes all 16 slots.
-  uint32_t k_at[8], v_at[4][2];
-#pragma unroll
-  for (int kk = 0; kk < 8; ++kk) k_at[kk] = col * 256 + (((2 * kk + h) ^ (col & 15)) << 4);
-#pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int i = lane & 15;
-      const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-      v_at[db][r] = kTileBytes + (8 * r + 4 * h + (i >> 2)) * 256 + ((chunk ^ (4 * (i >> 2) + 2 * r + h)) << 4) + (i & 1) * 8;
-    }
+  // transposed read of 4 keys x 32 dimensions takes all 16 slots.  Either way the
+  // chunk's number enters an address by exclusive or alone, so one address per
+  // lane gives all of them.
+  const uint32_t k_lane = lds0 + (first_key + col) * 256 + ((h ^ (col & 15)) << 4);
+  uint32_t v_lane;
+  {
+    const int i = lane & 15, c0 = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+    v_lane = lds0 + kRing * kTileBytes + (first_key + 4 * h + (i >> 2)) * 256 + ((4 * (i >> 2) + (c0 ^ h)) << 4) + (i & 1) * 8;
+  }
+  // DMA load g brings keys 4 g + (lane >> 4) of the wave's eight: a lane's row and
+  // the chunk that belongs in its 16 bytes (+ 1024 g, ^ 64 g or ^ 16 g).
+  const int key0 = wave * kWaveKeys;
+  const uint32_t k_dma = (lane >> 4) * 256 + (((lane & 15) ^ (key0 & 15) ^ (lane >> 4)) << 4);
+  const uint32_t v_dma = (lane >> 4) * 256 + (((lane & 15) ^ (4 * (lane >> 4)) ^ ((key0 >> 2) & 3)) << 4);
 
   for (;;) {
     const int unit = it.unit;
@@ -287,98 +344,154 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_extend_kernel(PagedAttnArgs 
     const bool whole = span.whole;
     const int32_t tok0 = it.index * a.tokens, toks = min(it.n - tok0, a.tokens);
     const int32_t rows = toks * c.group;
-    const int32_t seen = max(it.cached + tok0 + toks, 0);  // keys that the last token sees
-    const int32_t t0 = span.t0, t1 = min(span.t1, (seen + kPagedTile - 1) / kPagedTile);
-    // This lane's query (rows past the item's repeat the last one).
-    const int32_t row = min(wave * 32 + col, rows - 1);
-    const int32_t tok = row / c.group, head = row - tok * c.group;
+    // (the same on every lane, kept in scalar registers for the tiles' addresses)
+    const int32_t seen = __builtin_amdgcn_readfirstlane(max(it.cached + tok0 + toks, 0));  // keys that the last token sees
+    const int32_t t0 = __builtin_amdgcn_readfirstlane(span.t0);
+    const int32_t t1 = __builtin_amdgcn_readfirstlane(min(span.t1, (seen + kPagedTile - 1) / kPagedTile));
+    // This lane's query (a row past the item's repeats the last one).
+    const int32_t row = min(block * 32 + col, rows - 1), tok = row / c.group;
+    const int64_t qrow = (int64_t(layer) * c.total_new + it.row0 + tok0 + tok) * c.n_q_heads + int64_t(kv) * c.group +
+                         (row - tok * c.group);
     const int32_t limit = it.cached + tok0 + tok;  // last key that it sees
-    const int64_t qrow = (int64_t(layer) * c.total_new + it.row0 + tok0 + tok) * c.n_q_heads + int64_t(kv) * c.group + head;
-    const bool live = wave * 32 < rows;
-    const int32_t limit_lo = __builtin_amdgcn_readfirstlane(limit);
-    const int32_t limit_hi = __builtin_amdgcn_readlane(limit, 31);
-
     x8 qf[8];
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk)
       qf[kk] = __builtin_bit_cast(x8, *reinterpret_cast<const u32x4_t*>(a.q + qrow * kHeadDim + kk * 16 + h * 8));
-    float m_ref = -INFINITY, l_run = 0.0f;
+    const int32_t limit_lo = __builtin_amdgcn_readfirstlane(limit);
+    // last tile of this wave; none where its rows are past the item's
+    const int32_t t_last =
+        block * 32 < rows ? min((__builtin_amdgcn_readlane(limit, 31) - first_key) >> 6, t1 - 1) : -1;
+
+    float m_ref = -FLT_MAX, l_run = 0.0f;  // (finite: no difference of infinities while no key was seen)
     f32x16_t o[4];
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
+    for (int db = 0; db < 4; ++db) o[db] = f32x16_t{};
+    int32_t odd_lo = t1, odd_hi = -1;  // masked tiles whose values are not all finite
 
-    PageWindow pages(c, it.seq);
-    // Bad 16-key groups of tile t, which the window holds (bit g: keys 16 g .. 16 g + 15).
-    auto bad_groups = [&](int32_t t) {
-      if (pages.bad == 0) return 0u;
-      uint32_t m = 0;
+    // --- tiles into the rings ---
+    LdsPageWindow pages(c, it.seq, uint32_t(reinterpret_cast<uintptr_t>(sm_pages[wave])));
+    const int32_t last = t1 - 1;
+    int32_t k_page = 0;            // the page of this wave's keys in the K tile last fetched
+    uint32_t bad[kRing + 1] = {};  // bad 16-key groups of tiles t .. t + kRing
+    auto entry_of = [&](int32_t t, int32_t key) { return min(min(t, last) * kPagedTile + key, seen - 1) >> c.page_shift; };
+    auto fetch = [&](const uint16_t* pool, int32_t page, int32_t t, uint32_t dst, uint32_t at, uint32_t swizzle) {
+      const int64_t base = PagedPlan<NT>::uniform(page_row(c, unit, page) * kHeadDim);
+      const uint64_t from = reinterpret_cast<uint64_t>(pool + base);
+      const i32x4_t rsrc = {int32_t(uint32_t(from)), int32_t(uint32_t(from >> 32) & 0xffffu), (in_page + 1) * (kHeadDim * 2), kBufferFlags};
+      const int32_t key = t * kPagedTile + key0;
+      const uint32_t d = __builtin_amdgcn_readfirstlane(dst + wave * (kTileBytes / kExtWaves));
+      if (t < last) {
+        const uint32_t off = __builtin_amdgcn_readfirstlane(uint32_t(key & in_page) * (kHeadDim * 2));
 #pragma unroll
-      for (int g = 0; g < 4; ++g) m |= uint32_t(pages.is_bad(min((t * kExtTile + 16 * g) >> c.page_shift, c.max_pages - 1))) << g;
-      return m;
-    };
-
-    auto issue = [&](int32_t t, int stage) {
-      const int32_t first_entry = (t * kExtTile) >> c.page_shift;
-      pages.seek(first_entry);
-      // this wave's keys lie in one page
-      const int32_t key0 = t * kExtTile + wave * (kExtTile / NW);
-      const int32_t entry = min(key0, seen - 1) >> c.page_shift;
-      const int64_t base = page_row(c, unit, pages.page(entry)) * kHeadDim;
-      const __amdgpu_buffer_rsrc_t kr =
-          __builtin_amdgcn_make_buffer_rsrc(c.k + base, 0, (in_page + 1) * (kHeadDim * 2), kBufferFlags);
-      const __amdgpu_buffer_rsrc_t vr =
-          __builtin_amdgcn_make_buffer_rsrc(c.v + base, 0, (in_page + 1) * (kHeadDim * 2), kBufferFlags);
-      const uint32_t dst0 = lds0 + stage * (2 * kTileBytes) + wave * (kTileBytes / NW);
+        for (int g = 0; g < kTileLoads; ++g) {
+          dma16(rsrc, d + g * 1024, at ^ (g * swizzle), off + g * 1024);
+        }
+      } else {  // the last tile: keys past the end repeat the last one
 #pragma unroll
-      for (int g = 0; g < kLoads / 2; ++g) {
-        const int32_t kl = wave * (kExtTile / NW) + 4 * g + (lane >> 4);  // key within the tile
-        const uint32_t r = uint32_t(min(t * kExtTile + kl, seen - 1) & in_page) * (kHeadDim * 2);
-        const uint32_t kc = uint32_t((lane & 15) ^ (kl & 15)) * 16u;
-        const uint32_t vc = uint32_t((lane & 15) ^ (4 * (kl & 3) + ((kl >> 2) & 3))) * 16u;
-        uint32_t kd = dst0 + g * 1024, vd = kd + kTileBytes;
-        asm volatile("" : "+s"(kd), "+s"(vd));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void_t)(uintptr_t)kd, 16, r + kc, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void_t)(uintptr_t)vd, 16, r + vc, 0, 0, 0);
-      }
-      return bad_groups(t);
-    };
-
-    auto tile = [&](int32_t t, int stage, auto masked, uint32_t bad) {
-      constexpr bool kMasked = decltype(masked)::value;
-      const uint32_t base = lds0 + stage * (2 * kTileBytes);
-      f32x16_t s[2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const x8 kf = *reinterpret_cast<const __attribute__((address_space(3))) x8*>((uintptr_t)(base + k_at[kk] + kb * 8192));
-          s[kb] = E::mfma32(kf, qf[kk], s[kb]);
+        for (int g = 0; g < kTileLoads; ++g) {
+          const uint32_t r = uint32_t(min(key + 4 * g + (lane >> 4), seen - 1) & in_page) * (kHeadDim * 2);
+          dma16(rsrc, d + g * 1024, r + ((at ^ (g * swizzle)) & 255), 0);
         }
       }
-      if (kMasked) {
+    };
+    // K of tile t; returns its bad groups.  Behind the last tile that one is fetched
+    // again, into a slot that nobody reads any more: every step then waits for the
+    // same number of loads.
+    auto fetch_k = [&](int32_t t) {
+      pages.seek(entry_of(t, 0));
+      k_page = pages.page(entry_of(t, key0));
+      fetch(c.k, k_page, min(t, last), lds0 + ((t - t0) & (kRing - 1)) * kTileBytes, k_dma, 64);
+      uint32_t m = 0;
+      if (pages.bad)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int g = 0; g < 4; ++g) m |= uint32_t(pages.is_bad(entry_of(t, 16 * g))) << g;
+      return m;
+    };
+    auto fetch_v = [&](int32_t t, int32_t page) {
+      fetch(c.v, page, min(t, last), lds0 + (kRing + ((t - t0) & (kRing - 1))) * kTileBytes, v_dma, 16);
+    };
+
+    // --- one tile's arithmetic ---
+    auto full = [&](int32_t t, uint32_t b) { return b == 0 && t * kPagedTile + kPagedTile - 1 <= limit_lo; };
+    auto slot = [&](int32_t t) { return uint32_t((t - t0) & (kRing - 1)) * kTileBytes; };
+    auto read_k = [&](uint32_t at, int i) {  // keys 32 (i / 8) .., dimensions 16 (i % 8) .. (at: k_lane + slot)
+      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)((at ^ (i % 8 << 5)) + i / 8 * 8192));
+    };
+    auto read_v = [&](uint32_t at, int i) {  // keys 16 (i / 4) .., dimensions 32 (i % 4) .. (at: v_lane + slot)
+      const u32x2_t lo = read_transposed((at ^ (i % 4 << 6)) + i / 4 * 4096);
+      const u32x2_t hi = read_transposed((at ^ (i % 4 << 6) ^ 32) + i / 4 * 4096 + 2048);
+      return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+    };
+    f32x16_t s[KB];     // logits of the tile ahead
+    u32x4_t w[2 * KB];  // weights of the tile: eight keys of this lane to each 16
+    auto product = [&](int i, u32x4_t kf) {
+      s[i / 8] = E::mfma32(__builtin_bit_cast(x8, kf), qf[i % 8], i % 8 == 0 ? f32x16_t{} : s[i / 8]);
+    };
+    auto add = [&](int i, u32x4_t vf) {
+      o[i & 3] = E::mfma32(__builtin_bit_cast(x8, vf), __builtin_bit_cast(x8, w[i >> 2]), o[i & 3]);
+    };
+    constexpr int kSteps = 8 * KB;  // products of the logits, and of the values
+    constexpr int kAhead = 3;       // reads run that many products ahead
+
+    // The products of step t with everything in view.
+    auto products = [&](int32_t t) {
+      const uint32_t k_at = k_lane + slot(t + 1), v_at = v_lane + slot(t);
+      u32x4_t f[kAhead + 1];
+#pragma unroll
+      for (int i = -kAhead; i < 2 * kSteps; ++i) {
+        const int n = i + kAhead;
+        if (n < kSteps) f[n % (kAhead + 1)] = read_k(k_at, n);
+        else if (n < 2 * kSteps) f[n % (kAhead + 1)] = read_v(v_at, n - kSteps);
+        if (i < 0) continue;
+        if (i < kSteps) product(i, f[i % (kAhead + 1)]);
+        else add(i - kSteps, f[i % (kAhead + 1)]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // The values of tile t where some are masked: 0 * infinity is no zero, so what
+    // is not finite is left out of the product and reaches the queries that see it
+    // behind the last tile.
+    auto masked_values = [&](int32_t t) {
+      const uint32_t v_at = v_lane + slot(t);
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        u32x4_t vf = read_v(v_at, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t nf = E::not_finite(vf[j]);
+          odd |= nf;
+          vf[j] &= ~((nf >> 15) * 0xffffu);
+        }
+        add(i, vf);
+      }
+      if (__ballot(odd != 0)) {
+        odd_lo = min(odd_lo, t);
+        odd_hi = t;
+      }
+    };
+    // The weights of tile t from its logits.
+    auto weigh = [&](int32_t t, uint32_t b) {
+      if (!full(t, b)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int32_t key = t * kExtTile + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-            if (key > limit || ((bad >> (2 * kb + (i >> 3))) & 1)) s[kb][i] = -INFINITY;
+            const int32_t in_tile = first_key + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
+            if (t * kPagedTile + in_tile > limit || ((b >> (first_key / 16 + 2 * kb + (i >> 3))) & 1)) s[kb][i] = -INFINITY;
           }
       }
-      float mt = s[0][0];
+      float mt = fmaxf(s[0][0], s[KB - 1][1]);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kb][i]);
+        for (int i = 0; i < 16; i += 2) mt = fmaxf(fmaxf(mt, s[kb][i]), s[kb][i + 1]);
       float other = mt;
       swap32(mt, other);
       mt = fmaxf(mt, other) * a.scale2;
       if (__ballot(mt > m_ref + kLazy + E::kBias)) {
         const float m_new = fmaxf(m_ref, mt - E::kBias);
-        const float alpha = m_ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+        const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
         m_ref = m_new;
         l_run *= alpha;
 #pragma unroll
@@ -386,86 +499,109 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_extend_kernel(PagedAttnArgs 
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
       }
-      const float minus_m = m_ref == -INFINITY ? 0.0f : -m_ref;
-      x8 pf[4];
+      float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        u32x4_t w;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][8 * (kk & 1) + j], a.scale2, minus_m));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][8 * (kk & 1) + j + 1], a.scale2, minus_m));
-          l_run += p0 + p1;
-          w[j >> 1] = elem_pack<T>(p0, p1);
-        }
-        pf[kk] = __builtin_bit_cast(x8, w);
+      for (int n = 0; n < 8 * KB; ++n) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][2 * n & 15], a.scale2, -m_ref));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][(2 * n & 15) + 1], a.scale2, -m_ref));
+        sum[0] += p0;
+        sum[1] += p1;
+        w[n >> 2][n & 3] = elem_pack<T>(p0, p1);
       }
-      uint32_t odd = 0;
-#pragma unroll
-      for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const u32x2_t lo = read_transposed(base + v_at[db][0] + kk * 4096);
-          const u32x2_t hi = read_transposed(base + v_at[db][1] + kk * 4096);
-          u32x4_t w = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
-          if (kMasked) {
-            // 0 * infinity is no zero: what is not finite is left out here
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t nf = E::not_finite(w[j]);
-              odd |= nf;
-              w[j] &= ~((nf >> 15) * 0xffffu);
-            }
-          }
-          o[db] = E::mfma32(__builtin_bit_cast(x8, w), pf[kk], o[db]);
-        }
-      if (kMasked && __ballot(odd != 0)) {
-        // and reaches the queries that see it here: p v is v, for v infinite or NaN
-#pragma unroll 1
-        for (int32_t kl = 0; kl < kExtTile; ++kl) {
-          const int32_t key = t * kExtTile + kl;
-          if (key >= seen || ((bad >> (kl >> 4)) & 1)) continue;
-          const uint32_t swz = 4 * (kl & 3) + ((kl >> 2) & 3);
-#pragma unroll
-          for (int db = 0; db < 4; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const uint32_t dim = 32 * db + 8 * (i >> 2) + 4 * h + (i & 3);
-              const uint32_t at = base + kTileBytes + kl * 256 + (((dim >> 3) ^ swz) << 4) + (dim & 7) * 2;
-              const uint16_t e = *reinterpret_cast<const __attribute__((address_space(3))) uint16_t*>((uintptr_t)at);
-              if (E::not_finite(e) && key <= limit) o[db][i] += elem_lo<T>(e);
-            }
-        }
-      }
+      l_run += sum[0] + sum[1];
     };
 
     __syncthreads();  // the last item's tiles have been read
-    // (stores of the last item and loads so far must not count among the DMAs)
-    wait_vmcnt<0>();
-    uint32_t bad[kStages - 1] = {};  // of the tiles in flight
+    wait_vmcnt<0>();  // (the queries must not count among the DMAs)
+    if (t0 < t1) {
+      // K(t0) | K(t0+1), V(t0) | K(t0+2), V(t0+1); then a step fetches one of each
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i)
-      if (t0 + i < t1) bad[i] = issue(t0 + i, i);
-    int stage = 0;
-    for (int32_t t = t0; t < t1; ++t) {
-      if (kStages == 3 && t + 1 < t1) wait_vmcnt<kLoads>();
-      else wait_vmcnt<0>();
-      barrier_lds();
-      const uint32_t bad_now = bad[0];
-#pragma unroll
-      for (int i = 0; i + 1 < kStages - 1; ++i) bad[i] = bad[i + 1];
-      if (t + kStages - 1 < t1) bad[kStages - 2] = issue(t + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
-      if (live && t * kExtTile <= limit_hi) {
-        if (bad_now || t * kExtTile + kExtTile - 1 > limit_lo) tile(t, stage, std::true_type{}, bad_now);
-        else tile(t, stage, std::false_type{}, 0u);
+      for (int i = 0; i < kRing - 1; ++i) {
+        const int32_t page = k_page;
+        bad[i + 1] = fetch_k(t0 + i);
+        if (i > 0) fetch_v(t0 + i - 1, page);
       }
-      stage = stage + 1 == kStages ? 0 : stage + 1;
+      wait_vmcnt<2 * kTileLoads * (kRing - 2)>();
+      barrier_lds();
+      if (group) barrier_lds();
+      for (int32_t t = t0 - 1; t < t1; ++t) {
+        // bad: of tiles t .. t + kRing - 1
+        if (t >= t0 && t < t_last && full(t, bad[0])) {
+          products(t);
+        } else {
+          if (t < t_last) {
+            const uint32_t k_at = k_lane + slot(t + 1);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) product(i, read_k(k_at, i));
+          }
+          if (t >= t0 && t <= t_last) masked_values(t);
+        }
+        wait_vmcnt<2 * kTileLoads>();
+        barrier_lds();
+        if (t < t_last) weigh(t + 1, bad[1]);
+        const int32_t page = k_page;
+        bad[kRing] = fetch_k(t + kRing);
+        fetch_v(t + kRing - 1, page);
+#pragma unroll
+        for (int i = 0; i < kRing; ++i) bad[i] = bad[i + 1];
+        barrier_lds();
+      }
+      if (!group) barrier_lds();
+      wait_vmcnt<0>();  // no DMA may outlive the tiles that it writes
+    }
+    // Values of masked tiles that are not finite: p v is v for them, whatever the
+    // weight, and what is infinite or NaN already stays so.
+#pragma unroll 1
+    for (int32_t key = odd_lo * kPagedTile; key < min((odd_hi + 1) * kPagedTile, seen); ++key) {
+      pages.seek(key >> c.page_shift);
+      if (pages.is_bad(key >> c.page_shift)) continue;
+      if (KB == 1 && (key & 32) != first_key) continue;
+      const uint16_t* vr = c.v + (page_row(c, unit, pages.page(key >> c.page_shift)) + (key & in_page)) * kHeadDim + 4 * h;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const u32x2_t e = *reinterpret_cast<const u32x2_t*>(vr + 32 * db + 8 * g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t bits = e[j >> 1] >> (16 * (j & 1)) & 0xffffu;
+            o[db][4 * g + j] += E::not_finite(bits) && key <= limit ? elem_lo<T>(bits) : 0.0f;
+          }
+        }
     }
 
     float other = l_run;
     swap32(l_run, other);
     l_run += other;
-    if (wave * 32 + col < rows) {
+    if constexpr (KB == 1) {
+      // The second group's half of the keys joins the first's, through the tiles.
+      f32x4_t* sm_o = reinterpret_cast<f32x4_t*>(sm_tiles) + block * 1024 + lane;  // [16][64 lanes]
+      __syncthreads();
+      if (group) {
+#pragma unroll
+        for (int g = 0; g < 16; ++g)
+          sm_o[g * 64] = f32x4_t{o[g >> 2][4 * (g & 3)], o[g >> 2][4 * (g & 3) + 1], o[g >> 2][4 * (g & 3) + 2],
+                                 o[g >> 2][4 * (g & 3) + 3]};
+        if (h == 0) {
+          sm_ml[block][0][col] = m_ref;
+          sm_ml[block][1][col] = l_run;
+        }
+      }
+      __syncthreads();
+      if (!group) {
+        const float m1 = sm_ml[block][0][col], m = fmaxf(m_ref, m1);
+        const float f0 = __builtin_amdgcn_exp2f(m_ref - m), f1 = __builtin_amdgcn_exp2f(m1 - m);
+        m_ref = m;
+        l_run = l_run * f0 + sm_ml[block][1][col] * f1;
+#pragma unroll
+        for (int g = 0; g < 16; ++g) {
+          const f32x4_t p = sm_o[g * 64];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[g >> 2][4 * (g & 3) + j] = o[g >> 2][4 * (g & 3) + j] * f0 + p[j] * f1;
+        }
+      }
+    }
+    if (block * 32 + col < rows && (KB == 2 || !group)) {
       if (whole) {
         const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
         uint16_t* p = a.out + qrow * kHeadDim + 4 * h;
@@ -473,14 +609,14 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_extend_kernel(PagedAttnArgs 
         for (int db = 0; db < 4; ++db)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            u32x2_t w;
-            w[0] = elem_pack<T>(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
-            w[1] = elem_pack<T>(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
-            *reinterpret_cast<u32x2_t*>(p + 32 * db + 8 * g) = w;
+            u32x2_t e;
+            e[0] = elem_pack<T>(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
+            e[1] = elem_pack<T>(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
+            *reinterpret_cast<u32x2_t*>(p + 32 * db + 8 * g) = e;
           }
       } else {
-        const int64_t slot = paged_slot(blockIdx.x, plan.share, it.start) * kRows + wave * 32 + col;
-        float* p = a.po + slot * kHeadDim + 4 * h;
+        const int64_t at = paged_slot(blockIdx.x, share, it.start) * kRows + block * 32 + col;
+        float* p = a.po + at * kHeadDim + 4 * h;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -488,8 +624,8 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_extend_kernel(PagedAttnArgs 
             *reinterpret_cast<f32x4_t*>(p + 32 * db + 8 * g) =
                 f32x4_t{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
         if (h == 0) {
-          a.pm[slot] = m_ref;
-          a.pl[slot] = l_run;
+          a.pm[at] = m_ref;
+          a.pl[at] = l_run;
         }
       }
     }
@@ -590,9 +726,9 @@ hipError_t decode(const PagedAttnArgs& a, hipStream_t stream) {
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }
 
-template <typename T, int NW>
+template <typename T, int KB>
 hipError_t extend(const PagedAttnArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_extend_kernel<T, NW>), dim3(a.shares), dim3(NW * 64), 0, stream, a);
+  hipLaunchKernelGGL((paged_extend_kernel<T, KB>), dim3(a.shares), dim3(kExtWaves * 64), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }
@@ -603,9 +739,9 @@ hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t st
   return half ? decode<_Float16>(a, stream) : decode<__bf16>(a, stream);
 }
 
-hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, int32_t waves, hipStream_t stream) {
-  if (half) return waves == 8 ? extend<_Float16, 8>(a, stream) : extend<_Float16, 4>(a, stream);
-  return waves == 8 ? extend<__bf16, 8>(a, stream) : extend<__bf16, 4>(a, stream);
+hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t stream) {
+  if (half) return a.rows == 256 ? extend<_Float16, 2>(a, stream) : extend<_Float16, 1>(a, stream);
+  return a.rows == 256 ? extend<__bf16, 2>(a, stream) : extend<__bf16, 1>(a, stream);
 }
 
 }  // namespace stlite
