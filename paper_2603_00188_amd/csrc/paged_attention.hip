@@ -58,10 +58,11 @@ struct LdsPageWindow {
     *reinterpret_cast<volatile __attribute__((address_space(3))) int32_t*>((uintptr_t)(at + lane * 4)) = ok ? e : 0;
     bad = __ballot(!ok);
   }
-  __device__ int32_t page(int32_t entry) const {
-    return __builtin_amdgcn_readfirstlane(
-        *reinterpret_cast<const volatile __attribute__((address_space(3))) int32_t*>((uintptr_t)(at + (entry & 63) * 4)));
+  // The page on every lane (a read that the caller need not wait for yet).
+  __device__ int32_t peek(int32_t entry) const {
+    return *reinterpret_cast<const volatile __attribute__((address_space(3))) int32_t*>((uintptr_t)(at + (entry & 63) * 4));
   }
+  __device__ int32_t page(int32_t entry) const { return __builtin_amdgcn_readfirstlane(peek(entry)); }
   __device__ bool is_bad(int32_t entry) const { return (bad >> (entry & 63)) & 1; }
 };
 
@@ -260,20 +261,20 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // output is rescaled rarely.
 //
 // A step of a wave has two halves: its products (the logits of tile t + 1, the
-// values of tile t) and its vector work (the weights of tile t + 1, the DMA).  The
+// values of tile t) and its vector work (the weights of tile t + 1, and DMA).  The
 // two waves of a SIMD, w and w + 4, are half a step apart, so that one's products
-// run under the other's vector work; a barrier ends each half.  At the end of its
-// products in step t a wave waits for its part of K(t+2) and V(t+1), so both have
-// landed for everybody when anyone's step t + 1 begins; K(t) and V(t-1) are free
-// once both waves are through their products of step t - 1, which is when the
-// vector half of step t fetches K(t+4) and V(t+3) into their places.
+// run under the other's vector work; a barrier ends each half.  Waves 0 - 3 fetch K,
+// 4 - 7 V, into rings of four tiles: in the vector half of its step t the first group
+// fetches K(t+4) in place of K(t), the second V(t+3) in place of V(t-1), and both
+// groups' products of step t - 1, the last readers, are done by then.  At the end of
+// its products a wave waits for all but its last tile's DMA, so that K(t+1) and V(t)
+// have landed for everybody when anyone's step t begins.
 
 constexpr float kLazy = 8.0f;
 constexpr int kExtWaves = 8;
 constexpr int kRing = 4;
 constexpr int kTileBytes = kPagedTile * kHeadDim * 2;
-constexpr int kTileLoads = 16 / kExtWaves;         // DMA instructions of a wave per tile of K or V
-constexpr int kWaveKeys = kPagedTile / kExtWaves;  // keys of a tile that a wave fetches: they lie in one page
+constexpr int kTileLoads = 4;  // DMA instructions of a wave per tile: it fetches 16 keys, which lie in one page
 
 // Four keys of one dimension per lane: each group of 16 lanes reads 4 rows of 16
 // elements (lane i: row i >> 2, elements 4 (i & 3) ..) and gets them transposed.
@@ -304,6 +305,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   __shared__ __align__(1024) uint16_t sm_tiles[2 * kRing * kTileBytes / 2];  // K, then V: [slot][64][128]
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
   __shared__ int32_t sm_pages[kExtWaves][64];
+  __shared__ int2 sm_odd[kExtWaves];
   __shared__ float sm_ml[KB == 1 ? kBlocks : 1][2][32];  // a merged wave's maxima and sums
   const PagedDev& c = a.c;
   PagedPlan<NT> plan(a, sm_plan);
@@ -331,11 +333,13 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     const int i = lane & 15, c0 = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
     v_lane = lds0 + kRing * kTileBytes + (first_key + 4 * h + (i >> 2)) * 256 + ((4 * (i >> 2) + (c0 ^ h)) << 4) + (i & 1) * 8;
   }
-  // DMA load g brings keys 4 g + (lane >> 4) of the wave's eight: a lane's row and
+  // DMA load g brings keys 4 g + (lane >> 4) of the wave's sixteen: a lane's row and
   // the chunk that belongs in its 16 bytes (+ 1024 g, ^ 64 g or ^ 16 g).
-  const int key0 = wave * kWaveKeys;
-  const uint32_t k_dma = (lane >> 4) * 256 + (((lane & 15) ^ (key0 & 15) ^ (lane >> 4)) << 4);
-  const uint32_t v_dma = (lane >> 4) * 256 + (((lane & 15) ^ (4 * (lane >> 4)) ^ ((key0 >> 2) & 3)) << 4);
+  const int key0 = 16 * (wave & 3);
+  const uint32_t dma_lane = (lane >> 4) * 256 + (((lane & 15) ^ (group ? 4 * (lane >> 4) : lane >> 4)) << 4);
+  const uint32_t dma_swizzle = group ? 16 : 64;
+  const uint16_t* const pool = group ? c.v : c.k;
+  const uint32_t dma_lds = lds0 + (group * kRing * kPagedTile + key0) * (kHeadDim * 2);
 
   for (;;) {
     const int unit = it.unit;
@@ -366,56 +370,51 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     f32x16_t o[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db) o[db] = f32x16_t{};
-    int32_t odd_lo = t1, odd_hi = -1;  // masked tiles whose values are not all finite
+    int32_t odd_lo = t1, odd_hi = -1;  // masked tiles whose values were not all finite
 
     // --- tiles into the rings ---
     LdsPageWindow pages(c, it.seq, uint32_t(reinterpret_cast<uintptr_t>(sm_pages[wave])));
     const int32_t last = t1 - 1;
-    int32_t k_page = 0;            // the page of this wave's keys in the K tile last fetched
-    uint32_t bad[kRing + 1] = {};  // bad 16-key groups of tiles t .. t + kRing
     auto entry_of = [&](int32_t t, int32_t key) { return min(min(t, last) * kPagedTile + key, seen - 1) >> c.page_shift; };
-    auto fetch = [&](const uint16_t* pool, int32_t page, int32_t t, uint32_t dst, uint32_t at, uint32_t swizzle) {
-      const int64_t base = PagedPlan<NT>::uniform(page_row(c, unit, page) * kHeadDim);
-      const uint64_t from = reinterpret_cast<uint64_t>(pool + base);
+    // This group's next tile t.  Behind the last tile that one is fetched again, into
+    // a slot that nobody reads any more: every step then waits for the same number of
+    // loads.  The page is read one tile ahead.
+    int32_t ahead = 0;
+    auto look = [&](int32_t t) {
+      pages.seek(entry_of(t, 0));
+      ahead = pages.peek(entry_of(t, key0));
+    };
+    auto fetch = [&](int32_t t) {  // returns the tile's bad 16-key groups
+      const uint64_t from =
+          uint64_t(PagedPlan<NT>::uniform(reinterpret_cast<int64_t>(pool + page_row(c, unit, __builtin_amdgcn_readfirstlane(ahead)) * kHeadDim)));
       const i32x4_t rsrc = {int32_t(uint32_t(from)), int32_t(uint32_t(from >> 32) & 0xffffu), (in_page + 1) * (kHeadDim * 2), kBufferFlags};
-      const int32_t key = t * kPagedTile + key0;
-      const uint32_t d = __builtin_amdgcn_readfirstlane(dst + wave * (kTileBytes / kExtWaves));
+      const int32_t key = min(t, last) * kPagedTile + key0;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(dma_lds + ((t - t0) & (kRing - 1)) * kTileBytes);
       if (t < last) {
         const uint32_t off = __builtin_amdgcn_readfirstlane(uint32_t(key & in_page) * (kHeadDim * 2));
 #pragma unroll
-        for (int g = 0; g < kTileLoads; ++g) {
-          dma16(rsrc, d + g * 1024, at ^ (g * swizzle), off + g * 1024);
-        }
+        for (int g = 0; g < kTileLoads; ++g) dma16(rsrc, to + g * 1024, dma_lane ^ (g * dma_swizzle), off + g * 1024);
       } else {  // the last tile: keys past the end repeat the last one
 #pragma unroll
         for (int g = 0; g < kTileLoads; ++g) {
           const uint32_t r = uint32_t(min(key + 4 * g + (lane >> 4), seen - 1) & in_page) * (kHeadDim * 2);
-          dma16(rsrc, d + g * 1024, r + ((at ^ (g * swizzle)) & 255), 0);
+          dma16(rsrc, to + g * 1024, r + ((dma_lane ^ (g * dma_swizzle)) & 255), 0);
         }
       }
-    };
-    // K of tile t; returns its bad groups.  Behind the last tile that one is fetched
-    // again, into a slot that nobody reads any more: every step then waits for the
-    // same number of loads.
-    auto fetch_k = [&](int32_t t) {
-      pages.seek(entry_of(t, 0));
-      k_page = pages.page(entry_of(t, key0));
-      fetch(c.k, k_page, min(t, last), lds0 + ((t - t0) & (kRing - 1)) * kTileBytes, k_dma, 64);
       uint32_t m = 0;
       if (pages.bad)
 #pragma unroll
         for (int g = 0; g < 4; ++g) m |= uint32_t(pages.is_bad(entry_of(t, 16 * g))) << g;
+      look(t + 1);
       return m;
-    };
-    auto fetch_v = [&](int32_t t, int32_t page) {
-      fetch(c.v, page, min(t, last), lds0 + (kRing + ((t - t0) & (kRing - 1))) * kTileBytes, v_dma, 16);
     };
 
     // --- one tile's arithmetic ---
-    auto full = [&](int32_t t, uint32_t b) { return b == 0 && t * kPagedTile + kPagedTile - 1 <= limit_lo; };
+    auto full = [&](int32_t t, uint32_t b, int32_t first) { return b == 0 && t * kPagedTile + kPagedTile - 1 <= first; };
     auto slot = [&](int32_t t) { return uint32_t((t - t0) & (kRing - 1)) * kTileBytes; };
-    auto read_k = [&](uint32_t at, int i) {  // keys 32 (i / 8) .., dimensions 16 (i % 8) .. (at: k_lane + slot)
-      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)((at ^ (i % 8 << 5)) + i / 8 * 8192));
+    // (the 32-key blocks in turn: a product does not wait for the one before it)
+    auto read_k = [&](uint32_t at, int i) {  // keys 32 (i % KB) .., dimensions 16 (i / KB) .. (at: k_lane + slot)
+      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)((at ^ (i / KB << 5)) + i % KB * 8192));
     };
     auto read_v = [&](uint32_t at, int i) {  // keys 16 (i / 4) .., dimensions 32 (i % 4) .. (at: v_lane + slot)
       const u32x2_t lo = read_transposed((at ^ (i % 4 << 6)) + i / 4 * 4096);
@@ -425,7 +424,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     f32x16_t s[KB];     // logits of the tile ahead
     u32x4_t w[2 * KB];  // weights of the tile: eight keys of this lane to each 16
     auto product = [&](int i, u32x4_t kf) {
-      s[i / 8] = E::mfma32(__builtin_bit_cast(x8, kf), qf[i % 8], i % 8 == 0 ? f32x16_t{} : s[i / 8]);
+      s[i % KB] = E::mfma32(__builtin_bit_cast(x8, kf), qf[i / KB], i < KB ? f32x16_t{} : s[i % KB]);
     };
     auto add = [&](int i, u32x4_t vf) {
       o[i & 3] = E::mfma32(__builtin_bit_cast(x8, vf), __builtin_bit_cast(x8, w[i >> 2]), o[i & 3]);
@@ -433,7 +432,8 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     constexpr int kSteps = 8 * KB;  // products of the logits, and of the values
     constexpr int kAhead = 3;       // reads run that many products ahead
 
-    // The products of step t with everything in view.
+    // The products of step t.  (Behind the wave's last tile the logits are of
+    // whatever lies in the slot; nobody looks at them.)
     auto products = [&](int32_t t) {
       const uint32_t k_at = k_lane + slot(t + 1), v_at = v_lane + slot(t);
       u32x4_t f[kAhead + 1];
@@ -448,31 +448,31 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // The values of tile t where some are masked: 0 * infinity is no zero, so what
-    // is not finite is left out of the product and reaches the queries that see it
-    // behind the last tile.
-    auto masked_values = [&](int32_t t) {
-      const uint32_t v_at = v_lane + slot(t);
-      uint32_t odd = 0;
+    // 0 * infinity is no zero: in a tile where some queries do not see every key,
+    // values that are not finite are cleared as soon as they have landed, by the wave
+    // that fetched them, and reach the queries that see them behind the last tile.
+    auto clean_values = [&](int32_t t) {
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        u32x4_t vf = read_v(v_at, i);
+      for (int g = 0; g < kTileLoads; ++g) {
+        auto* p = reinterpret_cast<__attribute__((address_space(3))) u32x4_t*>((uintptr_t)(dma_lds + slot(t) + g * 1024 + lane * 16));
+        u32x4_t e = *p;
+        uint32_t odd = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t nf = E::not_finite(vf[j]);
+          const uint32_t nf = E::not_finite(e[j]);
           odd |= nf;
-          vf[j] &= ~((nf >> 15) * 0xffffu);
+          e[j] &= ~((nf >> 15) * 0xffffu);
         }
-        add(i, vf);
-      }
-      if (__ballot(odd != 0)) {
-        odd_lo = min(odd_lo, t);
-        odd_hi = t;
+        if (__ballot(odd != 0)) {
+          *p = e;
+          odd_lo = min(odd_lo, t);
+          odd_hi = t;
+        }
       }
     };
     // The weights of tile t from its logits.
     auto weigh = [&](int32_t t, uint32_t b) {
-      if (!full(t, b)) {
+      if (!full(t, b, limit_lo)) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -512,45 +512,54 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     };
 
     __syncthreads();  // the last item's tiles have been read
-    wait_vmcnt<0>();  // (the queries must not count among the DMAs)
     if (t0 < t1) {
-      // K(t0) | K(t0+1), V(t0) | K(t0+2), V(t0+1); then a step fetches one of each
+      look(t0);
+      // (the queries have come with the page: no later wait for them drains the DMA)
 #pragma unroll
-      for (int i = 0; i < kRing - 1; ++i) {
-        const int32_t page = k_page;
-        bad[i + 1] = fetch_k(t0 + i);
-        if (i > 0) fetch_v(t0 + i - 1, page);
-      }
-      wait_vmcnt<2 * kTileLoads * (kRing - 2)>();
+      for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));
+      // K(t0), K(t0+1), K(t0+2) and V(t0), V(t0+1); then a step fetches one of each
+      uint32_t bad = 0;  // bad 16-key groups of tiles t, t + 1, ..: four bits each
+#pragma unroll
+      for (int i = 0; i < kRing - 1; ++i)
+        if (i < kRing - 1 - group) bad |= fetch(t0 + i) << (4 * (i + 1));
+      wait_vmcnt<2 * kTileLoads>();
       barrier_lds();
       if (group) barrier_lds();
-      for (int32_t t = t0 - 1; t < t1; ++t) {
-        // bad: of tiles t .. t + kRing - 1
-        if (t >= t0 && t < t_last && full(t, bad[0])) {
-          products(t);
-        } else {
-          if (t < t_last) {
-            const uint32_t k_at = k_lane + slot(t + 1);
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) product(i, read_k(k_at, i));
-          }
-          if (t >= t0 && t <= t_last) masked_values(t);
-        }
-        wait_vmcnt<2 * kTileLoads>();
+      // What ends the products of step t: this wave's part of the tiles of step t + 1.
+      auto landed = [&](int32_t t) {
+        wait_vmcnt<kTileLoads>();
+        if (group && t + 1 < t1 && !full(t + 1, (bad >> 4) & 15, it.cached + tok0)) clean_values(t + 1);
         barrier_lds();
-        if (t < t_last) weigh(t + 1, bad[1]);
-        const int32_t page = k_page;
-        bad[kRing] = fetch_k(t + kRing);
-        fetch_v(t + kRing - 1, page);
-#pragma unroll
-        for (int i = 0; i < kRing; ++i) bad[i] = bad[i + 1];
+      };
+      auto vector_half = [&](int32_t t) {
+        if (t < t_last) weigh(t + 1, (bad >> 4) & 15);
+        bad = (bad | (fetch(t + kRing - group) << (4 * (kRing - group)))) >> 4;
         barrier_lds();
+      };
+      if (t0 <= t_last) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) product(i, read_k(k_lane, i));
+      }
+      landed(t0 - 1);
+      vector_half(t0 - 1);
+      for (int32_t t = t0; t < t1; ++t) {
+        if (t <= t_last) products(t);
+        landed(t);
+        vector_half(t);
       }
       if (!group) barrier_lds();
       wait_vmcnt<0>();  // no DMA may outlive the tiles that it writes
     }
-    // Values of masked tiles that are not finite: p v is v for them, whatever the
-    // weight, and what is infinite or NaN already stays so.
+    // All waves learn which tiles had values cleared.
+    if (lane == 0) sm_odd[wave] = make_int2(odd_lo, odd_hi);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kExtWaves; ++i) {
+      odd_lo = min(odd_lo, __builtin_amdgcn_readfirstlane(sm_odd[i].x));
+      odd_hi = max(odd_hi, __builtin_amdgcn_readfirstlane(sm_odd[i].y));
+    }
+    // The values that were cleared: p v is v for them, whatever the weight, and what
+    // is infinite or NaN already stays so.
 #pragma unroll 1
     for (int32_t key = odd_lo * kPagedTile; key < min((odd_hi + 1) * kPagedTile, seen); ++key) {
       pages.seek(key >> c.page_shift);
