@@ -67,6 +67,8 @@ struct PagedAttnArgs {
   int32_t rows;       // rows of an item's partial (decode 16, else 128 or 256)
   int32_t shares;     // work-groups
   int32_t min_share;  // keys
+  int32_t join_items; // joining by item: their number; 0: by boundary
+  int32_t join_rows;  // rows of an item per joining work-group
   float* pm;          // workspace [shares][2][rows]: max (log2 units)
   float* pl;          // workspace [shares][2][rows]: sum
   float* po;          // workspace [shares][2][rows][d]: O, unnormalised

@@ -117,7 +117,7 @@ PagedDev device_view(const stlite_paged* c) {
 // How an attention call runs, from what the host knows (not the lengths).
 struct AttnPlan {
   bool decode;
-  int32_t parts, tokens, rows, shares, min_share;
+  int32_t parts, tokens, rows, shares, min_share, join_items, join_rows;
   size_t bytes;
 };
 
@@ -152,6 +152,11 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // (no more shares than the longest possible range fills)
   const double keys = double(items) * c->max_len;
   p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(keys / p.min_share))));
+  // Joining: one round of work-groups (two per CU) where the items are few; else a
+  // work-group per boundary, which for several tokens takes half an item's rows.
+  const int64_t item_rows = p.decode ? std::min<int64_t>(group, 16) : p.tokens * group;
+  p.join_items = c->n_seqs == 1 && items < p.shares ? int32_t(items) : 0;
+  p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : p.decode ? 16 : 128;
   const size_t slots = size_t(p.shares) * 2 * p.rows;
   p.bytes = p.shares == 1 ? 0 : 2 * align_up(slots * sizeof(float)) + align_up(slots * kHeadDim * sizeof(float));
   return p;
@@ -328,6 +333,8 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.rows = p.rows;
   a.shares = p.shares;
   a.min_share = p.min_share;
+  a.join_items = p.join_items;
+  a.join_rows = p.join_rows;
   const size_t slots = size_t(p.shares) * 2 * p.rows;
   a.pm = static_cast<float*>(ws);
   a.pl = a.pm + align_up(slots * sizeof(float)) / sizeof(float);

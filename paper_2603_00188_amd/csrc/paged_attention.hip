@@ -648,83 +648,105 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 // Joining the parts
 // ---------------------------------------------------------------------------
 //
-// Work-group (w, z) joins the rows 8 z .. 8 z + 7 of the item that the boundary
-// between shares w and w + 1 cuts, if w is the first share in it: 32 lanes x 4
-// dimensions per part, 8 parts at a time.
-constexpr int kJoinRows = 8;
+// A work-group joins up to join_rows rows of an item: the item that the boundary
+// between shares x and x + 1 cuts, if x is the first share in it, or with join_items
+// (one sequence, fewer items than shares) item x.  32 lanes x 4 dimensions hold a row;
+// its parts (two mostly, up to all shares for one token over a long cache) are spread
+// over as many of the 32 groups as the rows leave.  Latency is all there is to it, so
+// kBatch parts are loaded at once.
+constexpr int kBatch = 4;
+constexpr int kJoinGroups = 32;
+
+struct Joined {
+  float m = -INFINITY, l = 0.0f;
+  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  __device__ void add(float pm, float pl, f32x4_t po) {
+    if (pm == -INFINITY) return;
+    const float mx = fmaxf(m, pm);
+    const float f = __builtin_amdgcn_exp2f(m - mx), g = __builtin_amdgcn_exp2f(pm - mx);
+    l = l * f + pl * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = o[i] * f + po[i] * g;
+    m = mx;
+  }
+};
 
 template <typename T>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
-  __shared__ float sm_m[8], sm_l[8];
-  __shared__ f32x4_t sm_o[8][32];
-  __shared__ typename PagedPlan<256>::Shared sm_plan;
+__global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnArgs a) {
+  constexpr int NT = kJoinGroups * 32;
+  __shared__ float sm_m[kJoinGroups], sm_l[kJoinGroups];
+  __shared__ f32x4_t sm_o[kJoinGroups][32];
+  __shared__ typename PagedPlan<NT>::Shared sm_plan;
   const PagedDev& c = a.c;
-  PagedPlan<256> plan(a, sm_plan);
-  const int64_t cut = (int64_t(blockIdx.x) + 1) * plan.share;
-  if (cut >= plan.total) return;
-  const PagedItem it = plan.find(cut);
-  if (it.start == cut || it.start / plan.share != int64_t(blockIdx.x)) return;
-  const int32_t w0 = blockIdx.x, w1 = int32_t((it.start + it.keys - 1) / plan.share);
+  PagedPlan<NT> plan(a, sm_plan);
+  PagedItem it;
+  if (a.join_items) {
+    it = plan.item(blockIdx.x);
+  } else {
+    const int64_t cut = (int64_t(blockIdx.x) + 1) * plan.share;
+    if (cut >= plan.total) return;
+    it = plan.find(cut);
+    if (it.start == cut || it.start / plan.share != int64_t(blockIdx.x)) return;
+  }
+  const int32_t w0 = int32_t(it.start / plan.share), w1 = int32_t((it.start + it.keys - 1) / plan.share);
+  if (w0 == w1) return;
   const int unit = it.unit / a.parts, part = it.unit % a.parts;
   const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
   const int32_t tok0 = it.index * a.tokens;
   const int32_t head0 = part * kDecHeads;  // (one part but for decode)
   const int32_t rows = a.parts > 1 ? min(c.group - head0, kDecHeads) : min(it.n - tok0, a.tokens) * c.group;
   const int grp = threadIdx.x >> 5, l32 = threadIdx.x & 31;
-  for (int32_t row = blockIdx.y * kJoinRows; row < min(rows, int32_t(blockIdx.y + 1) * kJoinRows); ++row) {
-    float M = -INFINITY, L = 0.0f;
-    f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int32_t w = w0 + grp; w <= w1; w += 8) {
-      const int64_t slot = paged_slot(w, plan.share, it.start) * a.rows + row;
-      const float m = a.pm[slot];
-      if (m == -INFINITY) continue;
-      const float l = a.pl[slot];
-      const f32x4_t o = *reinterpret_cast<const f32x4_t*>(a.po + slot * kHeadDim + 4 * l32);
-      const float mx = fmaxf(M, m);
-      const float f = __builtin_amdgcn_exp2f(M - mx), g = __builtin_amdgcn_exp2f(m - mx);
-      L = L * f + l * g;
+  for (int32_t row0 = blockIdx.y * a.join_rows; row0 < min(rows, int32_t(blockIdx.y + 1) * a.join_rows); row0 += kJoinGroups) {
+    const int32_t here = min(min(rows, int32_t(blockIdx.y + 1) * a.join_rows) - row0, kJoinGroups);
+    const int per_row = kJoinGroups / here;  // groups per row
+    const int32_t row = row0 + grp / per_row, step = per_row;
+    Joined r;
+    if (row < row0 + here)
+      for (int32_t w = w0 + grp % per_row; w <= w1; w += kBatch * step) {
+        float m[kBatch], l[kBatch];
+        f32x4_t o[kBatch];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) O[i] = O[i] * f + o[i] * g;
-      M = mx;
-    }
-    __syncthreads();
-    sm_o[grp][l32] = O;
-    if (l32 == 0) {
-      sm_m[grp] = M;
-      sm_l[grp] = L;
-    }
-    __syncthreads();
-    if (grp == 0) {
-      float mx = -INFINITY;
+        for (int i = 0; i < kBatch; ++i) {  // (past the last: that one again, left out)
+          const int64_t slot = paged_slot(min(w + i * step, w1), plan.share, it.start) * a.rows + row;
+          m[i] = a.pm[slot];
+          l[i] = a.pl[slot];
+          o[i] = *reinterpret_cast<const f32x4_t*>(a.po + slot * kHeadDim + 4 * l32);
+        }
 #pragma unroll
-      for (int g = 0; g < 8; ++g) mx = fmaxf(mx, sm_m[g]);
-      L = 0.0f;
-      O = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        const float f = sm_m[g] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[g] - mx);
-        L += f * sm_l[g];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) O[i] += f * sm_o[g][l32][i];
+        for (int i = 0; i < kBatch; ++i) r.add(w + i * step <= w1 ? m[i] : -INFINITY, l[i], o[i]);
       }
-      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-      const int32_t tok = row / c.group;
-      const int64_t orow = a.parts > 1 ? (int64_t(layer) * c.total_new + it.row0) * c.n_q_heads + int64_t(kv) * c.group + head0 + row
-                                       : (int64_t(layer) * c.total_new + it.row0 + tok0 + tok) * c.n_q_heads +
-                                             int64_t(kv) * c.group + (row - tok * c.group);
-      u32x2_t w;
-      w[0] = elem_pack<T>(O[0] * inv, O[1] * inv);
-      w[1] = elem_pack<T>(O[2] * inv, O[3] * inv);
-      *reinterpret_cast<u32x2_t*>(a.out + orow * kHeadDim + 4 * l32) = w;
+    if (per_row > 1) {
+      __syncthreads();
+      sm_o[grp][l32] = r.o;
+      if (l32 == 0) {
+        sm_m[grp] = r.m;
+        sm_l[grp] = r.l;
+      }
+      __syncthreads();
+      if (grp % per_row == 0)
+        for (int g = 1; g < per_row; ++g) r.add(sm_m[grp + g], sm_l[grp + g], sm_o[grp + g][l32]);
     }
+    if (grp % per_row != 0 || row >= row0 + here) continue;
+    const float inv = r.l == 0.0f ? 0.0f : 1.0f / r.l;
+    const int32_t tok = row / c.group;  // (decode: 0 with one part; with more, row is a head)
+    const int64_t orow = a.parts > 1 ? (int64_t(layer) * c.total_new + it.row0) * c.n_q_heads + int64_t(kv) * c.group + head0 + row
+                                     : (int64_t(layer) * c.total_new + it.row0 + tok0 + tok) * c.n_q_heads +
+                                           int64_t(kv) * c.group + (row - tok * c.group);
+    u32x2_t e;
+    e[0] = elem_pack<T>(r.o[0] * inv, r.o[1] * inv);
+    e[1] = elem_pack<T>(r.o[2] * inv, r.o[3] * inv);
+    *reinterpret_cast<u32x2_t*>(a.out + orow * kHeadDim + 4 * l32) = e;
   }
 }
 
 template <typename T>
 hipError_t launch_join(const PagedAttnArgs& a, hipStream_t stream) {
   if (a.shares < 2) return hipSuccess;
-  const int32_t rows = a.parts > 1 ? kDecHeads : a.tokens * a.c.group;
-  hipLaunchKernelGGL((paged_join_kernel<T>), dim3(a.shares - 1, (rows + kJoinRows - 1) / kJoinRows), dim3(256), 0, stream, a);
+  const int32_t rows = a.rows == kDecHeads ? min(a.c.group, kDecHeads) : a.tokens * a.c.group;
+  hipLaunchKernelGGL((paged_join_kernel<T>), dim3(a.join_items ? a.join_items : a.shares - 1, (rows + a.join_rows - 1) / a.join_rows),
+                     dim3(kJoinGroups * 32),
+                     0, stream, a);
   return hipGetLastError();
 }
 

@@ -34,28 +34,35 @@ struct PagedPlan {
   }
 
   __device__ PagedPlan(const PagedAttnArgs& args, Shared& shared) : a(args), sh(shared) {
-    const int32_t per = (a.c.n_seqs + NT - 1) / NT;
-    s0 = min(int32_t(threadIdx.x) * per, a.c.n_seqs);
-    s1 = min(s0 + per, a.c.n_seqs);
-    mine = 0;
-    for (int32_t s = s0; s < s1; ++s) mine += keys_of(s);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t sum = mine;
+    if (a.c.n_seqs == 1) {  // one trajectory: nothing to search
+      s0 = 0;
+      s1 = 1;
+      before = 0;
+      mine = per_unit = uniform(keys_of(0));
+    } else {
+      const int32_t per = (a.c.n_seqs + NT - 1) / NT;
+      s0 = min(int32_t(threadIdx.x) * per, a.c.n_seqs);
+      s1 = min(s0 + per, a.c.n_seqs);
+      mine = 0;
+      for (int32_t s = s0; s < s1; ++s) mine += keys_of(s);
+      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+      int64_t sum = mine;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t up = __shfl_up(sum, d);
-      if (lane >= d) sum += up;
-    }
-    if (lane == 63) sh.wave[wave] = sum;
-    __syncthreads();
-    before = sum - mine;
-    per_unit = 0;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int64_t up = __shfl_up(sum, d);
+        if (lane >= d) sum += up;
+      }
+      if (lane == 63) sh.wave[wave] = sum;
+      __syncthreads();
+      before = sum - mine;
+      per_unit = 0;
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-      if (w < wave) before += sh.wave[w];
-      per_unit += sh.wave[w];
+      for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) before += sh.wave[w];
+        per_unit += sh.wave[w];
+      }
+      per_unit = uniform(per_unit);
     }
-    per_unit = uniform(per_unit);
     total = per_unit * a.c.n_units * a.parts;
     share = paged_share(total, a.shares, a.min_share);
   }
@@ -70,6 +77,16 @@ struct PagedPlan {
   // work-group calls).
   __device__ PagedItem find(int64_t x) {
     const int64_t unit = x / per_unit, rem = x - unit * per_unit;
+    PagedItem it;
+    it.unit = int32_t(unit);
+    if (a.c.n_seqs == 1) {
+      it.seq = 0;
+      load_seq(it);
+      it.index = paged_item_of(rem, it.n, it.cached, a.tokens);
+      it.start = unit * per_unit + paged_prefix(it.index, it.cached, a.tokens);
+      set_keys(it);
+      return it;
+    }
     __syncthreads();
     if (mine > 0 && rem >= before && rem < before + mine) {
       int64_t b = before;
@@ -83,13 +100,24 @@ struct PagedPlan {
       sh.base = b;
     }
     __syncthreads();
-    PagedItem it;
-    it.unit = int32_t(unit);
     it.seq = __builtin_amdgcn_readfirstlane(sh.seq);
     const int64_t base = uniform(sh.base), in = rem - base;
     load_seq(it);
     it.index = paged_item_of(in, it.n, it.cached, a.tokens);
     it.start = unit * per_unit + base + paged_prefix(it.index, it.cached, a.tokens);
+    set_keys(it);
+    return it;
+  }
+
+  // Item i of a call with one sequence.
+  __device__ PagedItem item(int32_t i) const {
+    PagedItem it;
+    it.seq = 0;
+    load_seq(it);
+    const int32_t items = paged_items(it.n, a.tokens);
+    it.unit = i / items;
+    it.index = i % items;
+    it.start = it.unit * per_unit + paged_prefix(it.index, it.cached, a.tokens);
     set_keys(it);
     return it;
   }
