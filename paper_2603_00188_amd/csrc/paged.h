@@ -47,13 +47,13 @@ struct PagedAppendArgs {
   double turns[64];      // theta^(-i/64) / (2 pi): turns of pair i per position
 };
 
-// Attention runs as a flat range of keys, cut into equal shares.  The queries of
+// Attention runs as a flat range of places, cut into equal shares.  The queries of
 // a (unit, sequence) are cut into items of `tokens` new tokens (all heads of the
 // kv head: tokens * group rows; decode: one token, at most 16 heads); item i of a
 // sequence with n new tokens behind c cached ones counts c + min((i + 1) tokens,
-// n) keys, what its last token sees.  Items lie one after another, units
-// outermost; work-group w takes the keys [w share, (w + 1) share) of that range.
-// A share that holds a whole item writes its output; the parts of an item that
+// n) keys, what its last token sees, and takes item_cost places before them.  Items
+// lie one after another, units outermost; work-group w takes the keys in [w share,
+// (w + 1) share) of that range.  A share that holds a whole item writes its output; the parts of an item that
 // several shares cut leave (max, sum, O) in the workspace and are joined by a
 // second launch.  The lengths are read on the device only, so the grid does not
 // depend on them.
@@ -66,7 +66,8 @@ struct PagedAttnArgs {
   int32_t tokens;     // new tokens per item
   int32_t rows;       // rows of an item's partial (decode 16, else 128 or 256)
   int32_t shares;     // work-groups
-  int32_t min_share;  // keys
+  int32_t min_share;  // places
+  int32_t item_cost;  // places that beginning an item takes
   int32_t join_items; // joining by item: their number; 0: by boundary
   int32_t join_rows;  // rows of an item per joining work-group
   float* pm;          // workspace [shares][2][rows]: max (log2 units)

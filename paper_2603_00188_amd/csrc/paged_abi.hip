@@ -115,9 +115,15 @@ PagedDev device_view(const stlite_paged* c) {
 }
 
 // How an attention call runs, from what the host knows (not the lengths).
+//
+// item_cost: a work-group's queries, first page and tiles, unequal limits and output
+// take it as long as six tiles of several tokens, or four sub-tiles of one.  Counted
+// as none / as here, and flat within 1 % from half to twice that: 5 prompts of 131 to
+// 2999 tokens 324 / 219 us, 5 drafted tokens in each of 16 sequences 69.6 / 64, one
+// token of one layer 17 / 14.4; a screen behind 30k tokens and a step's decoding alike.
 struct AttnPlan {
   bool decode;
-  int32_t parts, tokens, rows, shares, min_share, join_items, join_rows;
+  int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows;
   size_t bytes;
 };
 
@@ -138,6 +144,7 @@ AttnPlan attn_plan(const stlite_paged* c) {
     p.rows = 16;
     p.shares = 512;
     p.min_share = 64;
+    p.item_cost = 64;
     items *= p.parts * live;
   } else {
     p.parts = 1;
@@ -145,13 +152,15 @@ AttnPlan attn_plan(const stlite_paged* c) {
     p.tokens = int32_t(p.rows / group);
     p.shares = 256;
     p.min_share = 256;
+    p.item_cost = 384;
     int64_t blocks = 0;
     for (int32_t s = 0; s < c->n_seqs; ++s) blocks += ceil_div(int64_t(c->h_cu_new[s + 1]) - c->h_cu_new[s], p.tokens);
     items *= blocks;
   }
+  if (items == 1) p.item_cost = 0;  // nothing to balance
   // (no more shares than the longest possible range fills)
-  const double keys = double(items) * c->max_len;
-  p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(keys / p.min_share))));
+  const double range = double(items) * (double(c->max_len) + p.item_cost);
+  p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(range / p.min_share))));
   // Joining: one round of work-groups (two per CU) where the items are few; else a
   // work-group per boundary, which for several tokens takes half an item's rows.
   const int64_t item_rows = p.decode ? std::min<int64_t>(group, 16) : p.tokens * group;
@@ -333,6 +342,7 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.rows = p.rows;
   a.shares = p.shares;
   a.min_share = p.min_share;
+  a.item_cost = p.item_cost;
   a.join_items = p.join_items;
   a.join_rows = p.join_rows;
   const size_t slots = size_t(p.shares) * 2 * p.rows;

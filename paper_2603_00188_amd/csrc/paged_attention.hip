@@ -97,6 +97,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
   const int64_t y = min(x + plan.share, plan.total);
   if (x >= y) return;
   PagedItem it = plan.find(x);
+  if (it.start >= y) return;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = lane & 15, quad = lane >> 4;
@@ -238,6 +239,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
     x = span.end;
     if (x >= y) break;
     plan.next(it);
+    if (it.start >= y) break;
   }
 }
 
@@ -313,6 +315,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   const int64_t y = min(x + plan.share, plan.total);
   if (x >= y) return;
   PagedItem it = plan.find(x);
+  if (it.start >= y) return;
   const int64_t share = plan.share;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -641,6 +644,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     x = span.end;
     if (x >= y) break;
     plan.next(it);
+    if (it.start >= y) break;
   }
 }
 
@@ -687,7 +691,7 @@ __global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnA
     const int64_t cut = (int64_t(blockIdx.x) + 1) * plan.share;
     if (cut >= plan.total) return;
     it = plan.find(cut);
-    if (it.start == cut || it.start / plan.share != int64_t(blockIdx.x)) return;
+    if (it.start >= cut || it.start / plan.share != int64_t(blockIdx.x)) return;
   }
   const int32_t w0 = int32_t(it.start / plan.share), w1 = int32_t((it.start + it.keys - 1) / plan.share);
   if (w0 == w1) return;

@@ -1,4 +1,4 @@
-// The flat range of keys of a paged attention call (PagedAttnArgs) as a
+// The flat range of a paged attention call (PagedAttnArgs) as a
 // work-group finds its way in it.
 #pragma once
 
@@ -11,8 +11,7 @@ namespace stlite {
 struct PagedItem {
   int32_t unit, seq, index;  // unit = (layer, kv head, head group)
   int32_t n, cached, row0;   // new tokens, tokens before them (negative: too short), first new token
-  int64_t start, keys;       // in the flat range
-
+  int64_t start, keys;       // place of its first key in the flat range
 };
 
 template <int NT>  // threads of the work-group, a multiple of 64
@@ -25,12 +24,12 @@ struct PagedPlan {
   const PagedAttnArgs& a;
   Shared& sh;
   int64_t per_unit, total, share;
-  int64_t mine, before;  // this thread's sequences' keys, and those of the threads before it
+  int64_t mine, before;  // this thread's sequences' places, and those of the threads before it
   int32_t s0, s1;        // this thread's sequences
 
-  __device__ int64_t keys_of(int32_t s) const {
+  __device__ int64_t range_of(int32_t s) const {
     const int32_t n = a.c.cu_new[s + 1] - a.c.cu_new[s];
-    return paged_keys(n, paged_len(a.c, s) - n, a.tokens);
+    return paged_range(n, paged_len(a.c, s) - n, a.tokens, a.item_cost);
   }
 
   __device__ PagedPlan(const PagedAttnArgs& args, Shared& shared) : a(args), sh(shared) {
@@ -38,13 +37,13 @@ struct PagedPlan {
       s0 = 0;
       s1 = 1;
       before = 0;
-      mine = per_unit = uniform(keys_of(0));
+      mine = per_unit = uniform(range_of(0));
     } else {
       const int32_t per = (a.c.n_seqs + NT - 1) / NT;
       s0 = min(int32_t(threadIdx.x) * per, a.c.n_seqs);
       s1 = min(s0 + per, a.c.n_seqs);
       mine = 0;
-      for (int32_t s = s0; s < s1; ++s) mine += keys_of(s);
+      for (int32_t s = s0; s < s1; ++s) mine += range_of(s);
       const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
       int64_t sum = mine;
 #pragma unroll
@@ -73,7 +72,7 @@ struct PagedPlan {
     return int64_t((uint64_t(hi) << 32) | lo);
   }
 
-  // The item that key x of the range lies in (0 <= x < total; the whole
+  // The item that place x of the range lies in (0 <= x < total; the whole
   // work-group calls).
   __device__ PagedItem find(int64_t x) {
     const int64_t unit = x / per_unit, rem = x - unit * per_unit;
@@ -82,8 +81,8 @@ struct PagedPlan {
     if (a.c.n_seqs == 1) {
       it.seq = 0;
       load_seq(it);
-      it.index = paged_item_of(rem, it.n, it.cached, a.tokens);
-      it.start = unit * per_unit + paged_prefix(it.index, it.cached, a.tokens);
+      it.index = paged_item_of(rem, it.n, it.cached, a.tokens, a.item_cost);
+      it.start = unit * per_unit + paged_prefix(it.index, it.cached, a.tokens, a.item_cost) + a.item_cost;
       set_keys(it);
       return it;
     }
@@ -92,7 +91,7 @@ struct PagedPlan {
       int64_t b = before;
       int32_t s = s0;
       for (; s + 1 < s1; ++s) {
-        const int64_t k = keys_of(s);
+        const int64_t k = range_of(s);
         if (rem < b + k) break;
         b += k;
       }
@@ -103,8 +102,8 @@ struct PagedPlan {
     it.seq = __builtin_amdgcn_readfirstlane(sh.seq);
     const int64_t base = uniform(sh.base), in = rem - base;
     load_seq(it);
-    it.index = paged_item_of(in, it.n, it.cached, a.tokens);
-    it.start = unit * per_unit + base + paged_prefix(it.index, it.cached, a.tokens);
+    it.index = paged_item_of(in, it.n, it.cached, a.tokens, a.item_cost);
+    it.start = unit * per_unit + base + paged_prefix(it.index, it.cached, a.tokens, a.item_cost) + a.item_cost;
     set_keys(it);
     return it;
   }
@@ -117,14 +116,14 @@ struct PagedPlan {
     const int32_t items = paged_items(it.n, a.tokens);
     it.unit = i / items;
     it.index = i % items;
-    it.start = it.unit * per_unit + paged_prefix(it.index, it.cached, a.tokens);
+    it.start = it.unit * per_unit + paged_prefix(it.index, it.cached, a.tokens, a.item_cost) + a.item_cost;
     set_keys(it);
     return it;
   }
 
   // The item behind `it` (it is not the last one of the range).
   __device__ void next(PagedItem& it) const {
-    it.start += it.keys;
+    it.start += it.keys + a.item_cost;
     if (++it.index < paged_items(it.n, a.tokens)) return set_keys(it);
     it.index = 0;
     do {

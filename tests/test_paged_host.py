@@ -39,23 +39,24 @@ using namespace stlite;
 struct Item { int64_t start, keys; int32_t tiles; };
 int main(int argc, char** argv) {
   const int64_t units = atoll(argv[1]);
-  const int32_t tokens = atoi(argv[2]), shares = atoi(argv[3]), min_share = atoi(argv[4]);
+  const int32_t tokens = atoi(argv[2]), shares = atoi(argv[3]), min_share = atoi(argv[4]), cost = atoi(argv[5]);
   std::vector<Item> items;
   int64_t at = 0;
   for (int64_t u = 0; u < units; ++u)
-    for (int i = 5; i + 1 < argc; i += 2) {
+    for (int i = 6; i + 1 < argc; i += 2) {
       const int32_t n = atoi(argv[i]), cached = atoi(argv[i + 1]);
       int64_t base = at;
       for (int32_t k = 0; k < paged_items(n, tokens); ++k) {
-        if (at != base + paged_prefix(k, cached, tokens)) { printf("prefix of item %d\n", k); return 1; }
+        if (at != base + paged_prefix(k, cached, tokens, cost)) { printf("prefix of item %d\n", k); return 1; }
         const int64_t keys = paged_item_keys(k, n, cached, tokens);
         const int64_t seen = cached + (int64_t(k) * tokens + tokens < n ? int64_t(k) * tokens + tokens : n);
         if (keys < seen || keys < 1) { printf("item %d counts %lld keys, sees %lld\n", k, (long long)keys, (long long)seen); return 1; }
-        if (paged_item_of(at - base, n, cached, tokens) != k || paged_item_of(at - base + keys - 1, n, cached, tokens) != k) { printf("item_of %d\n", k); return 1; }
+        if (paged_item_of(at - base, n, cached, tokens, cost) != k || paged_item_of(at - base + cost + keys - 1, n, cached, tokens, cost) != k) { printf("item_of %d\n", k); return 1; }
+        at += cost;
         items.push_back({at, keys, int32_t((keys + kPagedTile - 1) / kPagedTile)});
         at += keys;
       }
-      if (at - base != paged_keys(n, cached, tokens)) { printf("keys of a sequence\n"); return 1; }
+      if (at - base != paged_range(n, cached, tokens, cost)) { printf("places of a sequence\n"); return 1; }
     }
   const int64_t total = at, share = paged_share(total, shares, min_share);
   if (share * shares < total) { printf("shares do not cover the range\n"); return 1; }
@@ -67,7 +68,7 @@ int main(int argc, char** argv) {
     const int64_t y = x + share < total ? x + share : total;
     size_t i = 0;
     if (x < y) while (items[i].start + items[i].keys <= x) ++i;
-    for (; x < y; ++i) {
+    for (; x < y && items[i].start < y; ++i) {
       const PagedPart p = paged_part(x, y, items[i].start, items[i].keys);
       if (p.t0 != next[i] || p.t1 < p.t0) { printf("share %lld item %zu: tiles %d .. %d, %d covered\n", (long long)w, i, p.t0, p.t1, next[i]); return 1; }
       next[i] = p.t1;
@@ -87,7 +88,7 @@ int main(int argc, char** argv) {
     if (cut >= total) continue;
     size_t i = 0;
     while (items[i].start + items[i].keys <= cut) ++i;
-    if (items[i].start == cut || items[i].start / share != w) continue;
+    if (items[i].start >= cut || items[i].start / share != w) continue;
     ++joined[i];
     const int64_t w1 = (items[i].start + items[i].keys - 1) / share;
     for (int64_t k = w; k <= w1; ++k) {
@@ -118,9 +119,9 @@ def cuts(tmp_path_factory):
         f.write(PROGRAM)
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", f"-I{CSRC}", src, "-o", exe], check=True)
 
-    def run(units, tokens, shares, min_share, seqs):
+    def run(units, tokens, shares, min_share, seqs, cost=0):
         args = [str(x) for s in seqs for x in s]
-        r = subprocess.run([exe, str(units), str(tokens), str(shares), str(min_share), *args], capture_output=True, text=True)
+        r = subprocess.run([exe, str(units), str(tokens), str(shares), str(min_share), str(cost), *args], capture_output=True, text=True)
         assert r.returncode == 0, (units, tokens, shares, min_share, seqs, r.stdout)
         return int(r.stdout)
     return run
@@ -132,8 +133,9 @@ def cuts(tmp_path_factory):
     (4, 36, 256, 256, [(3136, 30105)]), (2, 32, 256, 256, [(131, 0), (2999, 0), (1, 0), (32, 0), (33, 0)]),
     (5, 18, 512, 256, [(5, -3), (5, 2), (5, 4000), (0, 9)]), (2, 1, 512, 256, [(7, 100)]), (1, 128, 512, 256, [(129, 1)]),
 ])
-def test_every_tile_and_output_once(cuts, units, tokens, shares, min_share, seqs):
-    cuts(units, tokens, shares, min_share, seqs)
+@pytest.mark.parametrize("cost", [0, 1, 32, 384])
+def test_every_tile_and_output_once(cuts, units, tokens, shares, min_share, seqs, cost):
+    cuts(units, tokens, shares, min_share, seqs, cost)
 
 
 def test_cuts_of_random_batches(cuts):
@@ -145,7 +147,7 @@ def test_cuts_of_random_batches(cuts):
         seqs = [(r.randint(0, most), r.choice([-1, 0, 0, 1, 63, r.randint(0, 3000)])) for _ in range(r.randint(1, 9))]
         if not any(n for n, _ in seqs):
             seqs[0] = (1, 10)
-        joined += cuts(r.randint(1, 6), tokens, r.choice([1, 2, 3, 17, 256, 512]), r.choice([1, 63, 64, 256]), seqs)
+        joined += cuts(r.randint(1, 6), tokens, r.choice([1, 2, 3, 17, 256, 512]), r.choice([1, 63, 64, 256]), seqs, r.choice([0, 0, 17, 64, 500]))
     assert joined > 100
 
 
