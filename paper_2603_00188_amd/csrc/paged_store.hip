@@ -27,7 +27,8 @@ __device__ inline int32_t seq_of(const int32_t* cu, int32_t n, int64_t j) {
 
 // Sixteen lanes move one 256-byte row of K and one of V; a work-group 64 rows of
 // a unit.  HBM-bound: all of a thread's loads are issued before its stores, and
-// both bypass the caches (each byte is touched once).
+// both bypass the caches (each byte is touched once).  3.47 GB (a trajectory of 150528
+// tokens, a fifth kept, 112 units) take 601 us, 5.8 TB/s; 78 MB (one screen) 16 us, 4.9.
 __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) {
   constexpr int kPer = kRowsPerGroup / 16;
   const int unit = blockIdx.y;
@@ -84,6 +85,9 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) 
 // once, one pair per lane, and kept in registers over the token's heads.
 // Angles: position * turns in 64 bits, reduced to a fraction of a turn there;
 // the sine of the reduced angle in fp32.
+// HBM-bound once there are a few thousand rows: 3136 tokens of 28 layers (1.62 GB read
+// and written) take 298 us, 5.4 TB/s; 64 tokens of 28 layers (44 MB) 12.3 us, 3.6 TB/s,
+// where the chain of dependent loads (sequence, length, page, row) is half of it.
 template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   constexpr int kTok = 4 / WAVES;  // tokens per work-group
@@ -94,6 +98,25 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   const int layer = blockIdx.y;
   const int64_t tok = int64_t(blockIdx.x) * kTok + tl;
   const bool live = tok < c.total_new;
+  const int cidx = lane & 7, sub = lane >> 3;
+  const int nq = a.q.data ? c.n_q_heads : 0, nk = c.n_kv_heads;
+  const int rows = nq + 2 * nk;
+  const uint16_t* q = a.q.data + layer * a.q.layer_stride + tok * a.q.token_stride;
+  const uint16_t* k = a.k.data + layer * a.k.layer_stride + tok * a.k.token_stride;
+  const uint16_t* v = a.v.data + layer * a.v.layer_stride + tok * a.v.token_stride;
+  const int64_t unit_rows = int64_t(c.n_pages) << c.page_shift;
+  // Row r of the token: queries, keys, values.  The first one's load runs under the
+  // angles and the search, each further one's under the row before it.
+  auto source = [&](int r) {
+    return r < nq ? q + r * kHeadDim : r < nq + nk ? k + (r - nq) * kHeadDim : v + (r - nq - nk) * kHeadDim;
+  };
+  u32x4_t lo_next{}, hi_next{};
+  auto load = [&](int r) {
+    const uint16_t* src = source(r) + 8 * cidx;
+    lo_next = *reinterpret_cast<const u32x4_t*>(src);
+    hi_next = *reinterpret_cast<const u32x4_t*>(src + 64);
+  };
+  if (live && part * 8 + sub < rows) load(part * 8 + sub);
   if (a.positions && live && part == 0) {
     const int axis = (lane >= a.axis1) + (lane >= a.axis2);
     const double turn = double(a.positions[axis * c.total_new + tok]) * a.turns[lane];
@@ -103,7 +126,6 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   __syncthreads();
   if (!live) return;
 
-  const int cidx = lane & 7, sub = lane >> 3;
   float cs[16], sn[16];  // of the low chunk's and the high chunk's pairs
   if (a.positions) {
 #pragma unroll
@@ -120,47 +142,35 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   // Where the token's keys and values go.
   int64_t slot = -1;  // row of the pool within a unit
   {
-    const int32_t s = [&] {
-      int32_t lo = 0, hi = c.n_seqs;
-      while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (c.cu_new[mid] <= tok) lo = mid;
-        else hi = mid;
-      }
-      return lo;
-    }();
+    int32_t s = 0;
+    for (int32_t n = c.n_seqs; n > 1;) {  // a wave's 64 probes at once: one round for 64 sequences
+      const int32_t step = (n + 63) / 64, at = lane * step;
+      s += step * (63 - __builtin_clzll(__ballot(at < n && c.cu_new[min(s + at, c.n_seqs)] <= tok) | 1));
+      n = min(step, c.n_seqs - s);
+    }
     const int64_t at = int64_t(paged_len(c, s)) - c.cu_new[s + 1] + tok;
     if (at >= 0) {
       const int32_t page = c.page_table[int64_t(s) * c.max_pages + (at >> c.page_shift)];
       if (page >= 0 && page < c.n_pages) slot = (int64_t(page) << c.page_shift) + (at & ((1 << c.page_shift) - 1));
     }
   }
-  const int nq = a.q.data ? c.n_q_heads : 0, nk = c.n_kv_heads;
-  const int rows = nq + 2 * nk;
-  const uint16_t* q = a.q.data + layer * a.q.layer_stride + tok * a.q.token_stride;
-  const uint16_t* k = a.k.data + layer * a.k.layer_stride + tok * a.k.token_stride;
-  const uint16_t* v = a.v.data + layer * a.v.layer_stride + tok * a.v.token_stride;
-  const int64_t unit_rows = int64_t(c.n_pages) << c.page_shift;
   for (int r = part * 8 + sub; r < rows; r += 8 * WAVES) {
-    const uint16_t* src;
+    const u32x4_t lo = lo_next, hi = hi_next;
+    if (r + 8 * WAVES < rows) load(r + 8 * WAVES);
     uint16_t* dst;
     const uint16_t* w = nullptr;
     bool turn = a.positions != nullptr;
     if (r < nq) {
-      src = q + r * kHeadDim;
       dst = a.q_out + ((layer * c.total_new + tok) * c.n_q_heads + r) * kHeadDim;
       w = a.q_norm;
     } else {
       const int h = (r - nq) % nk;
       const bool key = r - nq < nk;
-      src = (key ? k : v) + h * kHeadDim;
       const int64_t row = int64_t(layer * nk + h) * unit_rows + slot;
       dst = slot < 0 ? nullptr : (key ? c.k : c.v) + row * kHeadDim;
       w = key ? a.k_norm : nullptr;
       turn = turn && key;
     }
-    const u32x4_t lo = *reinterpret_cast<const u32x4_t*>(src + 8 * cidx);
-    const u32x4_t hi = *reinterpret_cast<const u32x4_t*>(src + 64 + 8 * cidx);
     u32x4_t ylo = lo, yhi = hi;
     if (w || turn) {
       float x[16];
@@ -232,8 +242,11 @@ hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t stream) {
-  // Few (token, layer) pairs: four waves each, for their latency; else a wave each.
-  const bool few = a.c.total_new * a.c.n_layers <= 2048;
+  // Few (token, layer) pairs: four waves each, for their latency; else a wave each, which
+  // forms the angles once.  28 query heads, a wave / four waves each: 1 pair 4.7 / 3.4 us,
+  // 448 pairs 6.0 / 4.7, 1024 pairs 6.9 / 5.9, 1792 pairs 9.2 / 10.1, 4096 pairs 14.3 /
+  // 16.3, 87808 pairs 303 / 317.
+  const bool few = a.c.total_new * a.c.n_layers <= 1024;
   const dim3 grid(uint32_t((a.c.total_new + (few ? 0 : 3)) / (few ? 1 : 4)), a.c.n_layers);
   if (half) {
     if (few) hipLaunchKernelGGL((paged_append_kernel<_Float16, 4>), grid, dim3(256), 0, stream, a);
