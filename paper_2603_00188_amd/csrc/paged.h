@@ -57,6 +57,8 @@ struct PagedAppendArgs {
 // several shares cut leave (max, sum, O) in the workspace and are joined by a
 // second launch.  The lengths are read on the device only, so the grid does not
 // depend on them.
+constexpr int32_t kDecHeads = 16;   // rows of an item: one token
+constexpr int32_t kExtRows = 256;   // several
 struct PagedAttnArgs {
   PagedDev c;
   const uint16_t* q;  // [layers][total_new][q_heads][d]
@@ -64,7 +66,7 @@ struct PagedAttnArgs {
   float scale2;       // scale * log2(e)
   int32_t parts;      // head groups of a kv head (decode: 16 heads each; else 1)
   int32_t tokens;     // new tokens per item
-  int32_t rows;       // rows of an item's partial (decode 16, else 128 or 256)
+  int32_t rows;       // rows of an item's partial (kDecHeads or kExtRows)
   int32_t shares;     // work-groups
   int32_t min_share;  // places
   int32_t item_cost;  // places that beginning an item takes

@@ -121,6 +121,11 @@ PagedDev device_view(const stlite_paged* c) {
 // as none / as here, and flat within 1 % from half to twice that: 5 prompts of 131 to
 // 2999 tokens 324 / 219 us, 5 drafted tokens in each of 16 sequences 69.6 / 64, one
 // token of one layer 17 / 14.4; a screen behind 30k tokens and a step's decoding alike.
+// min_share: five tokens behind 678 took 17.6 us with 128, 19 with 256, 24 with 512; one
+// token 11.3 with 64, 14.2 with 128.  Shares: one work-group of several tokens per CU
+// (its rings fill the LDS), two of one token (256 / 512 / 1024: a ragged batch 742 / 729
+// / 743 us, a step 265 / 270 / 274, a long cache 64.6 / 63.8 / 67.5).  One token by the
+// several-token kernel: 18 us for 11, 72 for 64, 309 for 270, 806 for 729.
 struct AttnPlan {
   bool decode;
   int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows;
@@ -139,19 +144,19 @@ AttnPlan attn_plan(const stlite_paged* c) {
   p.decode = most <= 1;
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
   if (p.decode) {
-    p.parts = int32_t(ceil_div(group, 16));
+    p.parts = int32_t(ceil_div(group, kDecHeads));
     p.tokens = 1;
-    p.rows = 16;
+    p.rows = kDecHeads;
     p.shares = 512;
     p.min_share = 64;
     p.item_cost = 64;
     items *= p.parts * live;
   } else {
     p.parts = 1;
-    p.rows = most * group <= 128 ? 128 : 256;
+    p.rows = kExtRows;
     p.tokens = int32_t(p.rows / group);
     p.shares = 256;
-    p.min_share = 256;
+    p.min_share = 128;
     p.item_cost = 384;
     int64_t blocks = 0;
     for (int32_t s = 0; s < c->n_seqs; ++s) blocks += ceil_div(int64_t(c->h_cu_new[s + 1]) - c->h_cu_new[s], p.tokens);
@@ -161,10 +166,11 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // (no more shares than the longest possible range fills)
   const double range = double(items) * (double(c->max_len) + p.item_cost);
   p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(range / p.min_share))));
-  // Joining: one round of work-groups (two per CU) where the items are few; else a
+  // Joining: one round of work-groups (two per CU) where the items are few (by boundary a
+  // long cache took 73 us, not 64, 64 tokens behind 3000 66, not 30); else a
   // work-group per boundary (with a quarter of an item's rows each, and four times the
   // work-groups, prompts of 131 to 2999 tokens took 220 us, with all of them 216).
-  const int64_t item_rows = p.decode ? std::min<int64_t>(group, 16) : p.tokens * group;
+  const int64_t item_rows = p.decode ? std::min<int64_t>(group, kDecHeads) : p.tokens * group;
   p.join_items = c->n_seqs == 1 && items < p.shares ? int32_t(items) : 0;
   p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : p.rows;
   const size_t slots = size_t(p.shares) * 2 * p.rows;

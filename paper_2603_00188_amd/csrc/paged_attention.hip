@@ -77,7 +77,6 @@ struct LdsPageWindow {
 //   O += P V      v_mfma_f32_16x16x4_f32, which takes one cached row per lane and
 //                 k-step: V needs no transpose and P stays fp32.
 constexpr int kDecWaves = 4;
-constexpr int kDecHeads = 16;
 
 __device__ inline u32x4_t load_row16(const uint16_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
@@ -247,13 +246,13 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // Several new tokens per sequence
 // ---------------------------------------------------------------------------
 //
-// An item's rows (token-major, all query heads of the kv head) are cut into
-// blocks of 32; eight waves stream 64-key tiles of K and V through rings in LDS
-// (direct DMA).  KB = 2: eight blocks, a wave takes all 64 keys of a tile for its
-// block; KB = 1, for at most 128 rows: four blocks, two waves take 32 keys each and
-// are merged behind the last tile.  Everything is transposed, so that a lane owns
-// one query (column lane & 31; two lanes share it, each with half the keys) and the
-// softmax needs no exchange but one swap:
+// An item's rows (token-major, all query heads of the kv head, at most 256) are cut
+// into blocks of 32, one for each of eight waves, which stream 64-key tiles of K and V
+// through rings in LDS (direct DMA); a wave without rows only fetches.  (Items of 128
+// rows, two waves to a block with 32 keys each, took the same 62 us for five drafted tokens,
+// and 268, not 219, for prompts.)  Everything is transposed, so that a lane owns one query
+// (column lane & 31; two lanes share it, each with half the keys) and the softmax
+// needs no exchange but one swap:
 //   S^T = K Q^T      32x32x16, A: K rows from LDS, B: queries in registers;
 //   P^T              exp2 of the accumulators, packed where they are: register
 //                    order is a permutation of the keys within 16, which the V
@@ -274,6 +273,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 
 constexpr float kLazy = 8.0f;
 constexpr int kExtWaves = 8;
+static_assert(kExtRows == kExtWaves * 32);
 constexpr int kRing = 4;
 constexpr int kTileBytes = kPagedTile * kHeadDim * 2;
 constexpr int kTileLoads = 4;  // DMA instructions of a wave per tile: it fetches 16 keys, which lie in one page
@@ -298,17 +298,15 @@ __device__ inline void dma16(i32x4_t rsrc, uint32_t to, uint32_t at, uint32_t fr
                : "memory");
 }
 
-template <typename T, int KB>
+template <typename T>
 __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
   constexpr int NT = kExtWaves * 64;
-  constexpr int kBlocks = 4 * KB, kRows = kBlocks * 32;
   __shared__ __align__(1024) uint16_t sm_tiles[2 * kRing * kTileBytes / 2];  // K, then V: [slot][64][128]
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
   __shared__ int32_t sm_pages[kExtWaves][64];
   __shared__ int2 sm_odd[kExtWaves];
-  __shared__ float sm_ml[KB == 1 ? kBlocks : 1][2][32];  // a merged wave's maxima and sums
   const PagedDev& c = a.c;
   PagedPlan<NT> plan(a, sm_plan);
   int64_t x = int64_t(blockIdx.x) * plan.share;
@@ -319,9 +317,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   const int64_t share = plan.share;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = wave >> 2;                      // half a step apart
-  const int block = KB == 2 ? wave : wave & 3;      // of 32 rows
-  const int first_key = KB == 2 ? 0 : 32 * group;   // of a tile
+  const int group = wave >> 2;  // half a step apart
   const int col = lane & 31, h = lane >> 5;
   const int32_t in_page = (1 << c.page_shift) - 1;
   const uint32_t lds0 = uint32_t(reinterpret_cast<uintptr_t>(sm_tiles));
@@ -330,11 +326,11 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   // transposed read of 4 keys x 32 dimensions takes all 16 slots.  Either way the
   // chunk's number enters an address by exclusive or alone, so one address per
   // lane gives all of them.
-  const uint32_t k_lane = lds0 + (first_key + col) * 256 + ((h ^ (col & 15)) << 4);
+  const uint32_t k_lane = lds0 + col * 256 + ((h ^ (col & 15)) << 4);
   uint32_t v_lane;
   {
     const int i = lane & 15, c0 = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    v_lane = lds0 + kRing * kTileBytes + (first_key + 4 * h + (i >> 2)) * 256 + ((4 * (i >> 2) + (c0 ^ h)) << 4) + (i & 1) * 8;
+    v_lane = lds0 + kRing * kTileBytes + (4 * h + (i >> 2)) * 256 + ((4 * (i >> 2) + (c0 ^ h)) << 4) + (i & 1) * 8;
   }
   // DMA load g brings keys 4 g + (lane >> 4) of the wave's sixteen: a lane's row and
   // the chunk that belongs in its 16 bytes (+ 1024 g, ^ 64 g or ^ 16 g).
@@ -356,7 +352,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     const int32_t t0 = __builtin_amdgcn_readfirstlane(span.t0);
     const int32_t t1 = __builtin_amdgcn_readfirstlane(min(span.t1, (seen + kPagedTile - 1) / kPagedTile));
     // This lane's query (a row past the item's repeats the last one).
-    const int32_t row = min(block * 32 + col, rows - 1), tok = row / c.group;
+    const int32_t row = min(wave * 32 + col, rows - 1), tok = row / c.group;
     const int64_t qrow = (int64_t(layer) * c.total_new + it.row0 + tok0 + tok) * c.n_q_heads + int64_t(kv) * c.group +
                          (row - tok * c.group);
     const int32_t limit = it.cached + tok0 + tok;  // last key that it sees
@@ -367,7 +363,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     const int32_t limit_lo = __builtin_amdgcn_readfirstlane(limit);
     // last tile of this wave; none where its rows are past the item's
     const int32_t t_last =
-        block * 32 < rows ? min((__builtin_amdgcn_readlane(limit, 31) - first_key) >> 6, t1 - 1) : -1;
+        wave * 32 < rows ? min(__builtin_amdgcn_readlane(limit, 31) >> 6, t1 - 1) : -1;
 
     float m_ref = -FLT_MAX, l_run = 0.0f;  // (finite: no difference of infinities while no key was seen)
     f32x16_t o[4];
@@ -416,24 +412,24 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     auto full = [&](int32_t t, uint32_t b, int32_t first) { return b == 0 && t * kPagedTile + kPagedTile - 1 <= first; };
     auto slot = [&](int32_t t) { return uint32_t((t - t0) & (kRing - 1)) * kTileBytes; };
     // (the 32-key blocks in turn: a product does not wait for the one before it)
-    auto read_k = [&](uint32_t at, int i) {  // keys 32 (i % KB) .., dimensions 16 (i / KB) .. (at: k_lane + slot)
-      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)((at ^ (i / KB << 5)) + i % KB * 8192));
+    auto read_k = [&](uint32_t at, int i) {  // keys 32 (i & 1) .., dimensions 16 (i >> 1) .. (at: k_lane + slot)
+      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)((at ^ (i >> 1 << 5)) + (i & 1) * 8192));
     };
     auto read_v = [&](uint32_t at, int i) {  // keys 16 (i / 4) .., dimensions 32 (i % 4) .. (at: v_lane + slot)
       const u32x2_t lo = read_transposed((at ^ (i % 4 << 6)) + i / 4 * 4096);
       const u32x2_t hi = read_transposed((at ^ (i % 4 << 6) ^ 32) + i / 4 * 4096 + 2048);
       return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
     };
-    f32x16_t s[KB];     // logits of the tile ahead
-    u32x4_t w[2 * KB];  // weights of the tile: eight keys of this lane to each 16
+    f32x16_t s[2];     // logits of the tile ahead
+    u32x4_t w[4];  // weights of the tile: eight keys of this lane to each 16
     auto product = [&](int i, u32x4_t kf) {
-      s[i % KB] = E::mfma32(__builtin_bit_cast(x8, kf), qf[i / KB], i < KB ? f32x16_t{} : s[i % KB]);
+      s[i & 1] = E::mfma32(__builtin_bit_cast(x8, kf), qf[i >> 1], i < 2 ? f32x16_t{} : s[i & 1]);
     };
     auto add = [&](int i, u32x4_t vf) {
       o[i & 3] = E::mfma32(__builtin_bit_cast(x8, vf), __builtin_bit_cast(x8, w[i >> 2]), o[i & 3]);
     };
-    constexpr int kSteps = 8 * KB;  // products of the logits, and of the values
-    constexpr int kAhead = 3;       // reads run that many products ahead
+    constexpr int kSteps = 16;  // products of the logits, and of the values
+    constexpr int kAhead = 3;   // reads run that many products ahead
 
     // The products of step t.  (Behind the wave's last tile the logits are of
     // whatever lies in the slot; nobody looks at them.)
@@ -477,16 +473,16 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     auto weigh = [&](int32_t t, uint32_t b) {
       if (!full(t, b, limit_lo)) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int32_t in_tile = first_key + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-            if (t * kPagedTile + in_tile > limit || ((b >> (first_key / 16 + 2 * kb + (i >> 3))) & 1)) s[kb][i] = -INFINITY;
+            const int32_t in_tile = kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
+            if (t * kPagedTile + in_tile > limit || ((b >> (2 * kb + (i >> 3))) & 1)) s[kb][i] = -INFINITY;
           }
       }
-      float mt = fmaxf(s[0][0], s[KB - 1][1]);
+      float mt = fmaxf(s[0][0], s[1][1]);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mt = fmaxf(fmaxf(mt, s[kb][i]), s[kb][i + 1]);
       float other = mt;
@@ -504,7 +500,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       }
       float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int n = 0; n < 8 * KB; ++n) {
+      for (int n = 0; n < 16; ++n) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][2 * n & 15], a.scale2, -m_ref));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][(2 * n & 15) + 1], a.scale2, -m_ref));
         sum[0] += p0;
@@ -567,7 +563,6 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     for (int32_t key = odd_lo * kPagedTile; key < min((odd_hi + 1) * kPagedTile, seen); ++key) {
       pages.seek(key >> c.page_shift);
       if (pages.is_bad(key >> c.page_shift)) continue;
-      if (KB == 1 && (key & 32) != first_key) continue;
       const uint16_t* vr = c.v + (page_row(c, unit, pages.page(key >> c.page_shift)) + (key & in_page)) * kHeadDim + 4 * h;
 #pragma unroll
       for (int db = 0; db < 4; ++db)
@@ -585,35 +580,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     float other = l_run;
     swap32(l_run, other);
     l_run += other;
-    if constexpr (KB == 1) {
-      // The second group's half of the keys joins the first's, through the tiles.
-      f32x4_t* sm_o = reinterpret_cast<f32x4_t*>(sm_tiles) + block * 1024 + lane;  // [16][64 lanes]
-      __syncthreads();
-      if (group) {
-#pragma unroll
-        for (int g = 0; g < 16; ++g)
-          sm_o[g * 64] = f32x4_t{o[g >> 2][4 * (g & 3)], o[g >> 2][4 * (g & 3) + 1], o[g >> 2][4 * (g & 3) + 2],
-                                 o[g >> 2][4 * (g & 3) + 3]};
-        if (h == 0) {
-          sm_ml[block][0][col] = m_ref;
-          sm_ml[block][1][col] = l_run;
-        }
-      }
-      __syncthreads();
-      if (!group) {
-        const float m1 = sm_ml[block][0][col], m = fmaxf(m_ref, m1);
-        const float f0 = __builtin_amdgcn_exp2f(m_ref - m), f1 = __builtin_amdgcn_exp2f(m1 - m);
-        m_ref = m;
-        l_run = l_run * f0 + sm_ml[block][1][col] * f1;
-#pragma unroll
-        for (int g = 0; g < 16; ++g) {
-          const f32x4_t p = sm_o[g * 64];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[g >> 2][4 * (g & 3) + j] = o[g >> 2][4 * (g & 3) + j] * f0 + p[j] * f1;
-        }
-      }
-    }
-    if (block * 32 + col < rows && (KB == 2 || !group)) {
+    if (wave * 32 + col < rows) {
       if (whole) {
         const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
         uint16_t* p = a.out + qrow * kHeadDim + 4 * h;
@@ -627,7 +594,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
             *reinterpret_cast<u32x2_t*>(p + 32 * db + 8 * g) = e;
           }
       } else {
-        const int64_t at = paged_slot(blockIdx.x, share, it.start) * kRows + block * 32 + col;
+        const int64_t at = paged_slot(blockIdx.x, share, it.start) * kExtRows + wave * 32 + col;
         float* p = a.po + at * kHeadDim + 4 * h;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
@@ -791,9 +758,9 @@ hipError_t decode(const PagedAttnArgs& a, hipStream_t stream) {
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }
 
-template <typename T, int KB>
+template <typename T>
 hipError_t extend(const PagedAttnArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_extend_kernel<T, KB>), dim3(a.shares), dim3(kExtWaves * 64), 0, stream, a);
+  hipLaunchKernelGGL((paged_extend_kernel<T>), dim3(a.shares), dim3(kExtWaves * 64), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }
@@ -805,8 +772,7 @@ hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t st
 }
 
 hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t stream) {
-  if (half) return a.rows == 256 ? extend<_Float16, 2>(a, stream) : extend<_Float16, 1>(a, stream);
-  return a.rows == 256 ? extend<__bf16, 2>(a, stream) : extend<__bf16, 1>(a, stream);
+  return half ? extend<_Float16>(a, stream) : extend<__bf16>(a, stream);
 }
 
 }  // namespace stlite

@@ -151,6 +151,8 @@ DECODE = [
     ((1000, 300), (1, 1), 256, "bf16", 1, 17, 1),      # two head groups, one head in the second
     ((700, 64, 1), (1, 1, 1), 16, "fp16", 1, 128, 1),  # eight head groups
     ((20000,), (1,), 32, "bf16", 1, 4, 2),
+    ((3000,), (1,), 16, "bf16", 1, 40, 1),             # one sequence, three head groups, each cut
+    ((9000,), (1,), 16, "fp16", 2, 2, 2),              # one row to an item, more parts than are joined at once
     (tuple(range(1, 300, 3)), (1,) * 100, 16, "bf16", 1, 4, 1),
 ]
 
@@ -194,6 +196,8 @@ EXTEND = [
     ((200,), (150,), 16, "bf16", 1, 128, 1),              # two tokens to a block
     ((6000,), (3,), 32, "bf16", 1, 28, 4),                # few rows over a long cache: joined
     ((2500,), (700,), 64, "bf16", 1, 7, 1),
+    ((3000,), (60,), 16, "fp16", 1, 128, 1),              # items of one sequence, each in many parts
+    ((900,) * 6, (200,) * 6, 32, "bf16", 3, 8, 2),        # items cut in two
     ((3, 0, 2), (5, 3, 9), 16, "bf16", 1, 2, 1),          # shorter than their new tokens
 ]
 
@@ -399,6 +403,24 @@ def test_append(torch_cuda, lens, new, page, dtype, layers, hq, hk, axes, interl
     rest = np.setdiff1d(np.arange(f.n_pages * page), r)
     for now, old in zip((_bits(f.k), _bits(f.v)), before):
         assert np.array_equal(now.reshape(layers, hk, -1, D)[:, :, rest], old.reshape(layers, hk, -1, D)[:, :, rest])
+
+
+@pytest.mark.parametrize("n_seqs", [63, 64, 65, 700, 4097])
+def test_append_finds_its_sequence(torch_cuda, n_seqs):
+    """Sequences without new tokens between the others, and at both ends."""
+    rng = np.random.default_rng(n_seqs)
+    new = rng.integers(0, 3, n_seqs)
+    new[0] = new[-1] = 0
+    lens = [int(n + rng.integers(0, 20)) for n in new]
+    f = Served(lens, new.tolist(), 16, "bf16", 1, 1, 1, seed=17)
+    k, v = (f.randn((1, f.total, 1, D)) for _ in range(2))
+    want = [_bits(x).reshape(-1, D).copy() for x in (f.k, f.v)]
+    f.P.paged_append(f.cache, f.batch, None, k, v)
+    places = OP.new_places(f.table, f.lens, f.cu, 16, f.n_pages, f.max_len)
+    for pool, x in zip(want, (k, v)):
+        pool[np.array(places)] = _bits(x).reshape(-1, D)
+    for pool, got in zip(want, (f.k, f.v)):
+        assert np.array_equal(_bits(got).reshape(-1, D), pool)
 
 
 def test_append_drops_rows_without_a_page(torch_cuda):
