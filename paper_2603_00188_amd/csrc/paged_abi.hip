@@ -128,7 +128,7 @@ PagedDev device_view(const stlite_paged* c) {
 // several-token kernel: 18 us for 11, 72 for 64, 309 for 270, 806 for 729.
 struct AttnPlan {
   bool decode;
-  int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows;
+  int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows, join_split;
   size_t bytes;
 };
 
@@ -166,13 +166,17 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // (no more shares than the longest possible range fills)
   const double range = double(items) * (double(c->max_len) + p.item_cost);
   p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(range / p.min_share))));
-  // Joining: one round of work-groups (two per CU) where the items are few (by boundary a
-  // long cache took 73 us, not 64, 64 tokens behind 3000 66, not 30); else a
-  // work-group per boundary (with a quarter of an item's rows each, and four times the
-  // work-groups, prompts of 131 to 2999 tokens took 220 us, with all of them 216).
-  const int64_t item_rows = p.decode ? std::min<int64_t>(group, kDecHeads) : p.tokens * group;
-  p.join_items = c->n_seqs == 1 && items < p.shares ? int32_t(items) : 0;
-  p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : p.rows;
+  // Joining by boundary gives every cut item to one work-group (with a quarter of its
+  // rows each, and four times the work-groups, prompts of 131 to 2999 tokens took 220 us,
+  // with all of them 216).  Where that is more than four rounds of its loads on average,
+  // one round of work-groups (two per CU) shares out the items' rows, which costs a second
+  // scan of the lengths.  By boundary / by item: one token behind 3 sequences of up to
+  // 79079 in 2 units 63.8 / 45.6 us, a long cache 73 / 64, 64 tokens behind 3000 66 / 30;
+  // five layers' 4 tokens in 2 sequences behind 1468 24.5 / 29.4, one token in 46 27 / 34.
+  const int64_t item_rows = p.decode ? std::min<int64_t>(group, kDecHeads) : std::min<int64_t>(p.tokens, most) * group;
+  p.join_items = items < p.shares && item_rows * p.shares >= 512 * items ? int32_t(items) : 0;
+  p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : int32_t(item_rows);
+  p.join_split = int32_t(ceil_div(item_rows, p.join_rows));
   const size_t slots = size_t(p.shares) * 2 * p.rows;
   p.bytes = p.shares == 1 ? 0 : 2 * align_up(slots * sizeof(float)) + align_up(slots * kHeadDim * sizeof(float));
   return p;
@@ -352,6 +356,7 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.item_cost = p.item_cost;
   a.join_items = p.join_items;
   a.join_rows = p.join_rows;
+  a.join_split = p.join_split;
   const size_t slots = size_t(p.shares) * 2 * p.rows;
   a.pm = static_cast<float*>(ws);
   a.pl = a.pm + align_up(slots * sizeof(float)) / sizeof(float);

@@ -621,7 +621,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 //
 // A work-group joins up to join_rows rows of an item: the item that the boundary
 // between shares x and x + 1 cuts, if x is the first share in it, or with join_items
-// (one sequence, fewer items than shares) item x.  32 lanes x 4 dimensions hold a row;
+// (few items in many parts) item x.  32 lanes x 4 dimensions hold a row;
 // its parts (two mostly, up to all shares for one token over a long cache) are spread
 // over the groups of lanes that the rows leave, kBatch loads at once, and merged
 // through LDS.  Bound by latency for one token (6 us for 11 parts of a layer, 8 us for
@@ -744,10 +744,8 @@ __global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnA
 template <typename T>
 hipError_t launch_join(const PagedAttnArgs& a, hipStream_t stream) {
   if (a.shares < 2) return hipSuccess;
-  const int32_t rows = a.rows == kDecHeads ? min(a.c.group, kDecHeads) : a.tokens * a.c.group;
-  hipLaunchKernelGGL((paged_join_kernel<T>), dim3(a.join_items ? a.join_items : a.shares - 1, (rows + a.join_rows - 1) / a.join_rows),
-                     dim3(kJoinGroups * 32),
-                     0, stream, a);
+  hipLaunchKernelGGL((paged_join_kernel<T>), dim3(a.join_items ? a.join_items : a.shares - 1, a.join_split),
+                     dim3(kJoinGroups * 32), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -19,7 +19,7 @@ struct PagedPlan {
   struct Shared {
     int64_t wave[NT / 64];
     int64_t base;
-    int32_t seq;
+    int32_t seq, index;
   };
   const PagedAttnArgs& a;
   Shared& sh;
@@ -27,9 +27,32 @@ struct PagedPlan {
   int64_t mine, before;  // this thread's sequences' places, and those of the threads before it
   int32_t s0, s1;        // this thread's sequences
 
+  __device__ int32_t items_of(int32_t s) const { return paged_items(a.c.cu_new[s + 1] - a.c.cu_new[s], a.tokens); }
   __device__ int64_t range_of(int32_t s) const {
     const int32_t n = a.c.cu_new[s + 1] - a.c.cu_new[s];
     return paged_range(n, paged_len(a.c, s) - n, a.tokens, a.item_cost);
+  }
+
+  // The sum of v over the threads before this one, and over all.
+  __device__ int64_t scan(int64_t v, int64_t& all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t sum = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    if (lane == 63) sh.wave[wave] = sum;
+    __syncthreads();
+    sum -= v;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < wave) sum += sh.wave[w];
+      all += sh.wave[w];
+    }
+    all = uniform(all);
+    return sum;
   }
 
   __device__ PagedPlan(const PagedAttnArgs& args, Shared& shared) : a(args), sh(shared) {
@@ -44,23 +67,7 @@ struct PagedPlan {
       s1 = min(s0 + per, a.c.n_seqs);
       mine = 0;
       for (int32_t s = s0; s < s1; ++s) mine += range_of(s);
-      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-      int64_t sum = mine;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int64_t up = __shfl_up(sum, d);
-        if (lane >= d) sum += up;
-      }
-      if (lane == 63) sh.wave[wave] = sum;
-      __syncthreads();
-      before = sum - mine;
-      per_unit = 0;
-#pragma unroll
-      for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) before += sh.wave[w];
-        per_unit += sh.wave[w];
-      }
-      per_unit = uniform(per_unit);
+      before = scan(mine, per_unit);
     }
     total = per_unit * a.c.n_units * a.parts;
     share = paged_share(total, a.shares, a.min_share);
@@ -108,15 +115,38 @@ struct PagedPlan {
     return it;
   }
 
-  // Item i of a call with one sequence.
-  __device__ PagedItem item(int32_t i) const {
+  // Item i of the call's join_items (the whole work-group calls).
+  __device__ PagedItem item(int32_t i) {
+    const int32_t per = a.join_items / (a.c.n_units * a.parts);
     PagedItem it;
+    it.unit = i / per;
+    it.index = i % per;
     it.seq = 0;
+    int64_t base = 0;
+    if (a.c.n_seqs > 1) {
+      int32_t count = 0;
+      for (int32_t s = s0; s < s1; ++s) count += items_of(s);
+      __syncthreads();  // (the last scan's sums have been read)
+      int64_t all;
+      int32_t at = it.index - int32_t(scan(count, all));
+      if (at >= 0 && at < count) {
+        int64_t b = before;
+        int32_t s = s0;
+        for (; at >= items_of(s); ++s) {
+          at -= items_of(s);
+          b += range_of(s);
+        }
+        sh.seq = s;
+        sh.index = at;
+        sh.base = b;
+      }
+      __syncthreads();
+      it.seq = __builtin_amdgcn_readfirstlane(sh.seq);
+      it.index = __builtin_amdgcn_readfirstlane(sh.index);
+      base = uniform(sh.base);
+    }
     load_seq(it);
-    const int32_t items = paged_items(it.n, a.tokens);
-    it.unit = i / items;
-    it.index = i % items;
-    it.start = it.unit * per_unit + paged_prefix(it.index, it.cached, a.tokens, a.item_cost) + a.item_cost;
+    it.start = it.unit * per_unit + base + paged_prefix(it.index, it.cached, a.tokens, a.item_cost) + a.item_cost;
     set_keys(it);
     return it;
   }
