@@ -162,8 +162,10 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  *   out  the same layout and type; 16-byte aligned, must not alias q
  *   scale  finite, > 0
  * fp32 logits, softmax statistics and sums.  With one new token per sequence the
- * weights stay fp32; with more they are rounded to the type of the call before
- * they meet v.  Rows of out belong to new tokens only: nothing behind total_new
+ * weights keep fp32's 24 bits (fp16: 22, or 2^-40 of the greatest weight); with more
+ * they are rounded to the type of the call before they meet v.  An infinity or NaN of
+ * a token that is seen reaches the output whatever its weight (an infinity of a weight
+ * that is rounded to 0 as NaN).  Rows of out belong to new tokens only: nothing behind total_new
  * is written.
  */
 stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, float scale, uint16_t* out,

@@ -49,7 +49,7 @@ struct PagedAppendArgs {
 
 // Attention runs as a flat range of places, cut into equal shares.  The queries of
 // a (unit, sequence) are cut into items of `tokens` new tokens (all heads of the
-// kv head: tokens * group rows; decode: one token, at most 16 heads); item i of a
+// kv head: tokens * group rows; decode: one token, at most 16 or 32 heads); item i of a
 // sequence with n new tokens behind c cached ones counts c + min((i + 1) tokens,
 // n) keys, what its last token sees, and takes item_cost places before them.  Items
 // lie one after another, units outermost; work-group w takes the keys in [w share,
@@ -57,16 +57,15 @@ struct PagedAppendArgs {
 // several shares cut leave (max, sum, O) in the workspace and are joined by a
 // second launch.  The lengths are read on the device only, so the grid does not
 // depend on them.
-constexpr int32_t kDecHeads = 16;   // rows of an item: one token
-constexpr int32_t kExtRows = 256;   // several
+constexpr int32_t kExtRows = 256;  // rows of an item of several tokens
 struct PagedAttnArgs {
   PagedDev c;
   const uint16_t* q;  // [layers][total_new][q_heads][d]
   uint16_t* out;
   float scale2;       // scale * log2(e)
-  int32_t parts;      // head groups of a kv head (decode: 16 heads each; else 1)
+  int32_t parts;      // head groups of a kv head (decode: `rows` heads each; else 1)
   int32_t tokens;     // new tokens per item
-  int32_t rows;       // rows of an item's partial (kDecHeads or kExtRows)
+  int32_t rows;       // rows of an item's partial (decode 16 or 32, else kExtRows)
   int32_t shares;     // work-groups
   int32_t min_share;  // places
   int32_t item_cost;  // places that beginning an item takes
@@ -90,6 +89,9 @@ hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t st
 // 16-bit element types: bf16 or IEEE half.
 template <typename T>
 struct Elem;
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
 template <>
 struct Elem<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
@@ -99,6 +101,19 @@ struct Elem<__bf16> {
   __device__ static uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
   // Weights are at most 2^8 of their running maximum's (kLazy): any exponent fits.
   static constexpr float kBias = 0.0f;
+
+  static __device__ f32x4_t mfma16(u32x2_t a, u32x2_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, b), c, 0, 0, 0);
+  }
+  // x as a sum of terms of this type: 3 x 8 bits are all of it.
+  static constexpr int kTerms = 3;
+  static constexpr float kTermsBias = 0.0f;
+  static __device__ uint32_t take(float& x0, float& x1) {
+    const uint32_t b0 = __builtin_bit_cast(uint32_t, x0) & 0xffff0000u, b1 = __builtin_bit_cast(uint32_t, x1) & 0xffff0000u;
+    x0 -= __builtin_bit_cast(float, b0);
+    x1 -= __builtin_bit_cast(float, b1);
+    return b0 >> 16 | b1;
+  }
 };
 template <>
 struct Elem<_Float16> {
@@ -109,6 +124,20 @@ struct Elem<_Float16> {
   // Half weights lose bits below 2^-14: they are formed 2^7 times as large, at
   // most 2^15 with kLazy.
   static constexpr float kBias = 7.0f;
+
+  static __device__ f32x4_t mfma16(u32x2_t a, u32x2_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, a), __builtin_bit_cast(f16x4_t, b), c, 0, 0, 0);
+  }
+  // Two terms of 11 bits, of weights of at most 2^15: what is left out is at most
+  // 2^-40 of the greatest weight, or 2^-22 of the weight itself.
+  static constexpr int kTerms = 2;
+  static constexpr float kTermsBias = 15.0f;
+  static __device__ uint32_t take(float& x0, float& x1) {
+    const auto h = __builtin_amdgcn_cvt_pkrtz(x0, x1);
+    x0 -= float(h[0]);
+    x1 -= float(h[1]);
+    return __builtin_bit_cast(uint32_t, h);
+  }
 };
 
 template <typename T>

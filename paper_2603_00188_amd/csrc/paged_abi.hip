@@ -144,9 +144,9 @@ AttnPlan attn_plan(const stlite_paged* c) {
   p.decode = most <= 1;
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
   if (p.decode) {
-    p.parts = int32_t(ceil_div(group, kDecHeads));
+    p.rows = group <= 16 ? 16 : 32;
+    p.parts = int32_t(ceil_div(group, p.rows));
     p.tokens = 1;
-    p.rows = kDecHeads;
     p.shares = 512;
     p.min_share = 64;
     p.item_cost = 64;
@@ -173,7 +173,7 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // scan of the lengths.  By boundary / by item: one token behind 3 sequences of up to
   // 79079 in 2 units 63.8 / 45.6 us, a long cache 73 / 64, 64 tokens behind 3000 66 / 30;
   // five layers' 4 tokens in 2 sequences behind 1468 24.5 / 29.4, one token in 46 27 / 34.
-  const int64_t item_rows = p.decode ? std::min<int64_t>(group, kDecHeads) : std::min<int64_t>(p.tokens, most) * group;
+  const int64_t item_rows = p.decode ? std::min<int64_t>(group, p.rows) : std::min<int64_t>(p.tokens, most) * group;
   p.join_items = items < p.shares && item_rows * p.shares >= 512 * items ? int32_t(items) : 0;
   p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : int32_t(item_rows);
   p.join_split = int32_t(ceil_div(item_rows, p.join_rows));

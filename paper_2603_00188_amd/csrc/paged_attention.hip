@@ -11,7 +11,6 @@ namespace stlite {
 namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 // The page table of one sequence as a wave reads it: 64 entries in a register,
 // one per lane, fetched by index without a memory access.
@@ -71,24 +70,31 @@ struct LdsPageWindow {
 // ---------------------------------------------------------------------------
 //
 // HBM-bound: the pass streams K and V once.  Four waves take 16-key sub-tiles of
-// a share in turn (a sub-tile lies in one page):
+// a share in turn (a sub-tile lies in one page), the next one's loads under this one's
+// arithmetic:
 //   S^T = K Q^T   16x16x32, cached rows as the A operand read straight from HBM,
-//                 the heads of the group (at most 16, zero padded) as B;
-//   O += P V      v_mfma_f32_16x16x4_f32, which takes one cached row per lane and
-//                 k-step: V needs no transpose and P stays fp32.
+//                 the heads of the group (zero padded to 16 or 32) as B;
+//   O += P V      16x16x16, whose layout takes P where S^T left it (four keys of a head
+//                 per lane) and V as it was read, four keys of a lane put together by
+//                 byte permutes.  P stays fp32 by way of terms: three bf16 (8 bits each),
+//                 or two fp16, a product each.  In fp32 products P and V took four times
+//                 as long, which two blocks of heads could not hide: 20 heads of a kv
+//                 head 66 us (16 at a time), now 48 with 32 at once and 64 with 16.
+// 28 layers x 28 heads behind 30105 tokens 267 us (1.73 GB, 6.5 TB/s), a layer behind
+// 150528 54 (308 MB, 5.7), 64 sequences of up to 8000 in 4 layers 697 (4.62 GB, 6.6).
 constexpr int kDecWaves = 4;
 
 __device__ inline u32x4_t load_row16(const uint16_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
 }
 
-template <typename T>
+template <typename T, int NG>  // 16 NG heads to an item
 __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
-  constexpr int NT = kDecWaves * 64;
-  __shared__ float sm_m[kDecWaves][kDecHeads], sm_l[kDecWaves][kDecHeads];
-  __shared__ float sm_o[kDecWaves][kDecHeads][kHeadDim];
+  constexpr int NT = kDecWaves * 64, kHeads = 16 * NG;
+  __shared__ float sm_m[kDecWaves][kHeads], sm_l[kDecWaves][kHeads];
+  __shared__ float sm_o[kDecWaves][kHeads][kHeadDim];
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
   const PagedDev& c = a.c;
   PagedPlan<NT> plan(a, sm_plan);
@@ -104,26 +110,27 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
   for (bool first = true;; first = false) {
     const int unit = it.unit / a.parts, part = it.unit % a.parts;
     const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
-    const int32_t heads = min(c.group - part * kDecHeads, kDecHeads);
+    const int32_t heads = min(c.group - part * kHeads, kHeads);
     const PagedPart span = paged_part(x, y, it.start, it.keys);
     const bool whole = span.whole;
     const int32_t k0 = span.t0 * kPagedTile, k1 = min(span.t1 * kPagedTile, max(it.cached + it.n, 0));
-    const int64_t qrow = (int64_t(layer) * c.total_new + it.row0) * c.n_q_heads + int64_t(kv) * c.group + part * kDecHeads;
+    const int64_t qrow = (int64_t(layer) * c.total_new + it.row0) * c.n_q_heads + int64_t(kv) * c.group + part * kHeads;
 
-    x8 qb[4];
+    x8 qb[NG][4];
     {
-      const uint16_t* p = a.q + (qrow + head) * kHeadDim;
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        u32x4_t w = u32x4_t{0u, 0u, 0u, 0u};
-        if (head < heads) w = *reinterpret_cast<const u32x4_t*>(p + kk * 32 + quad * 8);
-        qb[kk] = __builtin_bit_cast(x8, w);
+      for (int ng = 0; ng < NG; ++ng) {
+        const uint16_t* p = a.q + (qrow + 16 * ng + head) * kHeadDim;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          u32x4_t w = u32x4_t{0u, 0u, 0u, 0u};
+          if (16 * ng + head < heads) w = *reinterpret_cast<const u32x4_t*>(p + kk * 32 + quad * 8);
+          qb[ng][kk] = __builtin_bit_cast(x8, w);
+        }
       }
     }
-    float m_run = -INFINITY, l_run = 0.0f;
-    f32x4_t o[8];  // O[head 4 quad + r][dim 8 (lane & 15) + db]
-#pragma unroll
-    for (int db = 0; db < 8; ++db) o[db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run[NG], l_run[NG];
+    f32x4_t o[NG][8];  // O[head 16 ng + 4 quad + r][dim 8 (lane & 15) + db]
 
     PageWindow pages(c, it.seq);
     u32x4_t kx[4], vx[4];
@@ -144,73 +151,135 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
       }
       return pages.is_bad(entry);
     };
-    int32_t j0 = k0 + 16 * wave;
-    bool bad_next = false;
-    if (j0 < k1) bad_next = load(j0);
-    for (; j0 < k1; j0 += 16 * kDecWaves) {
-      const u32x4_t kc[4] = {kx[0], kx[1], kx[2], kx[3]};
-      u32x4_t vc[4] = {vx[0], vx[1], vx[2], vx[3]};
-      const bool bad = bad_next;
-      if (j0 + 16 * kDecWaves < k1) bad_next = load(j0 + 16 * kDecWaves);
-      if (bad) continue;
-      f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // The share's sub-tiles.  A term of a weight may be zero, and zero times infinity is no
+    // infinity: where something came out that is not finite, once more without the values
+    // that are not, which are then added (p v is v for them, whatever the weight).
+    bool again = false;
+    for (bool odd = false;; odd = true) {
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) s = E::mfma16(__builtin_bit_cast(x8, kc[kk]), qb[kk], s);
-      float xs[4];
+      for (int ng = 0; ng < NG; ++ng) {
+        m_run[ng] = -INFINITY;
+        l_run[ng] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xs[i] = s[i] * a.scale2;
-      if (j0 + 16 > k1) {  // rows past the end: no weight, and nothing for it to meet
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (j0 + 4 * quad + i >= k1) {
-            xs[i] = -INFINITY;
-            vc[i] = u32x4_t{0u, 0u, 0u, 0u};
-          }
+        for (int db = 0; db < 8; ++db) o[ng][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       }
-      float mt = fmaxf(fmaxf(xs[0], xs[1]), fmaxf(xs[2], xs[3]));
-      mt = fmaxf(mt, __shfl_xor(mt, 16));
-      mt = fmaxf(mt, __shfl_xor(mt, 32));
-      const float m_new = fmaxf(m_run, mt);
-      const float m_use = m_new == -INFINITY ? 0.0f : m_new;
-      if (__ballot(m_new > m_run)) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-        l_run *= alpha;
+      int32_t j0 = k0 + 16 * wave;
+      bool bad_next = false;
+      if (j0 < k1) bad_next = load(j0);
+      for (; j0 < k1; j0 += 16 * kDecWaves) {
+        const u32x4_t kc[4] = {kx[0], kx[1], kx[2], kx[3]};
+        u32x4_t vc[4] = {vx[0], vx[1], vx[2], vx[3]};
+        const bool bad = bad_next;
+        if (j0 + 16 * kDecWaves < k1) bad_next = load(j0 + 16 * kDecWaves);
+        if (bad) continue;
+        const bool ends = j0 + 16 > k1;
+        if (ends) {  // rows past the end: no weight, and nothing for it to meet
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float ar = __shfl(alpha, 4 * quad + r);
-#pragma unroll
-          for (int db = 0; db < 8; ++db) o[db][r] *= ar;
+          for (int i = 0; i < 4; ++i)
+            if (j0 + 4 * quad + i >= k1) vc[i] = u32x4_t{0u, 0u, 0u, 0u};
         }
-        m_run = m_new;
-      }
-      float p[4];
+        if (odd) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(xs[i] - m_use);
-      l_run += (p[0] + p[1]) + (p[2] + p[3]);
-      // k-step i pairs lane (head, quad) with key j0 + 4 quad + i
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < 4; ++j) vc[i][j] &= ~((E::not_finite(vc[i][j]) >> 15) * 0xffffu);
+        }
+        u32x2_t terms[NG][E::kTerms];  // the weights of four keys
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng) {
+          f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) s = E::mfma16(__builtin_bit_cast(x8, kc[kk]), qb[ng][kk], s);
+          float xs[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xs[i] = ends && j0 + 4 * quad + i >= k1 ? -INFINITY : s[i] * a.scale2;
+          float mt = fmaxf(fmaxf(xs[0], xs[1]), fmaxf(xs[2], xs[3]));
+          mt = fmaxf(mt, __shfl_xor(mt, 16));
+          mt = fmaxf(mt, __shfl_xor(mt, 32));
+          const float m_new = fmaxf(m_run[ng], mt);
+          const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+          if (__ballot(m_new > m_run[ng])) {
+            const float alpha = __builtin_amdgcn_exp2f(m_run[ng] - m_use);
+            l_run[ng] *= alpha;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float ar = __shfl(alpha, 4 * quad + r);
+#pragma unroll
+              for (int db = 0; db < 8; ++db) o[ng][db][r] *= ar;
+            }
+            m_run[ng] = m_new;
+          }
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(xs[i] - m_use + E::kTermsBias);
+          l_run[ng] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+          for (int n = 0; n < E::kTerms; ++n) {
+            terms[ng][n][0] = E::take(p[0], p[1]);
+            terms[ng][n][1] = E::take(p[2], p[3]);
+          }
+        }
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
-          const float b = (db & 1) ? elem_hi<T>(vc[i][db >> 1]) : elem_lo<T>(vc[i][db >> 1]);
-          o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[i], b, o[db], 0, 0, 0);
+          const uint32_t half = (db & 1) ? 0x07060302u : 0x05040100u;
+          u32x2_t b;  // dimension db of the lane's four keys
+          b[0] = __builtin_amdgcn_perm(vc[1][db >> 1], vc[0][db >> 1], half);
+          b[1] = __builtin_amdgcn_perm(vc[3][db >> 1], vc[2][db >> 1], half);
+#pragma unroll
+          for (int n = 0; n < E::kTerms; ++n)
+#pragma unroll
+            for (int ng = 0; ng < NG; ++ng) o[ng][db] = E::mfma16(terms[ng][n], b, o[ng][db]);
         }
+      }
+      if (odd) break;
+      float z = 0.0f;
+#pragma unroll
+      for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z = fmaf(o[ng][db][r], 0.0f, z);
+      again = __ballot(z != z) != 0;
+      if (!again) break;
     }
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
+    if (again) {
+#pragma unroll 1
+      for (int32_t j = k0 + 16 * wave; j < k1; j += (j & 15) == 15 ? 16 * kDecWaves - 15 : 1) {
+        pages.seek(j >> c.page_shift);
+        if (pages.is_bad(j >> c.page_shift)) continue;
+        const u32x4_t e = load_row16(c.v + (page_row(c, unit, pages.page(j >> c.page_shift)) + (j & in_page)) * kHeadDim + (lane & 15) * 8);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+          const uint32_t bits = e[db >> 1] >> (16 * (db & 1)) & 0xffffu;
+          const float x = E::not_finite(bits) ? elem_lo<T>(bits) : 0.0f;
+#pragma unroll
+          for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[ng][db][r] += x;
+        }
+      }
+    }
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) {
+      l_run[ng] += __shfl_xor(l_run[ng], 16);
+      l_run[ng] += __shfl_xor(l_run[ng], 32);
+    }
 
     // Merge the waves (one without rows has max -inf and weighs nothing).
     if (!first) __syncthreads();  // the last item's merge has read these
-    if (lane < kDecHeads) {
-      sm_m[wave][lane] = m_run;
-      sm_l[wave][lane] = l_run;
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) {
+      if (lane < 16) {
+        sm_m[wave][16 * ng + lane] = m_run[ng];
+        sm_l[wave][16 * ng + lane] = l_run[ng];
+      }
+#pragma unroll
+      for (int db = 0; db < 8; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sm_o[wave][16 * ng + 4 * quad + r][(lane & 15) * 8 + db] = o[ng][db][r];
     }
-#pragma unroll
-    for (int db = 0; db < 8; ++db)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sm_o[wave][4 * quad + r][(lane & 15) * 8 + db] = o[db][r];
     __syncthreads();
-    const int64_t slot = paged_slot(blockIdx.x, plan.share, it.start) * kDecHeads;
+    const int64_t slot = paged_slot(blockIdx.x, plan.share, it.start) * kHeads;
     for (int e = threadIdx.x; e < heads * (kHeadDim / 2); e += NT) {
       const int h = e / (kHeadDim / 2), dim = e % (kHeadDim / 2) * 2;
       float M = -INFINITY;
@@ -280,7 +349,6 @@ constexpr int kTileLoads = 4;  // DMA instructions of a wave per tile: it fetche
 
 // Four keys of one dimension per lane: each group of 16 lanes reads 4 rows of 16
 // elements (lane i: row i >> 2, elements 4 (i & 3) ..) and gets them transposed.
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
 __device__ inline u32x2_t read_transposed(uint32_t lds) {
   typedef __attribute__((address_space(3))) s16x4_t* ptr_t;
   return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr_t)(uintptr_t)lds));
@@ -667,8 +735,8 @@ __global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnA
   const int unit = it.unit / a.parts, part = it.unit % a.parts;
   const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
   const int32_t tok0 = it.index * a.tokens;
-  const int32_t head0 = part * kDecHeads;  // (one part but for decode)
-  const int32_t rows = a.parts > 1 ? min(c.group - head0, kDecHeads) : min(it.n - tok0, a.tokens) * c.group;
+  const int32_t head0 = part * a.rows;  // (one part but for decode)
+  const int32_t rows = a.parts > 1 ? min(c.group - head0, a.rows) : min(it.n - tok0, a.tokens) * c.group;
   const int grp = threadIdx.x >> 5, l32 = threadIdx.x & 31;
   const int32_t first = blockIdx.y * a.join_rows, end = min(rows, first + a.join_rows);
   auto load = [&](int32_t w, int32_t row, float& m, float& l, f32x4_t& o) {
@@ -751,7 +819,8 @@ hipError_t launch_join(const PagedAttnArgs& a, hipStream_t stream) {
 
 template <typename T>
 hipError_t decode(const PagedAttnArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_decode_kernel<T>), dim3(a.shares), dim3(kDecWaves * 64), 0, stream, a);
+  if (a.rows == 16) hipLaunchKernelGGL((paged_decode_kernel<T, 1>), dim3(a.shares), dim3(kDecWaves * 64), 0, stream, a);
+  else hipLaunchKernelGGL((paged_decode_kernel<T, 2>), dim3(a.shares), dim3(kDecWaves * 64), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }

@@ -10,7 +10,8 @@ type relative to the value, 2^-8 bf16, 2^-11 fp16):
   within 24 * 2^-24 relative.  Together under 2^-18 (|n_a| + |n_b|), and half the
   smallest step of fp16, 2^-25.
 * attention: the output is rounded once, u |o|; with several new tokens the
-  weights are too, u sum_j p_j |v_j|.  A logit is a sum of 128 exact products in
+  weights are too, u sum_j p_j |v_j| (with one they are fp32, or fp16 terms whose sum
+  is off by 2^-22 relative or 2^-40 of the greatest: inside what follows).  A logit is a sum of 128 exact products in
   fp32, off by at most 128 * 2^-24 of scale sum_c |q_c k_c|, and its weight by
   twice that (numerator and denominator); the exponential and its argument,
   |x| <= the same sum, by 2^-22 (1 + that); sums of n weights by n 2^-24 each in
@@ -261,6 +262,37 @@ def test_masked_values_have_no_influence(torch_cuda, new, dtype):
     assert torch.equal(out[~hit], clean[~hit])
     assert (out[0, first[0]:f.cu[1], 0:3, 5] == float("inf")).all() and (out[0, first[0]:f.cu[1], 0:3, 6] == float("-inf")).all()
     assert torch.isnan(out[0, first[1]:f.cu[2], 3:6, 7]).all() and torch.isnan(out[0, first[2]:f.cu[3], 3:6, :]).all()
+
+
+@pytest.mark.parametrize("new,hq", [(1, 3), (1, 20), (1, 40), (4, 20), (70, 3)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_values_that_are_seen_and_not_finite(torch_cuda, new, hq, dtype):
+    """They reach every token and head, with the greatest weight or none to speak of, and
+    no other dimension.  With several tokens the weights are rounded to the type of the
+    call first, and one below half its smallest step becomes 0: 0 * infinity is NaN."""
+    import torch
+    f = Served((300, 70), (new, new), 16, dtype, 1, hq, 1, seed=18)
+    q = f.randn((1, f.total, hq, D), 4.0)
+    clean = f.attend(q).clone()
+    v = f.v.view(1, 1, -1, D)
+    row = lambda s, j: OP.place(f.table, s, j, 16, f.n_pages)  # noqa: E731
+    v[0, 0, row(0, 0), 3] = v[0, 0, row(0, 77), 3] = float("inf")
+    v[0, 0, row(0, 78), 4] = float("-inf")
+    v[0, 0, row(0, 16), 127], v[0, 0, row(0, 17), 127] = float("inf"), float("-inf")
+    f.k.view(1, 1, -1, D)[0, 0, row(0, 78)] *= -8
+    k = f.k.clone()
+    dims = torch.tensor([d for d in range(D) if d not in (3, 4, 127)], device="cuda")
+    out = f.attend(q)
+    first = slice(0, int(f.cu[1]))
+    zero = torch.isnan(out[0, first]) & (new > 1)
+    assert ((out[0, first, :, 3] == float("inf")) | zero[..., 3]).all()
+    assert ((out[0, first, :, 4] == float("-inf")) | zero[..., 4]).all()
+    assert torch.isnan(out[0, first, :, 127]).all()
+    assert torch.equal(out[:, f.cu[1]:], clean[:, f.cu[1]:])
+    v[0, 0, row(0, 0), 3] = v[0, 0, row(0, 77), 3] = v[0, 0, row(0, 78), 4] = 0
+    v[0, 0, row(0, 16), 127] = v[0, 0, row(0, 17), 127] = 0
+    assert torch.equal(f.k, k)
+    assert torch.equal(out[..., dims], f.attend(q)[..., dims])
 
 
 @pytest.mark.parametrize("new", [1, 3, 140])
