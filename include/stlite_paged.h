@@ -160,7 +160,7 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  * What the mask leaves out has no influence, NaN and infinities among it.
  *   q    [n_layers][total_new][n_q_heads][d], 16-byte aligned
  *   out  the same layout and type; 16-byte aligned, must not alias q
- *   scale  finite, > 0
+ *   scale  > 0, at most 2^127
  * fp32 logits, softmax statistics and sums.  With one new token per sequence the
  * weights keep fp32's 24 bits (fp16: 22, or 2^-40 of the greatest weight); with more
  * they are rounded to the type of the call before they meet v.  An infinity or NaN of

@@ -40,6 +40,7 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int32_t kMaxGroup = 128;
 constexpr int64_t kMaxLen = int64_t(1) << 28;
 constexpr int64_t kIntRows = (int64_t(1) << 31) - 1;
@@ -334,7 +335,8 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
                                      size_t ws_bytes, void* stream) {
   const stlite_status st = check_cache(c, true);
   if (st != STLITE_OK) return st;
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(STLITE_ERR_INVALID_ARG, "scale must be finite and > 0");
+  if (!(scale > 0.0f) || !std::isfinite(scale * kLog2e))
+    return fail(STLITE_ERR_INVALID_ARG, "scale must be > 0 and at most 2^127");
   if (c->total_new == 0) return ok();
   const AttnPlan p = attn_plan(c);
   if (p.bytes > 0 && !ws) return fail(STLITE_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", p.bytes);
@@ -347,7 +349,7 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.c = device_view(c);
   a.q = q;
   a.out = out;
-  a.scale2 = scale * 1.4426950408889634f;
+  a.scale2 = scale * kLog2e;
   a.parts = p.parts;
   a.tokens = p.tokens;
   a.rows = p.rows;

@@ -239,7 +239,7 @@ def test_attention_rejections():
     assert lib.stlite_paged_workspace_size(f.ref, ctypes.byref(n)) == S.OK and n.value > 0 and n.value % 256 == 0
     call = lambda q=FAKE, scale=1.0, out=FAKE + 4096, ws=FAKE, nb=n.value: lib.stlite_paged_attention(  # noqa: E731
         f.ref, q, scale, out, ws, nb, None)
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 2.5e38):
         assert call(scale=scale) == S.ERR_INVALID_ARG and "scale" in _err()
     assert call(ws=None) == S.ERR_WORKSPACE
     assert call(nb=n.value - 1) == S.ERR_WORKSPACE
