@@ -30,7 +30,7 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
 def _is(t, name, shape, dtype, device):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (not contiguous)'}")
 
@@ -84,6 +84,7 @@ class NewTokens:
             raise ValueError("cu_new must be a list of n_seqs + 1 prefix sums")
         self.d = torch.from_numpy(self.h.copy()).to(device)
         self.total = int(self.h[-1])
+        self._h, self._d = self.h.ctypes.data, self.d.data_ptr()  # (a microsecond each time they are asked for)
 
 
 class PagedCache:
@@ -132,7 +133,7 @@ class PagedCache:
                 raise ValueError(f"the batch has {len(batch.h) - 1} sequences, the cache {self.n_seqs}")
             if batch.d.device != self.device:
                 raise ValueError(f"the batch is on {batch.d.device}, the cache on {self.device}")
-            c.total_new, c.cu_new, c.h_cu_new = batch.total, batch.d.data_ptr(), batch.h.ctypes.data
+            c.total_new, c.cu_new, c.h_cu_new = batch.total, batch._d, batch._h
         return c
 
     def validate(self, batch: NewTokens, page_table=None, seq_lens=None) -> None:
@@ -159,14 +160,15 @@ class PagedCache:
 
 
 def _rows(t, name, cache, batch, heads):
-    if tuple(t.shape) != (cache.n_layers, batch.total, heads, HEAD_DIM) or t.dtype != cache.dtype or t.device != cache.device:
-        raise ValueError(f"{name} must be {cache.dtype} {(cache.n_layers, batch.total, heads, HEAD_DIM)} on {cache.device}, "
+    n = batch.total
+    if t.shape != (cache.n_layers, n, heads, HEAD_DIM) or t.dtype != cache.dtype or t.device != cache.device:
+        raise ValueError(f"{name} must be {cache.dtype} {(cache.n_layers, n, heads, HEAD_DIM)} on {cache.device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     layer, token, head, dim = t.stride()
-    if batch.total and ((dim, head) != (1, HEAD_DIM) and (dim != 1 or heads > 1)):
+    if n and (dim != 1 or (head != HEAD_DIM and heads > 1)):
         raise ValueError(f"{name}: a token's heads must lie one after another (strides {t.stride()})")
     # (a size-1 axis may carry any stride)
-    return _CRows(t.data_ptr(), token if batch.total > 1 else heads * HEAD_DIM, layer if cache.n_layers > 1 else 0)
+    return _CRows(t.data_ptr(), token if n > 1 else heads * HEAD_DIM, layer if cache.n_layers > 1 else 0)
 
 
 def paged_compact(cache: PagedCache, p, k, v, kept, per_layer: bool = False, stream=None) -> None:
