@@ -303,7 +303,12 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
       a.axis2 = s[0] + s[1];
     }
     a.interleaved = rope->interleaved;
-    for (int i = 0; i < 64; ++i) a.turns[i] = std::pow(rope->theta, -i / 64.0) / (2.0 * M_PI);
+    double coarse[8], fine[8];  // (16 powers instead of 64: a microsecond of the host's)
+    for (int i = 0; i < 8; ++i) {
+      coarse[i] = std::pow(rope->theta, -i / 8.0) / (2.0 * M_PI);
+      fine[i] = std::pow(rope->theta, -i / 64.0);
+    }
+    for (int i = 0; i < 64; ++i) a.turns[i] = coarse[i / 8] * fine[i % 8];
   }
   if (c->total_new == 0) return ok();
   st = check_rows(k, c->n_kv_heads, "k");

@@ -155,6 +155,8 @@ DECODE = [
     ((3000,), (1,), 16, "bf16", 1, 40, 1),             # one sequence, three head groups, each cut
     ((9000,), (1,), 16, "fp16", 2, 2, 2),              # one row to an item, more parts than are joined at once
     (tuple(range(1, 300, 3)), (1,) * 100, 16, "bf16", 1, 4, 1),
+    ((9000, 40, 0, 6000), (1, 0, 1, 1), 16, "bf16", 1, 7, 1),  # few items, each in many parts, idle sequences between
+    ((5000, 300, 7000), (1, 1, 1), 64, "fp16", 1, 40, 1),      # the same with two head groups
 ]
 
 
@@ -200,6 +202,7 @@ EXTEND = [
     ((3000,), (60,), 16, "fp16", 1, 128, 1),              # items of one sequence, each in many parts
     ((900,) * 6, (200,) * 6, 32, "bf16", 3, 8, 2),        # items cut in two
     ((3, 0, 2), (5, 3, 9), 16, "bf16", 1, 2, 1),          # shorter than their new tokens
+    ((9000, 40, 3000, 10), (3, 0, 40, 1), 32, "fp16", 1, 7, 1),  # few items, each in many parts
 ]
 
 
@@ -214,6 +217,16 @@ def test_extend(torch_cuda, lens, new, page, dtype, layers, hq, hk):
         for t in range(max(new[s] - n, 0)):
             assert not out[:, f.cu[s] + t].any()
     assert np.array_equal(_bits(f.attend(q)), _bits(out)), "two calls differ"
+
+
+def test_extend_many_sequences(torch_cuda):
+    """More sequences than threads look them up, idle ones among them."""
+    rng = np.random.default_rng(4)
+    new = rng.integers(0, 4, 1100)
+    lens = [int(n + rng.integers(0, 90)) for n in new]
+    f = Served(lens, new.tolist(), 16, "fp16", 1, 2, 1, fill=float("nan"))
+    q = f.randn((1, f.total, 2, D))
+    f.compare(q, f.attend(q))
 
 
 @pytest.mark.parametrize("new", [1, 4, 150])
