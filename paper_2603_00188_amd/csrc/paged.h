@@ -71,6 +71,7 @@ struct PagedAttnArgs {
   int32_t item_cost;  // places that beginning an item takes
   int32_t join_items;  // joining by item: their number; 0: by boundary
   int32_t join_rows;  // rows of an item per joining work-group
+  int32_t join_groups;  // rows that a joining work-group takes at once, 8 or 32
   int32_t join_split;  // joining work-groups per item or boundary
   float* pm;          // workspace [shares][2][rows]: max (log2 units)
   float* pl;          // workspace [shares][2][rows]: sum

@@ -129,7 +129,7 @@ PagedDev device_view(const stlite_paged* c) {
 // several-token kernel: 18 us for 11, 72 for 64, 309 for 270, 806 for 729.
 struct AttnPlan {
   bool decode;
-  int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows, join_split;
+  int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows, join_groups, join_split;
   size_t bytes;
 };
 
@@ -169,14 +169,20 @@ AttnPlan attn_plan(const stlite_paged* c) {
   p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(range / p.min_share))));
   // Joining by boundary gives every cut item to one work-group (with a quarter of its
   // rows each, and four times the work-groups, prompts of 131 to 2999 tokens took 220 us,
-  // with all of them 216).  Where that is more than four rounds of its loads on average,
-  // one round of work-groups (two per CU) shares out the items' rows, which costs a second
-  // scan of the lengths.  By boundary / by item: one token behind 3 sequences of up to
-  // 79079 in 2 units 63.8 / 45.6 us, a long cache 73 / 64, 64 tokens behind 3000 66 / 30;
-  // five layers' 4 tokens in 2 sequences behind 1468 24.5 / 29.4, one token in 46 27 / 34.
+  // with all of them 216).  Where that is more than a round of its loads on average (rows
+  // times parts over 32 groups of lanes, four loads each), one round of work-groups (two
+  // per CU) shares out the items' rows, which costs a second scan of the lengths.  By
+  // boundary / by item: one token behind 3 sequences of up to 79079 in 2 units 63.8 / 45.6
+  // us, 4 of up to 6000 in 4 units 28.0 / 21.4, two layers of one behind 8000 24.2 / 18.4;
+  // 16 of up to 1000 in 4 units 19.0 / 24.0, five drafted tokens in 16 in 8 62 / 65.
   const int64_t item_rows = p.decode ? std::min<int64_t>(group, p.rows) : std::min<int64_t>(p.tokens, most) * group;
-  p.join_items = items < p.shares && item_rows * p.shares >= 512 * items ? int32_t(items) : 0;
+  p.join_items = items < p.shares && item_rows * p.shares >= 128 * items ? int32_t(items) : 0;
   p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : int32_t(item_rows);
+  // A boundary's work-group has 256 threads where that is few rounds of loads too, so that
+  // the 511 of one token run at once, else 1024.  256 / 1024 threads: 8 sequences of up to
+  // 1000 16.6 / 20.2 us, 64 of up to 150 in 8 layers 41 / 44, a step 263 / 266; the 255
+  // of several tokens gain less, five drafted ones in 16 sequences 64 / 62.
+  p.join_groups = !p.join_items && item_rows * (items + p.shares) <= (p.decode ? 128 : 64) * items ? 8 : 32;
   p.join_split = int32_t(ceil_div(item_rows, p.join_rows));
   const size_t slots = size_t(p.shares) * 2 * p.rows;
   p.bytes = p.shares == 1 ? 0 : 2 * align_up(slots * sizeof(float)) + align_up(slots * kHeadDim * sizeof(float));
@@ -363,6 +369,7 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.item_cost = p.item_cost;
   a.join_items = p.join_items;
   a.join_rows = p.join_rows;
+  a.join_groups = p.join_groups;
   a.join_split = p.join_split;
   const size_t slots = size_t(p.shares) * 2 * p.rows;
   a.pm = static_cast<float*>(ws);

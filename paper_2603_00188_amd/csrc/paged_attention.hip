@@ -696,12 +696,11 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 // between shares x and x + 1 cuts, if x is the first share in it, or with join_items
 // (few items in many parts) item x.  32 lanes x 4 dimensions hold a row;
 // its parts (two mostly, up to all shares for one token over a long cache) are spread
-// over the groups of lanes that the rows leave, kBatch loads at once, and merged
+// over the groups of lanes (8 or 32) that the rows leave, kBatch loads at once, and merged
 // through LDS.  Bound by latency for one token (6 us for 11 parts of a layer, 8 us for
 // 128 parts of 32k keys, 9 us for the 512 shares of 28 layers), by the partials' bytes
 // for several (68 MB of 255 cut items: 19 us, 3.5 TB/s).
 constexpr int kBatch = 4;
-constexpr int kJoinGroups = 32;
 
 struct Joined {
   float m = -INFINITY, l = 0.0f;
@@ -718,11 +717,11 @@ struct Joined {
   }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnArgs a) {
-  constexpr int NT = kJoinGroups * 32;
-  __shared__ float sm_m[kJoinGroups], sm_l[kJoinGroups];
-  __shared__ f32x4_t sm_o[kJoinGroups][32];
+template <typename T, int GROUPS>
+__global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a) {
+  constexpr int NT = GROUPS * 32;
+  __shared__ float sm_m[GROUPS], sm_l[GROUPS];
+  __shared__ f32x4_t sm_o[GROUPS][32];
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
   const PagedDev& c = a.c;
   PagedPlan<NT> plan(a, sm_plan);
@@ -762,7 +761,7 @@ __global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnA
     *reinterpret_cast<u32x2_t*>(a.out + orow * kHeadDim + 4 * l32) = e;
   };
   if (w1 - w0 == 1) {  // two parts: a row per group (through the loop below prompts took 218 us, not 211)
-    for (int32_t row = first + grp; row < end; row += kJoinGroups) {
+    for (int32_t row = first + grp; row < end; row += GROUPS) {
       float m[2], l[2];
       f32x4_t o[2];
 #pragma unroll
@@ -774,10 +773,10 @@ __global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnA
     }
     return;
   }
-  for (int32_t row0 = first; row0 < end; row0 += kJoinGroups) {
-    const int32_t here = min(end - row0, kJoinGroups);
+  for (int32_t row0 = first; row0 < end; row0 += GROUPS) {
+    const int32_t here = min(end - row0, GROUPS);
     // groups per row: none without parts
-    const int per_row = min(kJoinGroups / here, (w1 - w0 + kBatch) / kBatch);
+    const int per_row = min(GROUPS / here, (w1 - w0 + kBatch) / kBatch);
     const int32_t row = row0 + grp / per_row;
     Joined r;
     if (row < row0 + here)
@@ -817,8 +816,9 @@ __global__ __launch_bounds__(kJoinGroups * 32) void paged_join_kernel(PagedAttnA
 template <typename T>
 hipError_t launch_join(const PagedAttnArgs& a, hipStream_t stream) {
   if (a.shares < 2) return hipSuccess;
-  hipLaunchKernelGGL((paged_join_kernel<T>), dim3(a.join_items ? a.join_items : a.shares - 1, a.join_split),
-                     dim3(kJoinGroups * 32), 0, stream, a);
+  const dim3 grid(a.join_items ? a.join_items : a.shares - 1, a.join_split);
+  if (a.join_groups == 8) hipLaunchKernelGGL((paged_join_kernel<T, 8>), grid, dim3(8 * 32), 0, stream, a);
+  else hipLaunchKernelGGL((paged_join_kernel<T, 32>), grid, dim3(32 * 32), 0, stream, a);
   return hipGetLastError();
 }
 
