@@ -100,15 +100,16 @@ struct Elem<__bf16> {
   __device__ static f32x4_t mfma16(x8 a, x8 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   // Pairs of a dword whose exponent is all ones (bits 15 and 31).
   __device__ static uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-  // Weights are at most 2^8 of their running maximum's (kLazy): any exponent fits.
-  static constexpr float kBias = 0.0f;
+  // Weights are formed at most 2^-20 large (2^8 of their running maximum's with kLazy),
+  // so that the sums of 2^20 keys' values of any size stay finite before the division.
+  static constexpr float kBias = -28.0f;
 
   static __device__ f32x4_t mfma16(u32x2_t a, u32x2_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, b), c, 0, 0, 0);
   }
   // x as a sum of terms of this type: 3 x 8 bits are all of it.
   static constexpr int kTerms = 3;
-  static constexpr float kTermsBias = 0.0f;
+  static constexpr float kTermsBias = -20.0f;  // (as kBias)
   static __device__ uint32_t take(float& x0, float& x1) {
     const uint32_t b0 = __builtin_bit_cast(uint32_t, x0) & 0xffff0000u, b1 = __builtin_bit_cast(uint32_t, x1) & 0xffff0000u;
     x0 -= __builtin_bit_cast(float, b0);

@@ -339,6 +339,13 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // groups' products of step t - 1, the last readers, are done by then.  At the end of
 // its products a wave waits for all but its last tile's DMA, so that K(t+1) and V(t)
 // have landed for everybody when anyone's step t begins.
+//
+// A step of 256 rows x 64 keys takes 3680 cycles, 2048 of them matrix instructions on
+// every SIMD; by its instructions the softmax half is the longer one, and LDS reads take
+// about 1420 of a half's 1840 cycles.  3136 tokens x 28 heads behind 30105 tokens take 1.38 ms, 1.03 PFLOP/s, at
+// the 1.8 GHz that the power leaves; five tokens in each of 16 sequences 60 us, where the
+// cache (225 MB) comes at 5.9 TB/s once the first tiles have; prompts of 131 to 2999
+// tokens 206 us, 0.73 PFLOP/s.
 
 constexpr float kLazy = 8.0f;
 constexpr int kExtWaves = 8;

@@ -309,6 +309,23 @@ def test_values_that_are_seen_and_not_finite(torch_cuda, new, hq, dtype):
 
 
 @pytest.mark.parametrize("new", [1, 3, 140])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_values_at_the_limits_of_the_type(torch_cuda, new, dtype):
+    """Sums of the greatest and the smallest normal values."""
+    import torch
+    f = Served((1500, 300, 200), (new,) * 3, 16, dtype, 1, 7, 1, seed=19)
+    info = torch.finfo(f.dt)
+    f.v[..., 0::4] = info.max
+    f.v[..., 1::4] = -info.max
+    f.v[..., 2::4] *= info.max / 16
+    f.v[..., 3] = 2.0 ** -40 if dtype == "bf16" else info.tiny
+    q = f.randn((1, f.total, 7, D), 1.5)
+    out = f.attend(q)
+    assert torch.isfinite(out).all()
+    f.compare(q, out)
+
+
+@pytest.mark.parametrize("new", [1, 3, 140])
 def test_pages_out_of_range_are_left_out(torch_cuda, new):
     import torch
     f = Served((300, 200, 150, 260), (new,) * 4, 16, "bf16", 1, 4, 2, seed=7, fill=float("nan"))
