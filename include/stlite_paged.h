@@ -161,13 +161,13 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  *   q    [n_layers][total_new][n_q_heads][d], 16-byte aligned
  *   out  the same layout and type; 16-byte aligned, must not alias q
  *   scale  > 0, at most 2^127
- * fp32 logits, softmax statistics and sums, which stay finite for values of any size
- * and up to 2^20 keys.  With one new token per sequence the
- * weights keep fp32's 24 bits (fp16: 22, or 2^-40 of the greatest weight); with more
- * they are rounded to the type of the call before they meet v.  An infinity or NaN of
- * a token that is seen reaches the output whatever its weight (an infinity of a weight
- * that is rounded to 0 as NaN).  Rows of out belong to new tokens only: nothing behind total_new
- * is written.
+ * fp32 logits, softmax statistics and sums, which stay finite for values of any
+ * size and up to 2^20 keys.  With one new token per sequence the weights keep fp32's
+ * 24 bits (fp16: 22, or 2^-40 of the greatest weight); with more they are rounded to
+ * the type of the call before they meet v.  An infinity or NaN of a token that is
+ * seen reaches the output whatever its weight (an infinity of a weight that is
+ * rounded to 0 as NaN).  Rows of out belong to new tokens only: nothing behind
+ * total_new is written.
  */
 stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, float scale, uint16_t* out,
                                      void* workspace, size_t workspace_bytes, void* stream);

@@ -79,12 +79,15 @@ class NewTokens:
     """The new tokens of a call: prefix sums over the sequences, on the host and the device."""
 
     def __init__(self, cu_new, device="cuda"):
-        self.h = np.ascontiguousarray(cu_new, dtype=np.int32)
+        self.h = np.array(cu_new, dtype=np.int32)
         if self.h.ndim != 1 or len(self.h) < 2:
             raise ValueError("cu_new must be a list of n_seqs + 1 prefix sums")
         self.d = torch.from_numpy(self.h.copy()).to(device)
         self.total = int(self.h[-1])
         self._h, self._d = self.h.ctypes.data, self.d.data_ptr()  # (a microsecond each time they are asked for)
+
+    def __reduce__(self):  # a copy has addresses of its own
+        return NewTokens, (self.h, self.d.device)
 
 
 class PagedCache:

@@ -370,6 +370,15 @@ def test_cache_layout():
         c.layer(2)
 
 
+def test_copied_batches_have_their_own_addresses():
+    import copy
+    import pickle
+    a = P.NewTokens([0, 2, 5], device="cpu")
+    for b in (copy.copy(a), copy.deepcopy(a), pickle.loads(pickle.dumps(a))):
+        assert b.h is not a.h and b.h.tolist() == [0, 2, 5] and b.d.tolist() == [0, 2, 5] and b.total == 5
+        assert (b._h, b._d) == (b.h.ctypes.data, b.d.data_ptr()) and b._h != a._h and b._d != a._d
+
+
 def test_binding_rejects_tensors():
     c = _cache()
     table, lens = c.page_table, c.seq_lens
