@@ -124,7 +124,8 @@ stlite_status stlite_paged_workspace_size(const stlite_paged* c, size_t* bytes);
  * The kept rows of the compression into pages: for every unit u, sequence s and
  * j < B_s, row kept[u][cu_budget[s] + j] of k and v (the layout of
  * stlite_compact_kv) becomes token j of sequence s.  Exact row copies of 16-bit
- * patterns, bf16 or fp16 alike.  seq_lens[s] becomes B_s.  p and c must agree in
+ * patterns, which must be of the pool's type (the compression pass knows bf16 alone:
+ * its rows belong in a bf16 pool).  seq_lens[s] becomes B_s.  p and c must agree in
  * n_layers, n_kv_heads and n_seqs, and every B_s must be at most c->max_len; the
  * new tokens (total_new, cu_new, h_cu_new) are not read.  per_layer != 0: one
  * kept list per layer, as in stlite_compact_kv_layer.  A kept index outside

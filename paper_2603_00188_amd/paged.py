@@ -174,12 +174,33 @@ def _rows(t, name, cache, batch, heads):
     return _CRows(t.data_ptr(), token if n > 1 else heads * HEAD_DIM, layer if cache.n_layers > 1 else 0)
 
 
-def paged_compact(cache: PagedCache, p, k, v, kept, per_layer: bool = False, stream=None) -> None:
-    """The kept rows of the compression (problem p) into cache's pages; cache.seq_lens become the budgets."""
+def _check_source(cache: PagedCache, p, k, v) -> None:
+    """k and v of a compaction: rows of the pool's type, or 16-bit patterns as integers, which carry no type."""
     n = cache.n_layers * cache.n_kv_heads * p.total_tokens * HEAD_DIM
     for t, name in ((k, "k"), (v, "v")):
-        if t.numel() != n or t.element_size() != 2 or not t.is_contiguous() or t.device != cache.device:
-            raise ValueError(f"{name} must be a contiguous tensor of {n} 16-bit elements on {cache.device}")
+        if (t.numel() != n or t.dtype not in (cache.dtype, torch.int16, torch.uint16) or not t.is_contiguous()
+                or t.device != cache.device):
+            raise ValueError(f"{name} must be a contiguous tensor of {n} {cache.dtype} elements (or their bits as 16-bit "
+                             f"integers) on {cache.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def check_compression(cache: PagedCache, p, k, v) -> None:
+    """That the compression pass (problem p, bf16) can end in ``cache``; raises ValueError where it cannot."""
+    if cache.dtype != torch.bfloat16:
+        raise ValueError(f"the compression pass is bf16, the cache {cache.dtype}")
+    for what, mine, its in (("layers", cache.n_layers, p.n_layers), ("kv heads", cache.n_kv_heads, p.n_kv_heads),
+                            ("sequences", cache.n_seqs, p.n_seqs)):
+        if mine != its:
+            raise ValueError(f"the problem has {its} {what}, the cache {mine}")
+    kept = int(np.diff(p.h["cu_budget"]).max())
+    if kept > cache.max_len:
+        raise ValueError(f"a sequence keeps {kept} rows, more than the cache's max_len = {cache.max_len}")
+    _check_source(cache, p, k, v)
+
+
+def paged_compact(cache: PagedCache, p, k, v, kept, per_layer: bool = False, stream=None) -> None:
+    """The kept rows of the compression (problem p) into cache's pages; cache.seq_lens become the budgets."""
+    _check_source(cache, p, k, v)
     lists = cache.n_layers if per_layer else cache.n_layers * cache.n_kv_heads
     if (kept.dtype != torch.int32 or not kept.is_contiguous() or kept.device != cache.device
             or (p.total_budget and kept.numel() != lists * p.total_budget)):

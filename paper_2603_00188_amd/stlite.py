@@ -443,7 +443,7 @@ def compress(p: Problem, q_win, k, v, out: Buffers, alpha: float = 1.0, css: boo
              tsg: bool = True, stream=None, overlap: bool = False, mean_width: int = 0, cache=None) -> Buffers:
     """The whole pass: score, gate, saliency, select, compact (five C calls).
 
-    With ``cache`` (a paged.PagedCache) the kept rows go into its pages, which
+    With ``cache`` (a bf16 paged.PagedCache) the kept rows go into its pages, which
     serving goes on from, instead of out.k_out and out.v_out.
 
     mean_width > 0 ranks on the Mean-Attention prior (stlite_mean_attention of
@@ -456,6 +456,9 @@ def compress(p: Problem, q_win, k, v, out: Buffers, alpha: float = 1.0, css: boo
     Otherwise everything runs in order on ``stream``.
     """
     import torch
+    if cache is not None:
+        from . import paged
+        paged.check_compression(cache, p, k, v)
     main = stream if stream is not None else torch.cuda.current_stream()
     gate = out.gate if tsg else None
     if not overlap:
@@ -487,7 +490,6 @@ def compress(p: Problem, q_win, k, v, out: Buffers, alpha: float = 1.0, css: boo
     stlite_select_topk(p, prior, out.phi if css else None, out.gate if tsg else None, alpha,
                        out.kept, out.score, out.ws, main)
     if cache is not None:
-        from . import paged
         paged.paged_compact(cache, p, k, v, out.kept, stream=main)
     else:
         stlite_compact_kv(p, k, v, out.kept, out.k_out, out.v_out, main)

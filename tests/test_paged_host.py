@@ -475,3 +475,48 @@ def test_oracle_norm_and_attention_closed_forms():
     out, _, keys, _ = OP.attention(np.zeros((3, 1, 128)), k, v, table, [1, 99], [0, 2, 3], 16, 1.0, 1)
     assert not out[0].any() and np.allclose(out[1, 0], v[0, 2, 0]) and keys[:, 0].tolist() == [0, 1, 16]
     assert OP.new_places(table, [1, 99], [0, 2, 3], 16, 4, 16) == [None, 32, 63]
+
+
+# ---------------------------------------------------------------------------
+# Compaction: types and shapes, before anything is enqueued
+# ---------------------------------------------------------------------------
+
+
+def _compaction(dtype=torch.bfloat16, layers=2, hk=2, lens=(50, 60), max_len=40):
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    p = S.Problem(layers, 4 * hk, hk, 1, cu, np.zeros(len(lens) + 1), np.zeros((0, 3)), S.budgets(cu, 1, 2), device="cpu")
+    cache = P.PagedCache.alloc(2, 8, 2, 2, max_len, page_size=16, dtype=dtype, device="cpu")
+    k = torch.zeros((layers * hk, sum(lens), 128), dtype=torch.bfloat16)
+    return p, cache, k
+
+
+@needs_lib
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_compaction_refuses_another_type(dtype):
+    """Rows of one 16-bit type are not stored in a pool of the other; bit patterns carry no type."""
+    p, cache, k = _compaction(dtype)
+    kept = torch.zeros((4, p.total_budget), dtype=torch.int32)
+    other = torch.float16 if dtype == torch.bfloat16 else torch.bfloat16
+    for a, b in ((k.to(other), k.to(dtype)), (k.to(dtype), k.to(other)), (k.to(other), k.to(other))):
+        with pytest.raises(ValueError, match="must be"):
+            P.paged_compact(cache, p, a, b, kept)
+    for a in (k.to(dtype), k.to(torch.int16), k.view(torch.uint16)):
+        with pytest.raises(ValueError, match="run on a GPU"):  # nothing runs on the CPU
+            P.paged_compact(cache, p, a, a, kept)
+
+
+@needs_lib
+def test_compression_refuses_its_cache_first(monkeypatch):
+    """A cache that the pass cannot go into: refused with nothing enqueued."""
+    def enqueued(*a, **kw):
+        raise AssertionError("a stage was enqueued")
+    for stage in ("stlite_score_window", "stlite_tsg_gate", "stlite_css_saliency", "stlite_select_topk"):
+        monkeypatch.setattr(S, stage, enqueued)
+
+    class Out:
+        kept = torch.zeros((4, 55), dtype=torch.int32)
+    for change, text in ((dict(dtype=torch.float16), "bf16"), (dict(layers=3), "layers"), (dict(hk=1), "kv heads"),
+                         (dict(lens=(50,)), "sequences"), (dict(max_len=29), "max_len")):
+        p, cache, k = _compaction(**change)
+        with pytest.raises(ValueError, match=text):
+            S.compress(p, k, k, k, Out(), stream=0, cache=cache)
