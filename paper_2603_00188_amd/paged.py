@@ -65,7 +65,20 @@ class _On:
             torch.cuda.set_device(self.before)
 
 
-class Rope:
+class _Fixed:
+    """Attributes that the C structs took over at construction: set once, so that no call goes by another value."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__ and self.__dict__[name] is not value:  # (``+=`` on a tensor assigns the same one)
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: make another {type(self).__name__}, or write into "
+                                 "the tensor it holds")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+
+
+class Rope(_Fixed):
     """The position rotation (stlite_rope): one position axis, or three with ``sections`` pairs each."""
 
     def __init__(self, theta: float = 1e6, sections=(64,), interleaved: bool = False):
@@ -75,13 +88,14 @@ class Rope:
         self.c = _CRope(float(theta), int(bool(interleaved)), self.n_axes, (ctypes.c_int32 * 3)(*sections), 0)
 
 
-class NewTokens:
-    """The new tokens of a call: prefix sums over the sequences, on the host and the device."""
+class NewTokens(_Fixed):
+    """The new tokens of a call: prefix sums over the sequences, on the host and the device, which stay the same."""
 
     def __init__(self, cu_new, device="cuda"):
         self.h = np.array(cu_new, dtype=np.int32)
         if self.h.ndim != 1 or len(self.h) < 2:
             raise ValueError("cu_new must be a list of n_seqs + 1 prefix sums")
+        self.h.setflags(write=False)
         self.d = torch.from_numpy(self.h.copy()).to(device)
         self.total = int(self.h[-1])
         self._h, self._d = self.h.ctypes.data, self.d.data_ptr()  # (a microsecond each time they are asked for)
@@ -90,9 +104,12 @@ class NewTokens:
         return NewTokens, (self.h, self.d.device)
 
 
-class PagedCache:
+class PagedCache(_Fixed):
     """A pool of pages [n_layers][n_kv_heads][n_pages][page_size][128], the sequences' page table
-    [n_seqs][max_pages] int32 and their lengths [n_seqs] int32.  ``max_len``: no sequence grows longer."""
+    [n_seqs][max_pages] int32 and their lengths [n_seqs] int32.  ``max_len``: no sequence grows longer.
+
+    The tensors are the cache's for good (a captured graph and the caches of single layers hold them too): other
+    lengths or pages are written into them, ``cache.seq_lens.copy_(lens)``."""
 
     def __init__(self, k, v, page_table, seq_lens, n_q_heads: int, max_len: Optional[int] = None):
         if k.dim() != 5 or k.shape[4] != HEAD_DIM or k.dtype not in _DTYPES:
@@ -112,6 +129,9 @@ class PagedCache:
         self._c = _CPaged(self.n_layers, self.n_q_heads, self.n_kv_heads, HEAD_DIM, _DTYPES[k.dtype], self.page_size,
                           self.n_pages, self.n_seqs, self.max_pages, self.max_len, 0, k.data_ptr(), v.data_ptr(),
                           page_table.data_ptr(), seq_lens.data_ptr(), None, None)
+
+    def __reduce__(self):  # a copy has addresses of its own
+        return PagedCache, (self.k, self.v, self.page_table, self.seq_lens, self.n_q_heads, self.max_len)
 
     @classmethod
     def alloc(cls, n_layers: int, n_q_heads: int, n_kv_heads: int, n_seqs: int, max_len: int, page_size: int = 64,

@@ -520,3 +520,50 @@ def test_compression_refuses_its_cache_first(monkeypatch):
         p, cache, k = _compaction(**change)
         with pytest.raises(ValueError, match=text):
             S.compress(p, k, k, k, Out(), stream=0, cache=cache)
+
+
+# ---------------------------------------------------------------------------
+# What the binding froze at construction
+# ---------------------------------------------------------------------------
+
+
+def test_frozen_fields_are_not_assigned():
+    """The C structs hold addresses and sizes from construction: another tensor or size is refused, not ignored."""
+    c = _cache()
+    for name, other in (("k", c.k.clone()), ("v", c.v.clone()), ("page_table", c.page_table.clone()),
+                        ("seq_lens", c.seq_lens + 1), ("max_len", 39), ("n_q_heads", 4), ("n_pages", 8), ("n_seqs", 2),
+                        ("dtype", torch.float16)):
+        with pytest.raises(AttributeError, match=name):
+            setattr(c, name, other)
+    with pytest.raises(AttributeError):
+        del c.seq_lens
+    seq_lens = c.seq_lens
+    c.seq_lens += 1  # in place: the same tensor
+    c.seq_lens.add_(1)
+    assert c.seq_lens is seq_lens and c.seq_lens.tolist() == [2, 2, 2] and c._struct(None).seq_lens == seq_lens.data_ptr()
+    b = P.NewTokens([0, 1, 1, 4], device="cpu")
+    for name, other in (("h", b.h.copy()), ("d", b.d.clone()), ("total", 3)):
+        with pytest.raises(AttributeError, match=name):
+            setattr(b, name, other)
+    with pytest.raises(ValueError):  # the device's sums would no longer agree
+        b.h[1] = 2
+    r = P.Rope()
+    for name, other in (("n_axes", 3), ("c", P.Rope(sections=(16, 24, 24)).c)):
+        with pytest.raises(AttributeError, match=name):
+            setattr(r, name, other)
+
+
+def test_copied_caches():
+    import copy
+    import pickle
+    c = _cache()
+    c.seq_lens[1] = 7
+    one = copy.copy(c)  # the same tensors
+    assert one.seq_lens is c.seq_lens and one._struct(None).k == c.k.data_ptr()
+    for two in (copy.deepcopy(c), pickle.loads(pickle.dumps(c))):  # tensors, and so addresses, of their own
+        assert two.seq_lens.tolist() == [0, 7, 0] and two.k.data_ptr() != c.k.data_ptr() and two.max_len == 40
+        s = two._struct(None)
+        assert (s.k, s.v, s.page_table, s.seq_lens) == tuple(t.data_ptr() for t in (two.k, two.v, two.page_table, two.seq_lens))
+    r = P.Rope(1e4, (16, 24, 24), True)
+    for q in (copy.copy(r), copy.deepcopy(r)):
+        assert (q.n_axes, q.c.theta, q.c.interleaved, list(q.c.sections)) == (3, 1e4, 1, [16, 24, 24])
