@@ -163,7 +163,8 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  *   out  the same layout and type; 16-byte aligned, must not alias q
  *   scale  > 0, at most 2^127
  * fp32 logits, softmax statistics and sums, which stay finite for values of any
- * size and up to 2^20 keys.  With one new token per sequence the weights keep fp32's
+ * size and up to 2^20 keys, and for logits of any size in fp32's range (scale q . k
+ * log2(e) up to 2^128; a token that sees a greater one gets NaN).  With one new token per sequence the weights keep fp32's
  * 24 bits (fp16: 22, or 2^-40 of the greatest weight); with more they are rounded to
  * the type of the call before they meet v.  An infinity or NaN of a token that is
  * seen reaches the output whatever its weight (an infinity of a weight that is

@@ -100,7 +100,7 @@ struct Elem<__bf16> {
   __device__ static f32x4_t mfma16(x8 a, x8 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   // Pairs of a dword whose exponent is all ones (bits 15 and 31).
   __device__ static uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-  // Weights are formed at most 2^-20 large (2^8 of their running maximum's with kLazy),
+  // Weights are formed at most 2^-20 large (2^8 of those at the reference, with kLazy),
   // so that the sums of 2^20 keys' values of any size stay finite before the division.
   static constexpr float kBias = -28.0f;
 
@@ -155,6 +155,14 @@ __device__ inline uint32_t elem_pack(float lo, float hi) {  // each rounded to n
   typedef T pair_t __attribute__((ext_vector_type(2)));
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, pair_t));
+}
+
+// A logit in base 2, rounded: what a maximum is taken of and what it is taken from have
+// to be the same number.  (Contracted, s scale - maximum is the unrounded product's
+// distance, which for logits of 2^31 is up to 2^7.)
+__device__ inline float base2(float s, float scale2) {
+#pragma clang fp contract(off)
+  return s * scale2;
 }
 
 __device__ inline int32_t paged_len(const PagedDev& c, int32_t s) { return min(max(c.seq_lens[s], 0), c.max_len); }

@@ -192,7 +192,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
           for (int kk = 0; kk < 4; ++kk) s = E::mfma16(__builtin_bit_cast(x8, kc[kk]), qb[ng][kk], s);
           float xs[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) xs[i] = ends && j0 + 4 * quad + i >= k1 ? -INFINITY : s[i] * a.scale2;
+          for (int i = 0; i < 4; ++i) xs[i] = ends && j0 + 4 * quad + i >= k1 ? -INFINITY : base2(s[i], a.scale2);
           float mt = fmaxf(fmaxf(xs[0], xs[1]), fmaxf(xs[2], xs[3]));
           mt = fmaxf(mt, __shfl_xor(mt, 16));
           mt = fmaxf(mt, __shfl_xor(mt, 32));
@@ -327,8 +327,11 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 //                    order is a permutation of the keys within 16, which the V
 //                    reads follow;
 //   O^T += V^T P^T   A: V read transposed from LDS (ds_read_b64_tr_b16).
-// The running maximum moves only when a tile exceeds it by 2^kLazy, so that the
-// output is rescaled rarely.
+// The reference of the weights moves only when a tile exceeds it by 2^kLazy, so that the
+// output is rescaled rarely.  It is a whole number: its sum with kBias is exact, and one
+// fused product and sum gives an exponent (two roundings more would be another instruction
+// for each of a tile's weights).  Beyond kFar, where a logit's rounding is no longer small
+// against the headroom above the reference, the logits are rounded before it is taken off.
 //
 // A step of a wave has two halves: its products (the logits of tile t + 1, the
 // values of tile t) and its vector work (the weights of tile t + 1, and DMA).  The
@@ -348,6 +351,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // tokens 206 us, 0.73 PFLOP/s.
 
 constexpr float kLazy = 8.0f;
+constexpr float kFar = 65536.0f;  // an exponent is off by 2^-8 at most, 1.0027 of a weight
 constexpr int kExtWaves = 8;
 static_assert(kExtRows == kExtWaves * 32);
 constexpr int kRing = 4;
@@ -574,9 +578,9 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       }
       float other = mt;
       swap32(mt, other);
-      const float top = fmaxf(mt, other) * a.scale2;
-      if (__ballot(top > m_ref + kLazy + E::kBias)) {
-        const float m_new = fmaxf(m_ref, top - E::kBias);
+      const float top = base2(fmaxf(mt, other), a.scale2);
+      if (__ballot(top - m_ref > kLazy)) {
+        const float m_new = fmaxf(m_ref, ceilf(top));
         const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
         m_ref = m_new;
         l_run *= alpha;
@@ -585,11 +589,18 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
       }
+      float scale2 = a.scale2, shift = E::kBias - m_ref;
+      if (__ballot(fabsf(m_ref) > kFar && m_ref > -FLT_MAX)) {
+#pragma unroll
+        for (int n = 0; n < 32; ++n) s[n >> 4][n & 15] = base2(s[n >> 4][n & 15], a.scale2) - m_ref;
+        scale2 = 1.0f;
+        shift = E::kBias;
+      }
       float sum[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int n = 0; n < 16; ++n) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][2 * n & 15], a.scale2, -m_ref));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][(2 * n & 15) + 1], a.scale2, -m_ref));
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][2 * n & 15], scale2, shift));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n >> 3][(2 * n & 15) + 1], scale2, shift));
         sum[0] += p0;
         sum[1] += p1;
         w[n >> 2][n & 3] = elem_pack<T>(p0, p1);

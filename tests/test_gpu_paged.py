@@ -251,6 +251,45 @@ def test_rising_and_extreme_logits(torch_cuda, new, dtype):
 
 @pytest.mark.parametrize("new", [1, 3, 140])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_logits_of_any_size(torch_cuda, new, dtype):
+    """Logits up to 2^107.  Equal ones give the mean of the values that are seen; others
+    differ by more than 2^14, so that one key has all the weight.  Either way no logit's
+    rounding matters, and the tolerance has no part for it."""
+    import torch
+    f = Served((300, 200, 171), (new,) * 3, 16, dtype, 1, 4, 1, seed=22)
+    u, where = _half_step(dtype), [(s, j, OP.place(f.table, s, j, 16, f.n_pages)) for s in range(3) for j in range(f.lens[s])]
+    rows = f.k.view(1, 1, -1, D)
+
+    def check(q, scale, what):
+        out = f.attend(q, scale=scale)
+        ref, weight, keys, _ = OP.attention(_f64(q[0]), _f64(f.k[0]), _f64(f.v[0]), f.table, f.lens, f.cu, f.max_len, scale, 4)
+        lim = u * np.abs(ref) + ((0 if new == 1 else u) + 2.0 ** -22 + 2 * keys * 2.0 ** -24)[..., None] * weight + 2.0 ** -25
+        err = np.abs(_f64(out[0]) - ref)
+        assert (err <= lim).all(), (what, scale, np.argwhere(~(err <= lim))[:3].tolist(), _f64(out[0])[~(err <= lim)][:3])
+
+    q = torch.empty((1, f.total, 4, D), dtype=f.dt, device="cuda")
+    sizes = [(7000.0, 7000.0, D ** -0.5), (60000.0, 60000.0, D ** -0.5), (60000.0, -60000.0, D ** -0.5), (1.0, 1.0, 2.0 ** 15),
+             (1.0, -1.0, 2.0 ** 17), (3.0, 5.0, 2.0 ** 20), (1.0, 1.0, 2.0 ** 24), (1.0, -1.0, 2.0 ** 30), (1.0, 1.0, 2.0 ** 100)]
+    for a, b, scale in sizes + ([(1e10, 1e10, D ** -0.5)] if dtype == "bf16" else []):
+        q.fill_(a)
+        rows.fill_(b)
+        check(q, scale, ("equal", a, b))
+        rows.fill_(b / 2 if b > 0 else b)
+        for s in range(3):  # one that stands out, in the first tile, behind it, and among the new tokens
+            rows[0, 0, OP.place(f.table, s, (3, 100, f.lens[s] - 1)[s], 16, f.n_pages)] = b if b > 0 else b / 2
+        check(q, scale, ("one", a, b))
+    q.zero_()
+    q[..., :2] = 1
+    rows.zero_()
+    for slope in (1, -1):  # every key above the one before it, or below
+        for s, j, r in where:
+            rows[0, 0, r, 0], rows[0, 0, r, 1] = slope * (j % 128), slope * (j - j % 128)
+        for scale in (2.0 ** 14, 2.0 ** 15, 2.0 ** 18, 2.0 ** 24, 2.0 ** 60, 2.0 ** 99):
+            check(q, scale, ("slope", slope))
+
+
+@pytest.mark.parametrize("new", [1, 3, 140])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_masked_values_have_no_influence(torch_cuda, new, dtype):
     """Keys and values of later tokens that are infinite or NaN reach the tokens that
     see them, and no other."""
