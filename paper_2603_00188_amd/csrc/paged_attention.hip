@@ -734,9 +734,10 @@ struct Joined {
   float m = -INFINITY, l = 0.0f;
   f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
+  // (A part without a key has maximum -inf and weighs nothing.  So has one whose logits are
+  // all NaN, but its sums are NaN, and make what they are added to NaN with any factor.)
   __device__ void add(float pm, float pl, f32x4_t po) {
-    if (pm == -INFINITY) return;
-    const float mx = fmaxf(m, pm);
+    const float mx = fmaxf(fmaxf(m, pm), -FLT_MAX);
     const float f = __builtin_amdgcn_exp2f(m - mx), g = __builtin_amdgcn_exp2f(pm - mx);
     l = l * f + pl * g;
 #pragma unroll
@@ -815,7 +816,8 @@ __global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a
         for (int i = 0; i < kBatch; ++i)  // (past the last: that one again, left out)
           load(min(w + i * per_row, w1), row, m[i], l[i], o[i]);
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) r.add(w + i * per_row <= w1 ? m[i] : -INFINITY, l[i], o[i]);
+        for (int i = 0; i < kBatch; ++i)
+          if (w + i * per_row <= w1) r.add(m[i], l[i], o[i]);
       }
     if (per_row > 1) {
       __syncthreads();

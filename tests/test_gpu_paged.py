@@ -316,6 +316,32 @@ def test_masked_values_have_no_influence(torch_cuda, new, dtype):
     assert torch.isnan(out[0, first[1]:f.cu[2], 3:6, 7]).all() and torch.isnan(out[0, first[2]:f.cu[3], 3:6, :]).all()
 
 
+@pytest.mark.parametrize("lens,new,page,dtype,layers,hq,hk", [
+    ((20000,), (1,), 32, "bf16", 1, 4, 2), ((9000, 40, 0, 6000), (1, 0, 1, 1), 16, "bf16", 1, 7, 1),
+    ((5000, 300, 7000), (1, 1, 1), 64, "fp16", 1, 40, 1), ((900,) * 40, (1,) * 40, 16, "fp16", 2, 16, 2),
+    ((6000, 300), (3, 3), 32, "bf16", 1, 28, 4), ((3000,), (60,), 16, "fp16", 1, 128, 1), ((700,) * 9, (150,) * 9, 16, "bf16", 2, 8, 2)])
+def test_logits_that_are_nan(torch_cuda, lens, new, page, dtype, layers, hq, hk):
+    """A query or keys that are NaN make their own outputs NaN, however many parts a sequence is cut into, even where no
+    part has another logit; a token that sees nothing still gets 0."""
+    import torch
+    f = Served(lens, new, page, dtype, layers, hq, hk, seed=23)
+    q = f.randn((layers, f.total, hq, D))
+    clean = f.attend(q).clone()
+    want = torch.isnan(clean)
+    assert not want.any()
+    for s in range(0, len(lens), 2):
+        if new[s]:
+            q[:, f.cu[s], hq - 1, 5] = float("nan")
+            want[:, f.cu[s], hq - 1] = lens[s] > 0
+    out = f.attend(q)
+    assert torch.equal(torch.isnan(out), want) and torch.equal(out[~want], clean[~want])
+    for j in range(lens[0] - new[0] + 1):  # every key that the first sequence's first token sees, of one kv head
+        f.k.view(layers, hk, -1, D)[0, hk - 1, OP.place(f.table, 0, j, page, f.n_pages), 7] = float("nan")
+    want[0, :f.cu[1], hq - hq // hk:] = True
+    out = f.attend(q)
+    assert torch.equal(torch.isnan(out), want) and torch.equal(out[~want], clean[~want])
+
+
 @pytest.mark.parametrize("new,hq", [(1, 3), (1, 20), (1, 40), (4, 20), (70, 3)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_values_that_are_seen_and_not_finite(torch_cuda, new, hq, dtype):
