@@ -87,6 +87,13 @@ hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t st
 // Device helpers
 // ---------------------------------------------------------------------------
 
+template <typename T>
+__device__ inline uint32_t elem_pack(float lo, float hi) {  // each rounded to nearest
+  typedef T pair_t __attribute__((ext_vector_type(2)));
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, pair_t));
+}
+
 // 16-bit element types: bf16 or IEEE half.
 template <typename T>
 struct Elem;
@@ -107,10 +114,10 @@ struct Elem<__bf16> {
   static __device__ f32x4_t mfma16(u32x2_t a, u32x2_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, b), c, 0, 0, 0);
   }
-  // x as a sum of terms of this type: 3 x 8 bits are all of it.
+  // x as a sum of terms of this type: 3 x 8 bits are all of it.  A term is taken off.
   static constexpr int kTerms = 3;
   static constexpr float kTermsBias = -20.0f;  // (as kBias)
-  static __device__ uint32_t take(float& x0, float& x1) {
+  static __device__ uint32_t take(float& x0, float& x1, bool) {
     const uint32_t b0 = __builtin_bit_cast(uint32_t, x0) & 0xffff0000u, b1 = __builtin_bit_cast(uint32_t, x1) & 0xffff0000u;
     x0 -= __builtin_bit_cast(float, b0);
     x1 -= __builtin_bit_cast(float, b1);
@@ -130,11 +137,13 @@ struct Elem<_Float16> {
   static __device__ f32x4_t mfma16(u32x2_t a, u32x2_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, a), __builtin_bit_cast(f16x4_t, b), c, 0, 0, 0);
   }
-  // Two terms of 11 bits, of weights of at most 2^15: what is left out is at most
-  // 2^-40 of the greatest weight, or 2^-22 of the weight itself.
+  // Two terms of 11 bits, of weights of at most 2^15, the second rounded to nearest (cut
+  // off, the sums of the weights in the numerator would all lie below the denominator's):
+  // they are off by at most 2^-22 of the weight itself, or 2^-40 of the greatest.
   static constexpr int kTerms = 2;
   static constexpr float kTermsBias = 15.0f;
-  static __device__ uint32_t take(float& x0, float& x1) {
+  static __device__ uint32_t take(float& x0, float& x1, bool last) {
+    if (last) return elem_pack<_Float16>(x0, x1);
     const auto h = __builtin_amdgcn_cvt_pkrtz(x0, x1);
     x0 -= float(h[0]);
     x1 -= float(h[1]);
@@ -149,12 +158,6 @@ __device__ inline float elem_lo(uint32_t w) {
 template <typename T>
 __device__ inline float elem_hi(uint32_t w) {
   return float(__builtin_bit_cast(T, uint16_t(w >> 16)));
-}
-template <typename T>
-__device__ inline uint32_t elem_pack(float lo, float hi) {  // each rounded to nearest
-  typedef T pair_t __attribute__((ext_vector_type(2)));
-  typedef float f32x2_t __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, pair_t));
 }
 
 // A logit in base 2, rounded: what a maximum is taken of and what it is taken from have

@@ -215,8 +215,8 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
           l_run[ng] += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
           for (int n = 0; n < E::kTerms; ++n) {
-            terms[ng][n][0] = E::take(p[0], p[1]);
-            terms[ng][n][1] = E::take(p[2], p[3]);
+            terms[ng][n][0] = E::take(p[0], p[1], n == E::kTerms - 1);
+            terms[ng][n][1] = E::take(p[2], p[3], n == E::kTerms - 1);
           }
         }
 #pragma unroll

@@ -183,6 +183,36 @@ def test_decode_many_short_sequences(torch_cuda):
     f.compare(q, f.attend(q))
 
 
+def test_half_weights_are_rounded_to_nearest(torch_cuda):
+    """One token in fp16: a weight is two half terms, off by at most 2^-22 of itself and to
+    either side alike.  A key of weight p meets 2^14, keys of weight 1 meet what cancels all
+    but the last bits of it: the sums are exact, so that the output shows the terms' error.
+    In units of an fp32 step of the weight, terms that are cut off at 13 bits of which the
+    second holds the first 11 from its leading one lose 0.875 on average (half of all: 1.5 of
+    two bits, a quarter: 0.5 of one), terms that are rounded nothing; half of that is told
+    apart here.  The exponential's error is within one such step for each weight."""
+    import torch
+    n, big = 4096, 2.0 ** 14
+    f = Served((3,) * n, (1,) * n, 16, "fp16", 1, 1, 1, seed=24)
+    scale = np.float32(np.log(2.0))
+    x = (-np.linspace(0.01, 0.99, n)).astype(np.float16)
+    p = np.exp2((x.astype(np.float32) * np.float32(scale * np.float32(1.4426950408889634))).astype(np.float64))
+    c1 = (p * big).astype(np.float16)
+    c2 = (p * big - c1.astype(np.float64)).astype(np.float16)
+    at = np.array([[OP.place(f.table, s, j, 16, f.n_pages) for j in range(3)] for s in range(n)])
+    k, v = np.zeros((f.n_pages * 16, D), np.float16), np.zeros((f.n_pages * 16, D), np.float16)
+    k[at[:, 2], 0] = x
+    v[at[:, 0]], v[at[:, 1]], v[at[:, 2]] = -c1[:, None], -c2[:, None], big
+    f.k.copy_(torch.from_numpy(k).view(f.k.shape))
+    f.v.copy_(torch.from_numpy(v).view(f.v.shape))
+    q = torch.zeros((1, n, 1, D), dtype=f.dt, device="cuda")
+    q[..., 0] = 1
+    got = _f64(f.attend(q, scale=float(scale)))[0, :, 0, 0] * (2 + p)
+    err = (got - (p * big - c1.astype(np.float64) - c2.astype(np.float64))) / (big * 2.0 ** -24)
+    _log(f"half terms: mean error {err.mean():.3f} fp32 steps, worst {np.abs(err).max():.2f}")
+    assert abs(err.mean()) < 0.875 / 2 and np.abs(err).max() <= 2 + 1 + 0.5
+
+
 # ---------------------------------------------------------------------------
 # Attention of several new tokens
 # ---------------------------------------------------------------------------
