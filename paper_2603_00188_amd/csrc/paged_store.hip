@@ -79,6 +79,8 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) 
 // New tokens
 // ---------------------------------------------------------------------------
 
+constexpr int64_t kMaxBlocks = int64_t(1) << 23;  // along x
+
 // One (token, layer) by `WAVES` waves.  Eight lanes hold a head: lane c the
 // dimensions 8c .. 8c+7 and 64+8c .. 64+8c+7, so both members of every pair of
 // either pairing lie in one lane.  The 64 (cos, sin) of the token are formed
@@ -96,7 +98,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tl = wave / WAVES, part = wave % WAVES;
   const int layer = blockIdx.y;
-  const int64_t tok = int64_t(blockIdx.x) * kTok + tl;
+  const int64_t tok = (int64_t(blockIdx.z) * gridDim.x + blockIdx.x) * kTok + tl;
   const bool live = tok < c.total_new;
   const int cidx = lane & 7, sub = lane >> 3;
   const int nq = a.q.data ? c.n_q_heads : 0, nk = c.n_kv_heads;
@@ -247,7 +249,10 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t 
   // 448 pairs 6.0 / 4.7, 1024 pairs 6.9 / 5.9, 1792 pairs 9.2 / 10.1, 4096 pairs 14.3 /
   // 16.3, 87808 pairs 303 / 317.
   const bool few = a.c.total_new * a.c.n_layers <= 1024;
-  const dim3 grid(uint32_t((a.c.total_new + (few ? 0 : 3)) / (few ? 1 : 4)), a.c.n_layers);
+  // A grid has less than 2^32 threads along x, which 2^26 tokens reach: the rest of them
+  // along z.
+  const int64_t blocks = (a.c.total_new + (few ? 0 : 3)) / (few ? 1 : 4), x = blocks < kMaxBlocks ? blocks : kMaxBlocks;
+  const dim3 grid(uint32_t(x), a.c.n_layers, uint32_t((blocks + x - 1) / x));
   if (half) {
     if (few) hipLaunchKernelGGL((paged_append_kernel<_Float16, 4>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((paged_append_kernel<_Float16, 1>), grid, dim3(256), 0, stream, a);

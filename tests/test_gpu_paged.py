@@ -580,6 +580,30 @@ def test_append_finds_its_sequence(torch_cuda, n_seqs):
         assert np.array_equal(_bits(got).reshape(-1, D), pool)
 
 
+@pytest.mark.parametrize("more", [-1, 0, 5])
+def test_append_of_2_to_26_tokens(torch_cuda, more):
+    """More threads than a grid has along one axis.  The last tokens have pages, the others none."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    page, n, kept = 256, (1 << 26) + more, 1000
+    table = torch.full((1, -(-n // page)), -1, dtype=torch.int32, device="cuda")
+    first = (n - kept) // page
+    pages = table.shape[1] - first
+    table[0, first:] = torch.randperm(pages, device="cuda").to(torch.int32)
+    pool = [torch.zeros((1, 1, pages, page, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    cache = P.PagedCache(*pool, table, torch.tensor([n], dtype=torch.int32, device="cuda"), 1)
+    batch = P.NewTokens([0, n])
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(26)
+    k = torch.zeros((1, n, 1, D), dtype=torch.bfloat16, device="cuda")  # (values too)
+    last = torch.randn((n - first * page, D), generator=gen, device="cuda").to(torch.bfloat16)
+    k[0, first * page:, 0] = last
+    P.paged_append(cache, batch, None, k, k)
+    for x in pool:
+        got = x[0, 0][table[0, first:].long()].view(-1, D)
+        assert torch.equal(got[:len(last)], last) and not got[len(last):].any()
+
+
 def test_append_drops_rows_without_a_page(torch_cuda):
     import torch
     f = Served((40, 70), (40, 5), 16, "bf16", 1, 4, 2, seed=13)
