@@ -81,6 +81,12 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) 
 
 constexpr int64_t kMaxBlocks = int64_t(1) << 23;  // along x
 
+// Sums of squares that fp32 holds to its full precision.  A row outside (bf16 values above
+// 2^60 or all below 2^-50) is scaled by a power of two, and eps by its square, before its
+// norm; a small one only where eps does not hide it, so that the scaled eps stays finite.
+// (3136 normed tokens of 28 layers take 298 us; without it 295.5, in 64 bits 310.)
+constexpr float kLeastSum = 0x1p-100f, kMostSum = 0x1p120f, kLeastEps = 0x1p-80f;
+
 // One (token, layer) by `WAVES` waves.  Eight lanes hold a head: lane c the
 // dimensions 8c .. 8c+7 and 64+8c .. 64+8c+7, so both members of every pair of
 // either pairing lie in one lane.  The 64 (cos, sin) of the token are formed
@@ -183,8 +189,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
         x[8 + 2 * j] = elem_lo<T>(hi[j]);
         x[9 + 2 * j] = elem_hi<T>(hi[j]);
       }
-      // (the lanes of a head take the same side of this branch, so the sum below
-      // has all eight)
+      // (the lanes of a head take the same side of these branches, so the sums below
+      // have all eight)
       if (w) {
         float ss = 0.0f;
 #pragma unroll
@@ -192,7 +198,21 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
         ss += lane_xor<1>(ss);
         ss += lane_xor<2>(ss);
         ss += lane_xor<4>(ss);
-        const float rs = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps);
+        float eps = a.eps;
+        if (!(ss <= kMostSum) || (ss < kLeastSum && eps < kLeastEps)) {
+          const float up = ss < 1.0f ? 0x1p100f : 0x1p-70f;
+          eps = eps * up * up;
+          ss = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            x[j] *= up;
+            ss = fmaf(x[j], x[j], ss);
+          }
+          ss += lane_xor<1>(ss);
+          ss += lane_xor<2>(ss);
+          ss += lane_xor<4>(ss);
+        }
+        const float rs = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + eps);
         const uint16_t* wl = w + layer * kHeadDim + 8 * cidx;
         const u32x4_t w0 = *reinterpret_cast<const u32x4_t*>(wl), w1 = *reinterpret_cast<const u32x4_t*>(wl + 64);
 #pragma unroll

@@ -645,6 +645,33 @@ def test_append_special_values(torch_cuda):
     assert np.array_equal(_bits(f.v).reshape(-1, D)[row], _bits(v)[0, 5, 0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+@pytest.mark.parametrize("many", [False, True])
+def test_norms_of_rows_of_any_size(torch_cuda, dtype, eps, many):
+    """Rows whose squares pass fp32's range, or fall out of it: at the limits of the type, alone and beside others."""
+    import torch
+    n = 2000 if many else 40  # both forms of the kernel
+    f = Served((n,), (n,), 16, dtype, 1, 3, 1, seed=25)
+    q, k, v = (f.randn((1, n, h, D)) for h in (3, 1, 1))
+    info = torch.finfo(f.dt)
+    sizes = [1e10, 2e18, 1e19, 3e25, 1e37, info.max / 8, 1e-15, 1e-20, 1e-25, 1e-35] if dtype == "bf16" else [info.max / 8, info.tiny, 1.0]
+    for i, size in enumerate(sizes * 3):
+        q[0, i, i % 3] = (q[0, i, i % 3].float() * size).clamp(-info.max, info.max).to(f.dt)
+        k[0, i, 0] = (k[0, i, 0].float() * size).clamp(-info.max, info.max).to(f.dt)
+    q[0, 35], k[0, 35] = info.max, -info.max
+    q[0, 36] = 0
+    q[0, 36, :, 9] = info.max  # one element of a row
+    k[0, 36] = info.smallest_normal
+    w = f.randn((1, D)) + 1
+    out = f.P.paged_append(f.cache, f.batch, q, k, v, q_norm=w, k_norm=w, eps=eps)
+    u = _half_step(dtype)
+    places = OP.new_places(f.table, f.lens, f.cu, 16, f.n_pages, f.max_len)
+    for x, y in ((_f64(q)[0], _f64(out)[0]), (_f64(k)[0], _f64(f.k).reshape(1, -1, D)[0][np.array(places)][:, None])):
+        ref = OP.norm(x, _f64(w)[0], float(np.float32(eps)))
+        assert (np.abs(y - ref) <= (u + 2.0 ** -18) * np.abs(ref) + 2.0 ** -25).all()
+
+
 # ---------------------------------------------------------------------------
 # Compaction into pages
 # ---------------------------------------------------------------------------
