@@ -731,13 +731,13 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 constexpr int kBatch = 4;
 
 struct Joined {
-  float m = -INFINITY, l = 0.0f;
+  float m = -FLT_MAX, l = 0.0f;
   f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   // (A part without a key has maximum -inf and weighs nothing.  So has one whose logits are
   // all NaN, but its sums are NaN, and make what they are added to NaN with any factor.)
   __device__ void add(float pm, float pl, f32x4_t po) {
-    const float mx = fmaxf(fmaxf(m, pm), -FLT_MAX);
+    const float mx = fmaxf(m, pm);
     const float f = __builtin_amdgcn_exp2f(m - mx), g = __builtin_amdgcn_exp2f(pm - mx);
     l = l * f + pl * g;
 #pragma unroll
@@ -816,8 +816,10 @@ __global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a
         for (int i = 0; i < kBatch; ++i)  // (past the last: that one again, left out)
           load(min(w + i * per_row, w1), row, m[i], l[i], o[i]);
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-          if (w + i * per_row <= w1) r.add(m[i], l[i], o[i]);
+        for (int i = 0; i < kBatch; ++i) {
+          const bool there = w + i * per_row <= w1;
+          r.add(there ? m[i] : -FLT_MAX, there ? l[i] : 0.0f, there ? o[i] : f32x4_t{0.f, 0.f, 0.f, 0.f});
+        }
       }
     if (per_row > 1) {
       __syncthreads();
@@ -832,7 +834,7 @@ __global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a
         for (int g = 0; g < per_row; ++g) r.m = fmaxf(r.m, sm_m[grp + g]);
 #pragma unroll 4
         for (int g = 0; g < per_row; ++g) {
-          const float f = sm_m[grp + g] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[grp + g] - r.m);
+          const float f = __builtin_amdgcn_exp2f(sm_m[grp + g] - r.m);
           r.l += sm_l[grp + g] * f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) r.o[i] += sm_o[grp + g][l32][i] * f;
