@@ -12,7 +12,9 @@ arithmetic runs in the library's gfx950 kernels.  Tensors are bf16 or fp16, of
 the pool's type and on its device.  Everything runs on ``stream`` (the device's
 current one by default), allocates nothing where ``q_out``, ``out`` and
 ``workspace`` are given, and follows ``seq_lens`` and ``page_table`` on the
-device, so that a step can be captured into a graph and replayed.
+device, so that a step can be captured into a graph and replayed.  With a
+``torch.cuda.Stream`` the call's tensors, the batch's among them, may be dropped
+at once; with the handle of a stream the caller keeps them until the work has run.
 """
 from __future__ import annotations
 
@@ -41,12 +43,16 @@ class _On:
     def __init__(self, device, stream):
         if device.type != "cuda":
             raise ValueError(f"the cache is on {device}: the kernels run on a GPU")
+        if stream is None:
+            self.stream = torch.cuda.current_stream(device)
+            self.handle, self.own = self.stream.cuda_stream, True
+        else:
+            self.stream = stream
+            self.handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+            self.own = self.handle == torch.cuda.current_stream(device).cuda_stream
         self.device, self.before = device, torch.cuda.current_device()
         if self.before != device.index:
             torch.cuda.set_device(device.index)
-        self.stream = torch.cuda.current_stream(device) if stream is None else stream
-        self.handle = self.stream.cuda_stream if hasattr(self.stream, "cuda_stream") else int(self.stream)
-        self.own = stream is None
 
     def new(self, shape, dtype):
         """A tensor for this call's stream."""
@@ -56,6 +62,14 @@ class _On:
             s.wait_stream(torch.cuda.current_stream(self.device))  # what used this memory before
             t.record_stream(s)
         return t
+
+    def keep(self, *tensors):
+        """The call's tensors: their memory is not given away before the stream has used it, should the caller drop them.
+        (Not for a stream that the caller made, which may be gone when they are freed.)"""
+        if type(self.stream) is torch.cuda.Stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
 
     def __enter__(self):
         return self
@@ -121,7 +135,7 @@ class PagedCache(_Fixed):
         _is(v, "v", k.shape, k.dtype, k.device)
         _is(page_table, "page_table", page_table.shape, torch.int32, k.device)
         _is(seq_lens, "seq_lens", page_table.shape[:1], torch.int32, k.device)
-        self.k, self.v, self.page_table, self.seq_lens = k, v, page_table, seq_lens
+        self.k, self.v, self.page_table, self.seq_lens = self.tensors = k, v, page_table, seq_lens
         self.n_layers, self.n_kv_heads, self.n_pages, self.page_size = k.shape[:4]
         self.n_seqs, self.max_pages = page_table.shape
         self.n_q_heads, self.dtype, self.device = int(n_q_heads), k.dtype, k.device
@@ -226,6 +240,8 @@ def paged_compact(cache: PagedCache, p, k, v, kept, per_layer: bool = False, str
             or (p.total_budget and kept.numel() != lists * p.total_budget)):
         raise ValueError(f"kept must be a contiguous int32 tensor of {lists} x {p.total_budget} on {cache.device}")
     with _On(cache.device, stream) as on:
+        if not on.own:
+            on.keep(k, v, kept, p.d["cu_budget"], *cache.tensors)
         _check(load().stlite_paged_compact(p.ref, ctypes.byref(cache._struct(None)), k.data_ptr(), v.data_ptr(),
                                            kept.data_ptr(), int(bool(per_layer)), on.handle), "stlite_paged_compact")
 
@@ -256,6 +272,8 @@ def paged_append(cache: PagedCache, batch: NewTokens, q, k, v, positions=None, r
                 q_out = on.new(shape, cache.dtype)
             else:
                 _is(q_out, "q_out", shape, cache.dtype, cache.device)
+        if not on.own:
+            on.keep(q, k, v, positions, q_norm, k_norm, q_out, batch.d, *cache.tensors)
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         _check(load().stlite_paged_append(ctypes.byref(cache._struct(batch)), None if rope is None else ctypes.byref(rope.c),
                                           ptr(positions), rq, ctypes.byref(rows[0]), ctypes.byref(rows[1]), ptr(q_norm),
@@ -278,6 +296,8 @@ def paged_attention(cache: PagedCache, batch: NewTokens, q, out=None, workspace=
             out = on.new(shape, cache.dtype)
         if workspace is None:
             workspace = on.new(max(cache.workspace_size(batch), 256), torch.uint8)
+        if not on.own:
+            on.keep(q, out, workspace, batch.d, *cache.tensors)
         _check(load().stlite_paged_attention(ctypes.byref(cache._struct(batch)), q.data_ptr(),
                                              1.0 / math.sqrt(HEAD_DIM) if scale is None else float(scale), out.data_ptr(),
                                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), on.handle),

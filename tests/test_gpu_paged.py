@@ -881,6 +881,34 @@ def test_streams(torch_cuda):
         assert torch.equal(got, want) and torch.equal(got_q, want_q) and len(junk) == 8
 
 
+@pytest.mark.parametrize("new", [1, 3])
+def test_dropped_tensors_on_another_stream(torch_cuda, new):
+    """A call on a busy stream whose batch and inputs are dropped at once: their memory is not given to others before the
+    kernels have run.  (What would take their place is another batch of as many tokens: in bounds either way.)"""
+    import torch
+    f = Served((3000, 40, 700), (new,) * 3, 32, "bf16", 2, 8, 2, seed=27)
+    n = 3 * new
+    other = [0, n - 1, n - 1, n] if new == 3 else [0, 0, 2, 3]
+    rows = [f.randn((2, n, h, D)) for h in (8, 2, 2)]
+    want_q = f.P.paged_append(f.cache, f.batch, *rows)
+    want = f.P.paged_attention(f.cache, f.batch, want_q)
+    pools = f.k.clone(), f.v.clone()
+    f.k.zero_()
+    f.k.copy_(pools[0])
+    busy = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            torch.mm(busy, busy)
+    got_q = f.P.paged_append(f.cache, f.P.NewTokens(f.cu), *(x.clone() for x in rows), stream=side)
+    got = f.P.paged_attention(f.cache, f.P.NewTokens(f.cu), got_q, stream=side)
+    others = [f.P.NewTokens(other) for _ in range(8)] + [torch.full_like(x, 9.0) for x in rows for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got_q, want_q) and torch.equal(got, want) and len(others) == 20
+    assert torch.equal(f.k, pools[0]) and torch.equal(f.v, pools[1])
+
+
 def test_dense_decode_agrees(torch_cuda):
     """The dense decode call and the paged one over identity pages, on the same cache."""
     import torch

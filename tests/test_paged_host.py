@@ -567,3 +567,4 @@ def test_copied_caches():
     r = P.Rope(1e4, (16, 24, 24), True)
     for q in (copy.copy(r), copy.deepcopy(r)):
         assert (q.n_axes, q.c.theta, q.c.interleaved, list(q.c.sections)) == (3, 1e4, 1, [16, 24, 24])
+
