@@ -47,6 +47,9 @@ class _On:
             self.stream = torch.cuda.current_stream(device)
             self.handle, self.own = self.stream.cuda_stream, True
         else:
+            at = getattr(stream, "device", device)  # (a handle does not know)
+            if at != device:
+                raise ValueError(f"the stream is on {at}, the cache on {device}")
             self.stream = stream
             self.handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
             self.own = self.handle == torch.cuda.current_stream(device).cuda_stream

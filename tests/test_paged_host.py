@@ -568,3 +568,31 @@ def test_copied_caches():
     for q in (copy.copy(r), copy.deepcopy(r)):
         assert (q.n_axes, q.c.theta, q.c.interleaved, list(q.c.sections)) == (3, 1e4, 1, [16, 24, 24])
 
+
+class FakeStream:
+    """A stream as _On sees it."""
+
+    def __init__(self, device, handle=7):
+        self.device, self.cuda_stream = torch.device(device), handle
+
+
+def test_streams_and_devices_of_a_call(monkeypatch):
+    """A stream of another device is refused, and what is refused leaves the current device as it was."""
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "set_device", lambda i: current.__setitem__(0, i))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: FakeStream(device, 3))
+    device = torch.device("cuda:1")
+    for bad in (FakeStream("cuda:0"), FakeStream("cuda:2"), "seven", object()):
+        with pytest.raises((ValueError, TypeError)):
+            P._On(device, bad)
+        assert current == [0]
+    for good, handle, own in ((None, 3, True), (3, 3, True), (FakeStream("cuda:1", 3), 3, True), (FakeStream("cuda:1"), 7, False),
+                              (9, 9, False), (0, 0, False)):
+        with P._On(device, good) as on:
+            assert current == [1] and (on.handle, on.own) == (handle, own)
+        assert current == [0]
+    with pytest.raises(RuntimeError):
+        with P._On(device, None):
+            raise RuntimeError
+    assert current == [0]
