@@ -129,7 +129,7 @@ stlite_status stlite_paged_workspace_size(const stlite_paged* c, size_t* bytes);
  * n_layers, n_kv_heads and n_seqs, and every B_s must be at most c->max_len; the
  * new tokens (total_new, cu_new, h_cu_new) are not read.  per_layer != 0: one
  * kept list per layer, as in stlite_compact_kv_layer.  A kept index outside
- * [0, total_tokens) stores zeros.
+ * [0, total_tokens) stores zeros.  k and v must not alias the pool.
  */
 stlite_status stlite_paged_compact(const stlite_problem* p, const stlite_paged* c, const uint16_t* k,
                                    const uint16_t* v, const int32_t* kept, int32_t per_layer,
@@ -146,7 +146,8 @@ stlite_status stlite_paged_compact(const stlite_problem* p, const stlite_paged* 
  *   positions  int32 [n_axes][total_new]; rope and positions both NULL: no rotation
  *   q_norm, k_norm  [n_layers][d], each nullable, 16-byte aligned
  *   eps        finite, >= 0; read where a norm is
- * q->data and q_out both NULL: no queries.  q_out must not alias q, k or v.
+ * q->data and q_out both NULL: no queries.  q_out must not alias q, k, v or the pool;
+ * k and v must not lie where the call stores other rows.
  */
 stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope, const int32_t* positions,
                                   const stlite_rows* q, const stlite_rows* k, const stlite_rows* v,
@@ -160,7 +161,7 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  * over the tokens j that lie in valid pages; a token that sees none gets 0.
  * What the mask leaves out has no influence, NaN and infinities among it.
  *   q    [n_layers][total_new][n_q_heads][d], 16-byte aligned
- *   out  the same layout and type; 16-byte aligned, must not alias q
+ *   out  the same layout and type; 16-byte aligned, must not alias q or the pool
  *   scale  > 0, at most 2^127
  * fp32 logits, softmax statistics and sums, which stay finite for values of any
  * size and up to 2^20 keys, and for logits of any size in fp32's range (scale q . k
@@ -169,7 +170,7 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  * the type of the call before they meet v.  An infinity or NaN of a token that is
  * seen reaches the output whatever its weight (an infinity of a weight that is
  * rounded to 0 as NaN).  Rows of out belong to new tokens only: nothing behind
- * total_new is written.
+ * total_new is written.  The workspace must not alias q, out or the pool.
  */
 stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, float scale, uint16_t* out,
                                      void* workspace, size_t workspace_bytes, void* stream);

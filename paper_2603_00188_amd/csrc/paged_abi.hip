@@ -199,6 +199,32 @@ stlite_status check_rows(const stlite_rows* r, int64_t heads, const char* name) 
   return STLITE_OK;
 }
 
+bool meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+size_t pool_bytes(const stlite_paged* c) {
+  return size_t(c->n_layers) * c->n_kv_heads * c->n_pages * c->page_size * kHeadDim * sizeof(uint16_t);
+}
+size_t query_bytes(const stlite_paged* c) {
+  return size_t(c->n_layers) * c->total_new * c->n_q_heads * kHeadDim * sizeof(uint16_t);
+}
+bool meets_pool(const stlite_paged* c, const void* p, size_t bytes) {
+  return meet(p, bytes, c->k, pool_bytes(c)) || meet(p, bytes, c->v, pool_bytes(c));
+}
+
+// Whether rows of `heads` heads share an element with the `bytes` bytes at p; what lies
+// between two tokens' rows or two layers' is another's.
+bool rows_meet(const stlite_paged* c, const stlite_rows* r, int64_t heads, const void* p, size_t bytes) {
+  const int64_t own = heads * kHeadDim * int64_t(sizeof(uint16_t)), step = r->token_stride * int64_t(sizeof(uint16_t));
+  for (int64_t l = 0; l < c->n_layers; ++l) {
+    const int64_t from = int64_t(reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(r->data + l * r->layer_stride));
+    const int64_t t = from < own ? 0 : (from - own) / step + 1;  // the first token that ends behind p
+    if (t < c->total_new && t * step < from + int64_t(bytes)) return true;
+  }
+  return false;
+}
+
 RowsIn rows_in(const stlite_rows* r) {
   return r ? RowsIn{r->data, r->token_stride, r->layer_stride} : RowsIn{nullptr, 0, 0};
 }
@@ -271,6 +297,9 @@ stlite_status stlite_paged_compact(const stlite_problem* p, const stlite_paged* 
   if (!c->seq_lens) return fail(STLITE_ERR_INVALID_ARG, "seq_lens must be non-NULL");
   if (p->total_budget > 0 && (!k || !v || !kept)) return fail(STLITE_ERR_INVALID_ARG, "k, v and kept must be non-NULL");
   if (!aligned16(k) || !aligned16(v)) return fail(STLITE_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+  const size_t rows_bytes = size_t(p->n_layers) * p->n_kv_heads * p->total_tokens * kHeadDim * sizeof(uint16_t);
+  if (p->total_budget > 0 && (meets_pool(c, k, rows_bytes) || meets_pool(c, v, rows_bytes)))
+    return fail(STLITE_ERR_INVALID_ARG, "k and v must not alias the pool: rows are not moved in place");
   PagedCompactArgs a;
   a.c = device_view(c);
   a.cu_budget = p->cu_budget;
@@ -323,12 +352,16 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
   if (st == STLITE_OK && queries) st = check_rows(q, c->n_q_heads, "q");
   if (st != STLITE_OK) return st;
   if (queries != (q_out != nullptr)) return fail(STLITE_ERR_INVALID_ARG, "q and q_out must be both given or both NULL");
-  if (queries && (q_out == q->data || q_out == k->data || q_out == v->data))
-    return fail(STLITE_ERR_INVALID_ARG, "q_out must not alias an input");
   if (!aligned16(q_out) || !aligned16(q_norm) || !aligned16(k_norm))
     return fail(STLITE_ERR_INVALID_ARG, "q_out, q_norm and k_norm must be 16-byte aligned");
   if ((q_norm || k_norm) && !(eps >= 0.0f && std::isfinite(eps)))
     return fail(STLITE_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (queries) {
+    const size_t bytes = query_bytes(c);
+    if (rows_meet(c, q, c->n_q_heads, q_out, bytes) || rows_meet(c, k, c->n_kv_heads, q_out, bytes) ||
+        rows_meet(c, v, c->n_kv_heads, q_out, bytes) || meets_pool(c, q_out, bytes))
+      return fail(STLITE_ERR_INVALID_ARG, "q_out must not alias an input or the pool");
+  }
   a.c = device_view(c);
   a.q = rows_in(queries ? q : nullptr);
   a.k = rows_in(k);
@@ -354,8 +387,12 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   if (ws_bytes < p.bytes) return fail(STLITE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, p.bytes);
   if (reinterpret_cast<uintptr_t>(ws) % 256 != 0) return fail(STLITE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (!q || !out) return fail(STLITE_ERR_INVALID_ARG, "q and out must be non-NULL");
-  if (q == out) return fail(STLITE_ERR_INVALID_ARG, "out must not alias q");
+  const size_t bytes = query_bytes(c);
+  if (meet(q, bytes, out, bytes) || meets_pool(c, out, bytes))
+    return fail(STLITE_ERR_INVALID_ARG, "out must not alias q or the pool");
   if (!aligned16(q) || !aligned16(out)) return fail(STLITE_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  if (p.bytes > 0 && (meet(ws, p.bytes, q, bytes) || meet(ws, p.bytes, out, bytes) || meets_pool(c, ws, p.bytes)))
+    return fail(STLITE_ERR_WORKSPACE, "the workspace must not alias q, out or the pool");
   PagedAttnArgs a;
   a.c = device_view(c);
   a.q = q;

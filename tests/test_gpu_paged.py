@@ -909,6 +909,34 @@ def test_dropped_tensors_on_another_stream(torch_cuda, new):
     assert torch.equal(f.k, pools[0]) and torch.equal(f.v, pools[1])
 
 
+@pytest.mark.parametrize("new", [1, 5])
+def test_buffers_that_only_touch(torch_cuda, new):
+    """One allocation holds queries, output, workspace and pool without a byte between them, and an append's output lies
+    between its inputs' layers."""
+    import torch
+    f = Served((300, 40), (new, new), 16, "bf16", 2, 8, 2, seed=28)
+    n, size = 2 * 2 * new * 8 * D, max(f.cache.workspace_size(f.batch), 256) // 2
+    pool = f.k.numel()
+    buf = torch.empty(2 * pool + 2 * n + size, dtype=f.dt, device="cuda")
+    at = np.cumsum([0, n, n, size, pool, pool])
+    q, out, ws, k, v = (buf[a:b] for a, b in zip(at, at[1:]))
+    q, out, k, v = q.view(2, -1, 8, D), out.view(2, -1, 8, D), k.view(f.k.shape), v.view(f.v.shape)
+    k.copy_(f.k)
+    v.copy_(f.v)
+    q.copy_(f.randn(q.shape))
+    cache = f.P.PagedCache(k, v, f.cache.page_table, f.cache.seq_lens, 8, f.max_len)
+    f.P.paged_attention(cache, f.batch, q, out=out, workspace=ws)
+    f.compare(q, out)
+    m = f.total * (8 + 2 * 2) * D  # a layer of a fused projection
+    buf = f.randn((2 * m + n,))
+    qkv = torch.as_strided(buf, (2, f.total, 12, D), (m + n, 12 * D, D, 1))
+    parts = qkv.split([8, 2, 2], 2)
+    f.P.paged_append(cache, f.batch, *parts, q_out=buf[m:m + n].view(2, f.total, 8, D))
+    assert torch.equal(buf[m:m + n].view(2, f.total, 8, D), parts[0])
+    places = np.array(OP.new_places(f.table, f.lens, f.cu, 16, f.n_pages, f.max_len))
+    assert np.array_equal(_bits(k).reshape(2, 2, -1, D)[:, :, places], _bits(parts[1].contiguous()).transpose(0, 2, 1, 3))
+
+
 def test_dense_decode_agrees(torch_cuda):
     """The dense decode call and the paged one over identity pages, on the same cache."""
     import torch

@@ -596,3 +596,48 @@ def test_streams_and_devices_of_a_call(monkeypatch):
         with P._On(device, None):
             raise RuntimeError
     assert current == [0]
+
+
+# ---------------------------------------------------------------------------
+# Buffers that overlap
+# ---------------------------------------------------------------------------
+
+
+@needs_lib
+def test_overlaps_rejected():
+    """Outputs and workspaces that share a byte with an input, an output or the pool (never dereferenced here: every call
+    is refused)."""
+    lib, MB = S.load(), 1 << 20
+    f = Fake(counts=(0, 1, 3), k=1024 * MB, v=1025 * MB)
+    pool = 2 * 4 * 20 * 16 * 256
+    nq, nk = 2 * 3 * 28 * 256, 4 * 256
+    ws = ctypes.c_size_t(0)
+    assert lib.stlite_paged_workspace_size(f.ref, ctypes.byref(ws)) == S.OK and ws.value > nq and pool < MB
+
+    def attend(q=64 * MB, out=65 * MB, work=66 * MB):
+        return lib.stlite_paged_attention(f.ref, q, 1.0, out, work, ws.value, None)
+    for kw in (dict(q=64 * MB, out=64 * MB + 16), dict(q=64 * MB + nq - 16, out=64 * MB), dict(out=64 * MB + nq - 256),
+               dict(out=1024 * MB), dict(out=1024 * MB + pool - 16), dict(out=1025 * MB - nq + 16)):
+        assert attend(**kw) == S.ERR_INVALID_ARG and "alias" in _err(), kw
+    for kw in (dict(work=64 * MB), dict(work=65 * MB + (nq - 1) // 256 * 256), dict(work=64 * MB - 256), dict(work=1025 * MB),
+               dict(work=1024 * MB - (ws.value - 1) // 256 * 256)):
+        assert attend(**kw) == S.ERR_WORKSPACE and "alias" in _err(), kw
+
+    def append(q_out, q=64 * MB, k=80 * MB, v=96 * MB, stride=36 * 128, layer=1 << 20):
+        rows = [ctypes.byref(S._CRows(x, stride, layer)) for x in (q, k, v)]
+        return lib.stlite_paged_append(f.ref, None, None, *rows, None, None, 0.0, q_out, None)
+    last = 2 * 36 * 256  # the third token's row
+    for at, own in ((64 * MB, 28 * 256), (80 * MB, nk), (96 * MB, nk)):
+        for layer in (0, 2 * MB):
+            for q_out in (at + layer, at + layer + 16, at + layer - 16, at + layer + last + own - 16, at + layer - nq + 16):
+                assert append(q_out) == S.ERR_INVALID_ARG and "alias" in _err(), (at, layer, q_out)
+    # (from between the first two tokens' keys on it meets the second one's)
+    assert append(80 * MB + nk) == S.ERR_INVALID_ARG and "alias" in _err()
+    for q_out in (1024 * MB, 1025 * MB + pool - 256, 1024 * MB - nq + 16):
+        assert append(q_out) == S.ERR_INVALID_ARG and "alias" in _err()
+
+    cu = np.array([0, 50, 110])
+    p = S.Problem(2, 28, 4, 1, cu, np.zeros(3), np.zeros((0, 3)), S.budgets(cu, 1, 2), device="cpu")
+    size = 8 * 110 * 256
+    for k, v in ((1024 * MB, 64 * MB), (64 * MB, 1024 * MB), (1025 * MB + pool - 16, 64 * MB), (64 * MB, 1024 * MB - size + 16)):
+        assert lib.stlite_paged_compact(p.ref, f.ref, k, v, FAKE, 0, None) == S.ERR_INVALID_ARG and "alias" in _err()
