@@ -99,7 +99,7 @@ class Rope(_Fixed):
     """The position rotation (stlite_rope): one position axis, or three with ``sections`` pairs each."""
 
     def __init__(self, theta: float = 1e6, sections=(64,), interleaved: bool = False):
-        if len(sections) not in (1, 3) or sum(sections) != HEAD_DIM // 2:
+        if len(sections) not in (1, 3) or sum(sections) != HEAD_DIM // 2 or min(sections) < 0:
             raise ValueError(f"sections must be (64,) or three counts that add up to 64, got {tuple(sections)}")
         self.n_axes = len(sections)
         self.c = _CRope(float(theta), int(bool(interleaved)), self.n_axes, (ctypes.c_int32 * 3)(*sections), 0)
@@ -109,9 +109,13 @@ class NewTokens(_Fixed):
     """The new tokens of a call: prefix sums over the sequences, on the host and the device, which stay the same."""
 
     def __init__(self, cu_new, device="cuda"):
-        self.h = np.array(cu_new, dtype=np.int32)
-        if self.h.ndim != 1 or len(self.h) < 2:
+        given = np.asarray(cu_new)
+        if given.ndim != 1 or len(given) < 2:
             raise ValueError("cu_new must be a list of n_seqs + 1 prefix sums")
+        with np.errstate(invalid="ignore"):
+            self.h = given.astype(np.int32)
+        if not (self.h == given).all():
+            raise ValueError("cu_new must hold whole numbers of 32 bits")
         self.h.setflags(write=False)
         self.d = torch.from_numpy(self.h.copy()).to(device)
         self.total = int(self.h[-1])
@@ -143,6 +147,9 @@ class PagedCache(_Fixed):
         self.n_seqs, self.max_pages = page_table.shape
         self.n_q_heads, self.dtype, self.device = int(n_q_heads), k.dtype, k.device
         self.max_len = self.max_pages * self.page_size if max_len is None else int(max_len)
+        for name in ("n_q_heads", "max_len", "n_pages", "max_pages", "n_seqs"):
+            if not -2 ** 31 <= getattr(self, name) < 2 ** 31:  # (ctypes would cut it)
+                raise ValueError(f"{name} {getattr(self, name)} does not fit in 32 bits")
         self._c = _CPaged(self.n_layers, self.n_q_heads, self.n_kv_heads, HEAD_DIM, _DTYPES[k.dtype], self.page_size,
                           self.n_pages, self.n_seqs, self.max_pages, self.max_len, 0, k.data_ptr(), v.data_ptr(),
                           page_table.data_ptr(), seq_lens.data_ptr(), None, None)

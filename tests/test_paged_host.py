@@ -641,3 +641,27 @@ def test_overlaps_rejected():
     size = 8 * 110 * 256
     for k, v in ((1024 * MB, 64 * MB), (64 * MB, 1024 * MB), (1025 * MB + pool - 16, 64 * MB), (64 * MB, 1024 * MB - size + 16)):
         assert lib.stlite_paged_compact(p.ref, f.ref, k, v, FAKE, 0, None) == S.ERR_INVALID_ARG and "alias" in _err()
+
+
+# ---------------------------------------------------------------------------
+# Numbers that do not fit the C structs
+# ---------------------------------------------------------------------------
+
+
+def test_numbers_beyond_32_bits_rejected():
+    """They are refused, not cut to their low bits (2^32 + 40 to 40)."""
+    k = torch.zeros((1, 2, 3, 16, 128), dtype=torch.bfloat16)
+    table, lens = torch.zeros((1, 3), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    for kw in (dict(n_q_heads=2 ** 32 + 8), dict(n_q_heads=-2 ** 32 + 8), dict(n_q_heads=8, max_len=2 ** 32 + 40),
+               dict(n_q_heads=8, max_len=-2 ** 32 + 40)):
+        with pytest.raises(ValueError, match="32 bits"):
+            P.PagedCache(k, k, table, lens, **kw)
+    for cu in ([0, 2 ** 32 + 1], np.array([0, 2 ** 32 + 1]), torch.tensor([0, 2 ** 33]), [0, 1.5], [0.0, float("nan")], [0, 2.0 ** 40]):
+        with pytest.raises(ValueError, match="cu_new"):
+            P.NewTokens(cu, device="cpu")
+    for cu in ([0, 3], (0, 3), np.array([0, 3]), np.array([0.0, 3.0]), torch.tensor([0, 3]), np.array([0, 3], np.uint8)):
+        b = P.NewTokens(cu, device="cpu")
+        assert b.h.tolist() == b.d.tolist() == [0, 3] and b.h.dtype == np.int32 and b.total == 3
+    for sections in ((2 ** 32 + 16, 24, 24 - 2 ** 32), (16.0, 24, 24)):
+        with pytest.raises((ValueError, TypeError)):
+            P.Rope(sections=sections)
