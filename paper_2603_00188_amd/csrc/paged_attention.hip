@@ -368,13 +368,12 @@ __device__ inline u32x2_t read_transposed(uint32_t lds) {
 // 16 bytes per lane from offset `at` + `from` of a buffer to LDS address `to` + 16
 // lane.  In assembly because the compiler, which cannot tell the tiles apart, would
 // wait for every load in flight before each transposed read; it has no output
-// register, and wait_vmcnt counts it.  (The nops: M0 is read one wait state after
-// it is written, a scalar that the vector unit wrote, as a page read from LDS is,
-// five.)
+// register, and wait_vmcnt counts it.  The LDS address is an operand in M0, so that the
+// compiler knows what M0 holds.  (The nops: M0 is read one wait state after it is written,
+// a scalar that the vector unit wrote, as a page read from LDS is, five.)
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 __device__ inline void dma16(i32x4_t rsrc, uint32_t to, uint32_t at, uint32_t from) {
-  asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(at), "s"(rsrc), "s"(from), "s"(to)
-               : "memory");
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(at), "s"(rsrc), "s"(from), "{m0}"(to) : "memory");
 }
 
 template <typename T>

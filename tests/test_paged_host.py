@@ -665,3 +665,19 @@ def test_numbers_beyond_32_bits_rejected():
     for sections in ((2 ** 32 + 16, 24, 24 - 2 ** 32), (16.0, 24, 24)):
         with pytest.raises((ValueError, TypeError)):
             P.Rope(sections=sections)
+
+
+def test_assembly_leaves_m0_to_the_compiler():
+    """Inline assembly does not write M0, which indexed accesses and LDS loads go by, behind the compiler's back: what
+    reads it has it as an operand."""
+    import re
+    reads = 0
+    for name in sorted(os.listdir(CSRC)):
+        with open(os.path.join(CSRC, name)) as f:
+            text = f.read()
+        for m in re.finditer(r"\basm\b(?:\s+volatile)?\s*\((.*?)\)\s*;", text, re.S):
+            assert not re.search(r"\bm0\s*,", m.group(1)), (name, m.group(0))
+            if re.search(r"\blds\\?[\"n]", m.group(1)) and "load" in m.group(1):
+                reads += 1
+                assert '"{m0}"' in m.group(1), (name, m.group(0))
+    assert reads >= 1
