@@ -249,6 +249,17 @@ def test_extend(torch_cuda, lens, new, page, dtype, layers, hq, hk):
     assert np.array_equal(_bits(f.attend(q)), _bits(out)), "two calls differ"
 
 
+@pytest.mark.parametrize("group,tokens", [(7, 36), (1, 256), (3, 85), (20, 12), (128, 2)])
+def test_extend_at_the_ends_of_blocks(torch_cuda, group, tokens):
+    """A block has 256 rows, whole tokens of `group` heads: one token less, as many, one more, two blocks and one more,
+    each beside the others and behind a few keys or none."""
+    _log(f"paged extend, {tokens} tokens of {group} heads to a block")
+    new = [tokens - 1, tokens, tokens + 1, 2 * tokens, 2 * tokens + 1]
+    f = Served([n + c for n, c in zip(new, (0, 63, 1, 0, 130))], new, 16, "bf16", 1, 2 * group, 2, seed=29, fill=float("nan"))
+    q = f.randn((1, f.total, 2 * group, D), 1.5)
+    f.compare(q, f.attend(q))
+
+
 def test_extend_many_sequences(torch_cuda):
     """More sequences than threads look them up, idle ones among them."""
     rng = np.random.default_rng(4)

@@ -351,6 +351,19 @@ def test_workspace_does_not_depend_on_lengths_and_is_bounded():
     assert lib.stlite_paged_workspace_size(tiny.ref, ctypes.byref(n)) == S.OK and n.value == 0
 
 
+@needs_lib
+def test_workspace_is_what_the_shares_leave():
+    """Two parts of an item for each share, a row's maximum, sum and 128 sums in fp32: 512 shares of 16 or 32 heads with
+    one token each, 256 of 256 rows with more, however few or many tokens or heads those are."""
+    lib, n = S.load(), ctypes.c_size_t(0)
+    for cu, heads, shares, rows in (((0, 1, 2), 4, 512, 16), ((0, 0, 1), 64, 512, 16), ((0, 1, 2), 80, 512, 32),
+                                    ((0, 1, 2), 512, 512, 32), ((0, 2, 3), 4, 256, 256), ((0, 5, 6), 28, 256, 256),
+                                    ((0, 70, 71), 28, 256, 256), ((0, 70, 70), 512, 256, 256)):
+        f = Fake(counts=cu, n_layers=28, n_q_heads=heads, max_pages=10000, n_pages=10000, max_len=150000)
+        assert lib.stlite_paged_workspace_size(f.ref, ctypes.byref(n)) == S.OK
+        assert n.value == shares * 2 * rows * (1 + 1 + 128) * 4, (cu, heads)
+
+
 # ---------------------------------------------------------------------------
 # The binding
 # ---------------------------------------------------------------------------
