@@ -83,20 +83,26 @@ class _On:
 
 
 class _Fixed:
-    """Attributes that the C structs took over at construction: set once, so that no call goes by another value."""
+    """Attributes (``_fixed``) that the C structs took over at construction: set once, so that no call goes by another."""
+
+    _fixed = ()
 
     def __setattr__(self, name, value):
-        if name in self.__dict__ and self.__dict__[name] is not value:  # (``+=`` on a tensor assigns the same one)
+        if name in self._fixed and self.__dict__.get(name, value) is not value:  # (``+=`` on a tensor assigns the same one)
             raise AttributeError(f"{type(self).__name__}.{name} is fixed: make another {type(self).__name__}, or write into "
                                  "the tensor it holds")
         super().__setattr__(name, value)
 
     def __delattr__(self, name):
-        raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+        if name in self._fixed:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+        super().__delattr__(name)
 
 
 class Rope(_Fixed):
     """The position rotation (stlite_rope): one position axis, or three with ``sections`` pairs each."""
+
+    _fixed = ("n_axes", "c")
 
     def __init__(self, theta: float = 1e6, sections=(64,), interleaved: bool = False):
         if len(sections) not in (1, 3) or sum(sections) != HEAD_DIM // 2 or min(sections) < 0:
@@ -107,6 +113,8 @@ class Rope(_Fixed):
 
 class NewTokens(_Fixed):
     """The new tokens of a call: prefix sums over the sequences, on the host and the device, which stay the same."""
+
+    _fixed = ("h", "d", "total", "_h", "_d")
 
     def __init__(self, cu_new, device="cuda"):
         given = np.asarray(cu_new)
@@ -131,6 +139,9 @@ class PagedCache(_Fixed):
 
     The tensors are the cache's for good (a captured graph and the caches of single layers hold them too): other
     lengths or pages are written into them, ``cache.seq_lens.copy_(lens)``."""
+
+    _fixed = ("k", "v", "page_table", "seq_lens", "tensors", "n_layers", "n_q_heads", "n_kv_heads", "n_pages", "page_size",
+              "n_seqs", "max_pages", "max_len", "dtype", "device", "_c")
 
     def __init__(self, k, v, page_table, seq_lens, n_q_heads: int, max_len: Optional[int] = None):
         if k.dim() != 5 or k.shape[4] != HEAD_DIM or k.dtype not in _DTYPES:

@@ -566,6 +566,15 @@ def test_frozen_fields_are_not_assigned():
             setattr(r, name, other)
 
 
+def test_a_programs_own_attributes_are_its_own():
+    for x in (_cache(), P.NewTokens([0, 1], device="cpu"), P.Rope()):
+        x.step = 1
+        x.step = 2
+        assert x.step == 2
+        del x.step
+        assert not hasattr(x, "step")
+
+
 def test_copied_caches():
     import copy
     import pickle
