@@ -231,6 +231,8 @@ def _rows(t, name, cache, batch, heads):
 
 def _check_source(cache: PagedCache, p, k, v) -> None:
     """k and v of a compaction: rows of the pool's type, or 16-bit patterns as integers, which carry no type."""
+    if p.d["cu_budget"].device != cache.device:
+        raise ValueError(f"the problem is on {p.d['cu_budget'].device}, the cache on {cache.device}")
     n = cache.n_layers * cache.n_kv_heads * p.total_tokens * HEAD_DIM
     for t, name in ((k, "k"), (v, "v")):
         if (t.numel() != n or t.dtype not in (cache.dtype, torch.int16, torch.uint16) or not t.is_contiguous()

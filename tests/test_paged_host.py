@@ -519,6 +519,17 @@ def test_compaction_refuses_another_type(dtype):
 
 
 @needs_lib
+def test_compaction_refuses_a_problem_of_another_device():
+    """The kernel reads the problem's prefix sums: they lie where the cache does."""
+    p, cache, k = _compaction()
+    kept = torch.zeros((4, p.total_budget), dtype=torch.int32)
+    p.d["cu_budget"] = p.d["cu_budget"].to("meta")
+    for call in (lambda: P.paged_compact(cache, p, k, k, kept), lambda: P.check_compression(cache, p, k, k)):
+        with pytest.raises(ValueError, match="problem is on meta"):
+            call()
+
+
+@needs_lib
 def test_compression_refuses_its_cache_first(monkeypatch):
     """A cache that the pass cannot go into: refused with nothing enqueued."""
     def enqueued(*a, **kw):
