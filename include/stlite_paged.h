@@ -163,14 +163,15 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  *   q    [n_layers][total_new][n_q_heads][d], 16-byte aligned
  *   out  the same layout and type; 16-byte aligned, must not alias q or the pool
  *   scale  > 0, at most 2^127
- * fp32 logits, softmax statistics and sums, which stay finite for values of any
- * size and up to 2^20 keys, and for logits of any size in fp32's range (scale q . k
- * log2(e) up to 2^128; a token that sees a greater one gets NaN).  With one new token per sequence the weights keep fp32's
- * 24 bits (fp16: 22, or 2^-40 of the greatest weight); with more they are rounded to
- * the type of the call before they meet v.  An infinity or NaN of a token that is
- * seen reaches the output whatever its weight (an infinity of a weight that is
- * rounded to 0 as NaN).  Rows of out belong to new tokens only: nothing behind
- * total_new is written.  The workspace must not alias q, out or the pool.
+ * fp32 logits, softmax statistics and sums, which stay finite for logits (scale q . k
+ * log2(e)) and values of any size in fp32's range and up to 2^20 keys.  With one new
+ * token per sequence the weights keep fp32's 24 bits (fp16: 22, or 2^-40 of the greatest
+ * weight); with more they are rounded to the type of the call before they meet v.
+ * An infinity or NaN of a value that is seen reaches the output whatever its weight (an
+ * infinity of a weight that is rounded to 0 as NaN).  A logit of infinity or NaN makes
+ * its token's head NaN; one of -infinity weighs nothing, and where all are, the output
+ * is 0.  Rows of out belong to new tokens only: nothing behind total_new is written.
+ * The workspace must not alias q, out or the pool.
  */
 stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, float scale, uint16_t* out,
                                      void* workspace, size_t workspace_bytes, void* stream);

@@ -327,6 +327,9 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 //                    order is a permutation of the keys within 16, which the V
 //                    reads follow;
 //   O^T += V^T P^T   A: V read transposed from LDS (ds_read_b64_tr_b16).
+// The weights are rounded to the type of the call, which the matrix instructions take: half
+// a step of it, as the output.  A second term of each, as for one token, would add 1024
+// cycles of products to a step's 2048.
 // The reference of the weights moves only when a tile exceeds it by 2^kLazy, so that the
 // output is rescaled rarely.  It is a whole number: its sum with kBias is exact, and one
 // fused product and sum gives an exponent (two roundings more would be another instruction

@@ -331,6 +331,35 @@ def test_logits_of_any_size(torch_cuda, new, dtype):
 
 @pytest.mark.parametrize("new", [1, 3, 140])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("long", [False, True])
+def test_infinite_logits(torch_cuda, new, dtype, long):
+    """Keys whose logit is -infinity weigh nothing, and a token all of whose logits are gets 0; a logit of infinity makes
+    the tokens that see it NaN.  In one part and in many."""
+    import torch
+    f = Served((9000, 5000, 6000) if long else (300, 200, 171), (new,) * 3, 16, dtype, 1, 4, 1, seed=30)
+    rows = f.k.view(1, 1, -1, D)
+    rows.zero_()
+    at = lambda s, j: OP.place(f.table, s, j, 16, f.n_pages)  # noqa: E731
+    for j in (0, 5, 63, 64, 70, f.lens[0] - new):
+        rows[0, 0, at(0, j), 0] = float("-inf")
+    for j in range(f.lens[1]):
+        rows[0, 0, at(1, j), 0] = float("-inf")
+    last = f.lens[2] - new // 2 - 1
+    rows[0, 0, at(2, last), 0] = float("inf")
+    q = torch.zeros((1, f.total, 4, D), dtype=f.dt, device="cuda")
+    q[..., 0] = 1
+    out = f.attend(q)
+    sees = int(f.cu[2]) + max(last - (f.lens[2] - new), 0)
+    assert not out[0, f.cu[1]:f.cu[2]].any() and torch.isnan(out[0, sees:]).all()
+    ref, weight, keys, _ = OP.attention(_f64(q[0]), _f64(f.k[0]), _f64(f.v[0]), f.table, f.lens, f.cu, f.max_len, D ** -0.5, 4)
+    u = _half_step(dtype)
+    lim = u * np.abs(ref) + ((0 if new == 1 else u) + 2.0 ** -22 + 2 * keys * 2.0 ** -24)[..., None] * weight + 2.0 ** -25
+    for part in (slice(0, f.cu[1]), slice(f.cu[2], sees)):
+        assert (np.abs(_f64(out[0]) - ref) <= lim)[part].all()
+
+
+@pytest.mark.parametrize("new", [1, 3, 140])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_masked_values_have_no_influence(torch_cuda, new, dtype):
     """Keys and values of later tokens that are infinite or NaN reach the tokens that
     see them, and no other."""
