@@ -331,10 +331,13 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // a step of it, as the output.  A second term of each, as for one token, would add 1024
 // cycles of products to a step's 2048.
 // The reference of the weights moves only when a tile exceeds it by 2^kLazy, so that the
-// output is rescaled rarely.  It is a whole number: its sum with kBias is exact, and one
-// fused product and sum gives an exponent (two roundings more would be another instruction
-// for each of a tile's weights).  Beyond kFar, where a logit's rounding is no longer small
-// against the headroom above the reference, the logits are rounded before it is taken off.
+// output is rescaled rarely.  It is the greatest logit to within 2^-15, so that the
+// greatest weight, a power of two to that precision, is rounded to one (a whole number
+// instead made the error against 64 bits 0.0023, not 0.0020, behind 30k tokens), and has
+// 14 bits behind the point: its sum with kBias is exact up to kFar, and one fused product
+// and sum gives an exponent.  Beyond kFar the logits are rounded before it is taken off
+// (an instruction more for each, but there a logit's rounding would use up the headroom
+// above the reference, and the bias would be lost in it).
 //
 // A step of a wave has two halves: its products (the logits of tile t + 1, the
 // values of tile t) and its vector work (the weights of tile t + 1, and DMA).  The
@@ -354,7 +357,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // tokens 206 us, 0.73 PFLOP/s.
 
 constexpr float kLazy = 8.0f;
-constexpr float kFar = 65536.0f;  // an exponent is off by 2^-8 at most, 1.0027 of a weight
+constexpr float kFar = 960.0f;  // 960 + 28 has 10 bits before the point
 constexpr int kExtWaves = 8;
 static_assert(kExtRows == kExtWaves * 32);
 constexpr int kRing = 4;
@@ -582,7 +585,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       swap32(mt, other);
       const float top = base2(fmaxf(mt, other), a.scale2);
       if (__ballot(top - m_ref > kLazy)) {
-        const float m_new = fmaxf(m_ref, ceilf(top));
+        const float m_new = fmaxf(m_ref, fabsf(top) > kFar ? top : rintf(top * 0x1p14f) * 0x1p-14f);
         const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
         m_ref = m_new;
         l_run *= alpha;

@@ -358,6 +358,28 @@ def test_infinite_logits(torch_cuda, new, dtype, long):
         assert (np.abs(_f64(out[0]) - ref) <= lim)[part].all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("scale", [D ** -0.5, 0.7, 100.0, 1e6])
+def test_the_greatest_weight_is_not_rounded(torch_cuda, dtype, scale):
+    """A token that sees one key, or many that another outweighs by 2^100, gets that one's value bit by bit: its weight is
+    a power of two to 2^-15, well inside half a step of either type."""
+    import torch
+    f = Served((150, 90, 40), (150, 20, 1), 16, dtype, 1, 4, 1, seed=31)
+    q = f.randn((1, f.total, 4, D), 1.5)
+    out = f.attend(q, scale=scale)
+    value = lambda s, j: f.v.view(-1, D)[OP.place(f.table, s, j, 16, f.n_pages)]  # noqa: E731
+    assert torch.equal(out[0, 0], value(0, 0).expand(4, D))
+    q.zero_()
+    q[..., 0] = 3.0
+    rows, rng = f.k.view(-1, D), np.random.default_rng(31)
+    for s, at in enumerate((7, 70, 5)):
+        for j in range(f.lens[s]):  # below the one that stands out by 2^100 in base 2
+            rows[OP.place(f.table, s, j, 16, f.n_pages), 0] = float((rng.random() - (0 if j == at else 101)) * 0.7 / 3 / scale)
+        seen = slice(int(f.cu[s]) + max(at - (f.lens[s] - f.new[s]), 0), int(f.cu[s + 1]))
+        want = value(s, at)
+        assert torch.equal(f.attend(q, scale=scale)[0, seen], want.expand(seen.stop - seen.start, 4, D)), s
+
+
 @pytest.mark.parametrize("new", [1, 3, 140])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_masked_values_have_no_influence(torch_cuda, new, dtype):
