@@ -12,7 +12,8 @@ arithmetic runs in the library's gfx950 kernels.  Tensors are bf16 or fp16, of
 the pool's type and on its device.  Everything runs on ``stream`` (the device's
 current one by default), allocates nothing where ``q_out``, ``out`` and
 ``workspace`` are given, and follows ``seq_lens`` and ``page_table`` on the
-device, so that a step can be captured into a graph and replayed.  With a
+device, so that a step can be captured into a graph and replayed (the cache, the
+batch and the call's tensors live as long as the graph).  With a
 ``torch.cuda.Stream`` the call's tensors, the batch's among them, may be dropped
 at once; with the handle of a stream the caller keeps them until the work has run.
 """

@@ -999,6 +999,44 @@ def test_buffers_that_only_touch(torch_cuda, new):
     assert np.array_equal(_bits(k).reshape(2, 2, -1, D)[:, :, places], _bits(parts[1].contiguous()).transpose(0, 2, 1, 3))
 
 
+@pytest.mark.parametrize("layers,seqs,hq,extend", [(4, 65535, 128, False), (4, 65535, 128, True), (65535, 2, 2, False),
+                                                   (65535, 2, 2, True)])
+def test_limits_of_a_call(torch_cuda, layers, seqs, hq, extend):
+    """As many sequences, or layers, as a call may have, and queries of more than 2^32 elements.  Every token sees one key,
+    so that its output is that key's value, but for the second token of the last sequence, which sees two equal keys."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(32)
+    new = torch.ones(seqs, dtype=torch.int64)
+    new[-1] += extend
+    batch = P.NewTokens(torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)]))
+    n = batch.total
+    table = torch.randperm(seqs, generator=gen, device="cuda").to(torch.int32).view(seqs, 1)
+    pool = [torch.full((layers, 1, seqs, 16, D), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    cache = P.PagedCache(*pool, table, new.to(torch.int32).cuda(), hq)
+    k, v = (torch.randn((layers, n, 1, D), generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    if extend:
+        k[:, -1] = k[:, -2]
+    q = torch.randn((1, n, hq, D), generator=gen, device="cuda", dtype=torch.bfloat16).expand(layers, -1, -1, -1)
+    rotated = P.paged_append(cache, batch, q, k, v)
+    assert torch.equal(rotated, q)
+    first = slice(0, n - extend)
+    at = table[:, 0].long()
+    for x, rows in zip(pool, (k, v)):
+        assert torch.equal(x[:, 0, at, 0], rows[:, first, 0]) and torch.isnan(x[:, 0, at[:-1], 1:]).all()
+        if extend:
+            assert torch.equal(x[:, 0, at[-1], 1], rows[:, -1, 0])
+    out = P.paged_attention(cache, batch, rotated)
+    for layer in range(0, layers, max(layers // 64, 1)):
+        assert torch.equal(out[layer, first], v[layer, first].expand(-1, hq, -1)), layer
+    assert torch.equal(out[-1, first], v[-1, first].expand(-1, hq, -1))
+    if extend:
+        mean = (v[:, -1].float() + v[:, -2].float()) / 2
+        bound = 2.0 ** -8 * mean.abs() + (2.0 ** -8 + 2.0 ** -20) * (v[:, -1].float().abs() + v[:, -2].float().abs()) / 2
+        assert ((out[:, -1].float() - mean).abs() <= bound + 2.0 ** -100).all()
+
+
 def test_dense_decode_agrees(torch_cuda):
     """The dense decode call and the paged one over identity pages, on the same cache."""
     import torch
