@@ -9,6 +9,10 @@
  *   stlite_paged_append     new tokens: the per-head norm and the rotation of
  *                           queries and keys, keys and values into pages
  *   stlite_paged_attention  causal attention of the new tokens over the pages
+ *   stlite_paged_read       the new tokens' rows out of the pages
+ *   stlite_paged_grow       lengths, pages and places for the next new tokens
+ *   stlite_paged_release    pages behind a sequence's end, back to the free ones
+ *   stlite_verify_drafts    drafted tokens against the target's probabilities
  *
  * Conventions (pointers, streams, units, ownership, errors) are those of
  * stlite.h: the calls only enqueue work, allocate nothing, keep no state, and
@@ -20,6 +24,17 @@
  * page_table [n_seqs][max_pages] is shared by all layers and kv heads: token j of
  * sequence s is row j % page_size of page page_table[s][j / page_size].  A cache
  * of one layer is the same struct with n_layers = 1 and k, v at that layer.
+ *
+ * A pool in 4 bits (a dtype with STLITE_KV4).  k and v are bytes, [n_layers]
+ * [n_kv_heads][n_pages][page_size * 68]: a page is page_size rows of 64 bytes of codes
+ * and then page_size rows of 4 scale bytes.  Block b of a row is its values 32 b to
+ * 32 b + 31; value 2 i is the low half of byte i, value 2 i + 1 the high half: a sign
+ * (bit 3) and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6, times 2^(scale byte - 127).  A row that
+ * is stored gets for each block the least power of two of which 7 times reaches the
+ * block's greatest magnitude, cut to 2^-120 .. 2^125 (fp16: 2^-14 .. 2^13), and each value
+ * the nearest code, ties to the even one, beyond 6 to 6.  A block with an infinity or NaN
+ * gets scale byte 255: all of its values are NaN.  The same calls store and read such a
+ * pool; what they compute, they compute of the values that the codes stand for.
  *
  * Lengths live on the device, so that a captured graph follows them: seq_lens[s]
  * counts the tokens of sequence s INCLUDING the new ones of this call.  The new
@@ -44,10 +59,14 @@
 extern "C" {
 #endif
 
-/* Type of q, k, v, the pool, the norm weights and the outputs of a call. */
+/* Type of q, k, v, the pool, the norm weights and the outputs of a call; the pool's
+ * own with STLITE_KV4. */
 typedef enum stlite_dtype {
   STLITE_BF16 = 0,
-  STLITE_FP16 = 1 /* IEEE half */
+  STLITE_FP16 = 1,                           /* IEEE half */
+  STLITE_KV4 = 16,                           /* flag: the pool holds 4 bits */
+  STLITE_BF16_KV4 = STLITE_BF16 | STLITE_KV4,
+  STLITE_FP16_KV4 = STLITE_FP16 | STLITE_KV4
 } stlite_dtype;
 
 /*
@@ -72,8 +91,8 @@ typedef struct stlite_paged {
   int64_t total_new;         /* = cu_new[n_seqs] */
   void* k;                   /* the pools, 16-byte aligned */
   void* v;
-  const int32_t* page_table; /* device [n_seqs][max_pages] */
-  int32_t* seq_lens;         /* device [n_seqs]; only stlite_paged_compact writes it */
+  int32_t* page_table;       /* device [n_seqs][max_pages]; only grow and release write it */
+  int32_t* seq_lens;         /* device [n_seqs]; compact, grow, release and verify write it */
   const int32_t* cu_new;     /* device [n_seqs+1], prefix sums of the new tokens, cu_new[0] = 0 */
   const int32_t* h_cu_new;   /* host mirror of cu_new */
 } stlite_paged;
@@ -125,7 +144,7 @@ stlite_status stlite_paged_workspace_size(const stlite_paged* c, size_t* bytes);
  * j < B_s, row kept[u][cu_budget[s] + j] of k and v (the layout of
  * stlite_compact_kv) becomes token j of sequence s.  Exact row copies of 16-bit
  * patterns, which must be of the pool's type (the compression pass knows bf16 alone:
- * its rows belong in a bf16 pool).  seq_lens[s] becomes B_s.  p and c must agree in
+ * its rows belong in a bf16 pool); into a 4-bit pool, their codes.  seq_lens[s] becomes B_s.  p and c must agree in
  * n_layers, n_kv_heads and n_seqs, and every B_s must be at most c->max_len; the
  * new tokens (total_new, cu_new, h_cu_new) are not read.  per_layer != 0: one
  * kept list per layer, as in stlite_compact_kv_layer.  A kept index outside
@@ -140,7 +159,9 @@ stlite_status stlite_paged_compact(const stlite_problem* p, const stlite_paged* 
  * every layer, new token i and head, with x a row of q or k:
  *   n = x * w / sqrt(mean(x^2) + eps)   where norm weights w are given, else x
  *   (y_a, y_b) = (n_a cos - n_b sin, n_b cos + n_a sin)   for every pair (a, b)
- * in fp32, rounded once; the angles are formed in 64 bits.  The q rows' y go to
+ * in fp32, rounded once; the angles are formed in 64 bits.  (What goes into a 4-bit pool
+ * is formed in 64 bits throughout: the codes are those of the exact y but where y lies
+ * within 64 bits' rounding of a border.)  The q rows' y go to
  * q_out [n_layers][total_new][n_q_heads][d], the k rows' y and the v rows as they
  * are to the tokens' places in the pool.
  *   positions  int32 [n_axes][total_new]; rope and positions both NULL: no rotation
@@ -166,7 +187,8 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  * fp32 logits, softmax statistics and sums, which stay finite for logits (scale q . k
  * log2(e)) and values of any size in fp32's range and up to 2^20 keys.  With one new
  * token per sequence the weights keep fp32's 24 bits (fp16: 22, or 2^-40 of the greatest
- * weight); with more they are rounded to the type of the call before they meet v.
+ * weight); with more, and over a 4-bit pool, they are rounded to the type of the call
+ * before they meet v.
  * An infinity or NaN of a value that is seen reaches the output whatever its weight (an
  * infinity of a weight that is rounded to 0 as NaN).  A logit of infinity or NaN makes
  * its token's head NaN; one of -infinity weighs nothing, and where all are, the output
@@ -175,6 +197,14 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
  */
 stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, float scale, uint16_t* out,
                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The new tokens' rows out of the pages: k_out, v_out [n_layers][total_new][n_kv_heads][d]
+ * in the call's 16-bit type, each nullable, 16-byte aligned; they must not alias the pool.
+ * A row of an invalid page, or whose index would be negative, is zeros.  With cu_new the
+ * prefix sums of the lengths it reads whole sequences (to move them, or to a dense cache).
+ */
+stlite_status stlite_paged_read(const stlite_paged* c, uint16_t* k_out, uint16_t* v_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -8,9 +8,9 @@ namespace stlite {
 
 // The cache and the batch of new tokens, as the kernels see them.
 struct PagedDev {
-  uint16_t* k;  // [units][n_pages][page][d]
+  uint16_t* k;  // [units][n_pages][page][d]; of a 4-bit pool: [units][n_pages][page * 68 bytes]
   uint16_t* v;
-  const int32_t* page_table;  // [n_seqs][max_pages]
+  int32_t* page_table;  // [n_seqs][max_pages]; only growing and releasing write it
   int32_t* seq_lens;          // [n_seqs], new tokens included
   const int32_t* cu_new;      // [n_seqs + 1]
   int32_t n_layers, n_q_heads, n_kv_heads, n_units, group;
@@ -27,6 +27,12 @@ struct PagedCompactArgs {
   const uint16_t* v;
   const int32_t* kept;
   int32_t kept_per_layer;
+};
+
+struct PagedReadArgs {
+  PagedDev c;
+  uint16_t* k_out;  // [layers][total_new][kv_heads][d], nullable
+  uint16_t* v_out;
 };
 
 struct RowsIn {
@@ -78,10 +84,14 @@ struct PagedAttnArgs {
   float* po;          // workspace [shares][2][rows][d]: O, unnormalised
 };
 
-hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream);
-hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t stream);
+// four: a 4-bit pool; half: fp16, else bf16
+hipError_t launch_paged_compact(const PagedCompactArgs& a, bool four, bool half, hipStream_t stream);
+hipError_t launch_paged_read(const PagedReadArgs& a, bool four, bool half, hipStream_t stream);
+hipError_t launch_paged_append(const PagedAppendArgs& a, bool four, bool half, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
-hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t stream);
+hipError_t launch_paged4_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
+hipError_t launch_paged_extend(const PagedAttnArgs& a, bool four, bool half, hipStream_t stream);
+hipError_t launch_paged_join(const PagedAttnArgs& a, bool half, hipStream_t stream);
 
 // ---------------------------------------------------------------------------
 // Device helpers

@@ -8,7 +8,7 @@
 #include <new>
 #include <vector>
 
-#include "paged.h"
+#include "paged4.h"
 #include "stlite.h"
 #include "stlite_paged.h"
 
@@ -58,8 +58,9 @@ stlite_status check_cache(const stlite_paged* c, bool batch) {
   if (c->n_q_heads / c->n_kv_heads > kMaxGroup)
     return fail(STLITE_ERR_UNSUPPORTED, "%d query heads per kv head: at most %d", c->n_q_heads / c->n_kv_heads,
                 kMaxGroup);
-  if (c->dtype != STLITE_BF16 && c->dtype != STLITE_FP16)
-    return fail(STLITE_ERR_INVALID_ARG, "dtype must be STLITE_BF16 or STLITE_FP16 (got %d)", c->dtype);
+  if ((c->dtype & ~STLITE_KV4) != STLITE_BF16 && (c->dtype & ~STLITE_KV4) != STLITE_FP16)
+    return fail(STLITE_ERR_INVALID_ARG, "dtype must be STLITE_BF16 or STLITE_FP16, with STLITE_KV4 or without (got %d)",
+                c->dtype);
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128 && c->page_size != 256)
     return fail(STLITE_ERR_UNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256 (got %d)", c->page_size);
   if (c->n_pages < 1) return fail(STLITE_ERR_INVALID_ARG, "n_pages must be >= 1");
@@ -92,6 +93,9 @@ stlite_status check_cache(const stlite_paged* c, bool batch) {
                 c->h_cu_new[c->n_seqs]);
   return STLITE_OK;
 }
+
+bool is_four(const stlite_paged* c) { return (c->dtype & STLITE_KV4) != 0; }
+bool is_half(const stlite_paged* c) { return (c->dtype & ~STLITE_KV4) == STLITE_FP16; }
 
 PagedDev device_view(const stlite_paged* c) {
   PagedDev d;
@@ -204,7 +208,7 @@ bool meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
   return a && b && x < y + b_bytes && y < x + a_bytes;
 }
 size_t pool_bytes(const stlite_paged* c) {
-  return size_t(c->n_layers) * c->n_kv_heads * c->n_pages * c->page_size * kHeadDim * sizeof(uint16_t);
+  return size_t(c->n_layers) * c->n_kv_heads * c->n_pages * c->page_size * (is_four(c) ? kRow4 : kHeadDim * sizeof(uint16_t));
 }
 size_t query_bytes(const stlite_paged* c) {
   return size_t(c->n_layers) * c->total_new * c->n_q_heads * kHeadDim * sizeof(uint16_t);
@@ -309,7 +313,7 @@ stlite_status stlite_paged_compact(const stlite_problem* p, const stlite_paged* 
   a.v = v;
   a.kept = kept;
   a.kept_per_layer = per_layer != 0;
-  return hip_status(launch_paged_compact(a, static_cast<hipStream_t>(stream)), "paged_compact launch");
+  return hip_status(launch_paged_compact(a, is_four(c), is_half(c), static_cast<hipStream_t>(stream)), "paged_compact launch");
 }
 
 stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope, const int32_t* positions,
@@ -371,7 +375,7 @@ stlite_status stlite_paged_append(const stlite_paged* c, const stlite_rope* rope
   a.k_norm = k_norm;
   a.eps = eps;
   a.positions = positions;
-  return hip_status(launch_paged_append(a, c->dtype == STLITE_FP16, static_cast<hipStream_t>(stream)),
+  return hip_status(launch_paged_append(a, is_four(c), is_half(c), static_cast<hipStream_t>(stream)),
                     "paged_append launch");
 }
 
@@ -412,10 +416,28 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.pm = static_cast<float*>(ws);
   a.pl = a.pm + align_up(slots * sizeof(float)) / sizeof(float);
   a.po = a.pl + align_up(slots * sizeof(float)) / sizeof(float);
-  const bool half = c->dtype == STLITE_FP16;
+  const bool four = is_four(c), half = is_half(c);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return hip_status(p.decode ? launch_paged_decode(a, half, s) : launch_paged_extend(a, half, s),
+  return hip_status(!p.decode ? launch_paged_extend(a, four, half, s)
+                    : four    ? launch_paged4_decode(a, half, s)
+                              : launch_paged_decode(a, half, s),
                     "paged_attention launch");
+}
+
+stlite_status stlite_paged_read(const stlite_paged* c, uint16_t* k_out, uint16_t* v_out, void* stream) {
+  const stlite_status st = check_cache(c, true);
+  if (st != STLITE_OK) return st;
+  if (c->total_new == 0 || (!k_out && !v_out)) return ok();
+  if (!aligned16(k_out) || !aligned16(v_out))
+    return fail(STLITE_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  const size_t bytes = size_t(c->n_layers) * c->total_new * c->n_kv_heads * kHeadDim * sizeof(uint16_t);
+  if (meets_pool(c, k_out, bytes) || meets_pool(c, v_out, bytes) || meet(k_out, bytes, v_out, bytes))
+    return fail(STLITE_ERR_INVALID_ARG, "k_out and v_out must not alias the pool or one another");
+  PagedReadArgs a;
+  a.c = device_view(c);
+  a.k_out = k_out;
+  a.v_out = v_out;
+  return hip_status(launch_paged_read(a, is_four(c), is_half(c), static_cast<hipStream_t>(stream)), "paged_read launch");
 }
 
 }  // extern "C"

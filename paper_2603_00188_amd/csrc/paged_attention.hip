@@ -4,6 +4,9 @@
 // joins the parts of items that several work-groups share.
 #include <float.h>
 
+#include <type_traits>
+
+#include "paged4.h"
 #include "paged_plan.h"
 #include "tile_lds.h"
 
@@ -12,32 +15,7 @@ namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-// The page table of one sequence as a wave reads it: 64 entries in a register,
-// one per lane, fetched by index without a memory access.
-struct PageWindow {
-  const int32_t* row;
-  int32_t n_pages, last;  // last: index of the row's last entry
-  int32_t base;           // first entry held
-  int32_t held;           // this lane's entry
-  uint64_t bad;           // entries out of range
-
-  __device__ PageWindow(const PagedDev& c, int32_t seq)
-      : row(c.page_table + int64_t(seq) * c.max_pages), n_pages(c.n_pages), last(c.max_pages - 1), base(-1), held(0), bad(0) {}
-
-  // Makes the window hold `entry` (wave-uniform).
-  __device__ void seek(int32_t entry) {
-    if ((entry & ~63) == base) return;
-    base = entry & ~63;
-    const int32_t e = row[min(base + int32_t(threadIdx.x & 63), last)];
-    const bool ok = e >= 0 && e < n_pages;
-    held = ok ? e : 0;
-    bad = __ballot(!ok);
-  }
-  __device__ int32_t page(int32_t entry) const { return __builtin_amdgcn_readlane(held, entry & 63); }
-  __device__ bool is_bad(int32_t entry) const { return (bad >> (entry & 63)) & 1; }
-};
-
-// The same with the entries in LDS, 64 words of this wave's own: a register held
+// A PageWindow with the entries in LDS, 64 words of this wave's own: a register held
 // through a long loop is dear in the several-token kernel.
 struct LdsPageWindow {
   const int32_t* row;
@@ -382,12 +360,26 @@ __device__ inline void dma16(i32x4_t rsrc, uint32_t to, uint32_t at, uint32_t fr
   asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(at), "s"(rsrc), "s"(from), "{m0}"(to) : "memory");
 }
 
-template <typename T>
+// The same of 4 bytes; lane j lands at `to` + 4 j.
+__device__ inline void dma4(i32x4_t rsrc, uint32_t to, uint32_t at, uint32_t from) {
+  asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, %2 offen lds" ::"v"(at), "s"(rsrc), "s"(from), "{m0}"(to) : "memory");
+}
+
+// FOUR: over a 4-bit pool.  The tiles come as they are, by DMA, kAhead4 of them under way
+// (a wave's sixteen keys of a tile are one run of codes and one of scales), and the wave
+// that fetched them turns them into 16-bit tiles in the vector half of its step, a block of
+// 32 values to a lane: K(t+2) in place of K(t), V(t+2) in place of V(t), so rings of two do.
+constexpr int kAhead4 = 8;
+constexpr int kRaw4 = 16 * kCodes4 + 256;  // a wave's part of a tile: codes, and a row's scales for each lane
+
+template <typename T, bool FOUR>
 __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
   constexpr int NT = kExtWaves * 64;
-  __shared__ __align__(1024) uint16_t sm_tiles[2 * kRing * kTileBytes / 2];  // K, then V: [slot][64][128]
+  constexpr int kSlots = FOUR ? 2 : kRing;
+  __shared__ __align__(1024) uint16_t sm_tiles[2 * kSlots * kTileBytes / 2];  // K, then V: [slot][64][128]
+  __shared__ __align__(1024) uint8_t sm_raw[FOUR ? kExtWaves * kAhead4 * kRaw4 : 16];
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
   __shared__ int32_t sm_pages[kExtWaves][64];
   __shared__ int2 sm_odd[kExtWaves];
@@ -419,7 +411,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   uint32_t v_lane;
   {
     const int i = lane & 15, c0 = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    v_lane = lds0 + kRing * kTileBytes + (4 * h + (i >> 2)) * 256 + ((4 * (i >> 2) + (c0 ^ h)) << 4) + (i & 1) * 8;
+    v_lane = lds0 + kSlots * kTileBytes + (4 * h + (i >> 2)) * 256 + ((4 * (i >> 2) + (c0 ^ h)) << 4) + (i & 1) * 8;
   }
   // DMA load g brings keys 4 g + (lane >> 4) of the wave's sixteen: a lane's row and
   // the chunk that belongs in its 16 bytes (+ 1024 g, ^ 64 g or ^ 16 g).
@@ -427,7 +419,13 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   const uint32_t dma_lane = (lane >> 4) * 256 + (((lane & 15) ^ (group ? 4 * (lane >> 4) : lane >> 4)) << 4);
   const uint32_t dma_swizzle = group ? 16 : 64;
   const uint16_t* const pool = group ? c.v : c.k;
-  const uint32_t dma_lds = lds0 + (group * kRing * kPagedTile + key0) * (kHeadDim * 2);
+  const uint32_t dma_lds = lds0 + (group * kSlots * kPagedTile + key0) * (kHeadDim * 2);
+  // FOUR: a lane's block, lane & 3, of key lane4 of the wave's sixteen (eight lanes write
+  // two keys' chunks at once, of V two whose slots differ in more than the block), and where
+  // its first chunk goes (the next ones: ^ 16, ^ 32, ^ 48).
+  const int lane4 = group ? ((lane >> 2 & 3) << 2) | lane >> 4 : lane >> 2;
+  const uint32_t raw_lds = uint32_t(reinterpret_cast<uintptr_t>(sm_raw)) + wave * (kAhead4 * kRaw4);
+  const uint32_t write4 = dma_lds + lane4 * 256 + (((lane & 3) << 2 ^ (group ? 4 * (lane4 & 3) + (lane4 >> 2) : lane4)) << 4);
 
   for (;;) {
     const int unit = it.unit;
@@ -499,7 +497,51 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 
     // --- one tile's arithmetic ---
     auto full = [&](int32_t t, uint32_t b, int32_t first) { return b == 0 && t * kPagedTile + kPagedTile - 1 <= first; };
-    auto slot = [&](int32_t t) { return uint32_t((t - t0) & (kRing - 1)) * kTileBytes; };
+    auto slot = [&](int32_t t) { return uint32_t((t - t0) & (kSlots - 1)) * kTileBytes; };
+    // FOUR: this wave's part of tile t on its way (rows past the sequence's end lie in its
+    // last page, whatever they hold), and its sixteen keys' bad groups.
+    auto fetch4 = [&](int32_t t) {
+      const uint64_t from = uint64_t(PagedPlan<NT>::uniform(
+          reinterpret_cast<int64_t>(reinterpret_cast<const uint8_t*>(pool) + page4(c, unit, __builtin_amdgcn_readfirstlane(ahead)))));
+      const i32x4_t rsrc = {int32_t(uint32_t(from)), int32_t(uint32_t(from >> 32) & 0xffffu), (in_page + 1) * kRow4, kBufferFlags};
+      const uint32_t row = __builtin_amdgcn_readfirstlane(uint32_t((min(t, last) * kPagedTile + key0) & in_page));
+      const uint32_t to = __builtin_amdgcn_readfirstlane(raw_lds + ((t - t0) & (kAhead4 - 1)) * kRaw4);
+      dma16(rsrc, to, lane * 16, row * kCodes4);
+      dma4(rsrc, to + 16 * kCodes4, lane4 * 4, (in_page + 1) * kCodes4 + row * 4);
+      uint64_t m = 0;
+      if (pages.bad)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) m |= uint64_t(pages.is_bad(entry_of(t, 16 * g))) << g;
+      look(t + 1);
+      return m;
+    };
+    // FOUR: that part, once it has landed, into the 16-bit tile.  0 * NaN is no zero: in a
+    // tile where some queries do not see every key, blocks of values that are not finite are
+    // cleared, and reach the queries that see them behind the last tile.
+    auto convert4 = [&](int32_t t, uint32_t b) {
+      wait_vmcnt<2 * (kAhead4 - 1)>();
+      const uint32_t at = raw_lds + ((t - t0) & (kAhead4 - 1)) * kRaw4;
+      u32x4_t e = *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)(at + lane4 * kCodes4 + (lane & 3) * 16));
+      uint32_t byte = *reinterpret_cast<const __attribute__((address_space(3))) uint8_t*>((uintptr_t)(at + 16 * kCodes4 + lane * 4 + (lane & 3)));
+      if (group && !full(t, b, it.cached + tok0)) {
+        const bool odd = byte > uint32_t(Four<T>::kMost);
+        if (__ballot(odd)) {
+          if (odd) {
+            e = u32x4_t{0u, 0u, 0u, 0u};
+            byte = Four<T>::kLeast;
+          }
+          odd_lo = min(odd_lo, t);
+          odd_hi = t;
+        }
+      }
+      const float scale = scale_of(byte);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t x[4];
+        values_of<T>(e[j], scale, x);
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4_t*>((uintptr_t)((write4 ^ j << 4) + slot(t))) = u32x4_t{x[0], x[1], x[2], x[3]};
+      }
+    };
     // (the 32-key blocks in turn: a product does not wait for the one before it)
     auto read_k = [&](uint32_t at, int i) {  // keys 32 (i & 1) .., dimensions 16 (i >> 1) .. (at: k_lane + slot)
       return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)((at ^ (i >> 1 << 5)) + (i & 1) * 8192));
@@ -620,22 +662,35 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));
       // K(t0), K(t0+1), K(t0+2) and V(t0), V(t0+1); then a step fetches one of each
-      uint32_t bad = 0;  // bad 16-key groups of tiles t, t + 1, ..: four bits each
+      std::conditional_t<FOUR, uint64_t, uint32_t> bad = 0;  // bad 16-key groups of tiles t, t + 1, ..: four bits each
+      if constexpr (FOUR) {
+        for (int i = 0; i < kAhead4; ++i) bad |= fetch4(t0 + i) << (4 * (i + 1));
+        convert4(t0, (bad >> 4) & 15);
+        bad |= fetch4(t0 + kAhead4) << (4 * (kAhead4 + 1));
+      } else {
 #pragma unroll
-      for (int i = 0; i < kRing - 1; ++i)
-        if (i < kRing - 1 - group) bad |= fetch(t0 + i) << (4 * (i + 1));
-      wait_vmcnt<2 * kTileLoads>();
+        for (int i = 0; i < kRing - 1; ++i)
+          if (i < kRing - 1 - group) bad |= fetch(t0 + i) << (4 * (i + 1));
+        wait_vmcnt<2 * kTileLoads>();
+      }
       barrier_lds();
       if (group) barrier_lds();
       // What ends the products of step t: this wave's part of the tiles of step t + 1.
       auto landed = [&](int32_t t) {
-        wait_vmcnt<kTileLoads>();
-        if (group && t + 1 < t1 && !full(t + 1, (bad >> 4) & 15, it.cached + tok0)) clean_values(t + 1);
+        if constexpr (!FOUR) {
+          wait_vmcnt<kTileLoads>();
+          if (group && t + 1 < t1 && !full(t + 1, (bad >> 4) & 15, it.cached + tok0)) clean_values(t + 1);
+        }
         barrier_lds();
       };
       auto vector_half = [&](int32_t t) {
         if (t < t_last) weigh(t + 1, (bad >> 4) & 15);
-        bad = (bad | (fetch(t + kRing - group) << (4 * (kRing - group)))) >> 4;
+        if constexpr (FOUR) {
+          convert4(t + 2, (bad >> 8) & 15);
+          bad = (bad | (fetch4(t + 2 + kAhead4) << (4 * (kAhead4 + 2)))) >> 4;
+        } else {
+          bad = (bad | (fetch(t + kRing - group) << (4 * (kRing - group)))) >> 4;
+        }
         barrier_lds();
       };
       if (t0 <= t_last) {
@@ -669,6 +724,17 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     for (int32_t key = odd_lo * kPagedTile; key < min((odd_hi + 1) * kPagedTile, seen); ++key) {
       pages.seek(key >> c.page_shift);
       if (pages.is_bad(key >> c.page_shift)) continue;
+      if constexpr (FOUR) {
+        const uint8_t* p = reinterpret_cast<const uint8_t*>(c.v) + page4(c, unit, pages.page(key >> c.page_shift));
+        const uint32_t scales = *reinterpret_cast<const uint32_t*>(p + (in_page + 1) * kCodes4 + (key & in_page) * 4);
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+          const float x = (scales >> (8 * db) & 255u) > uint32_t(Four<T>::kMost) && key <= limit ? __builtin_nanf("") : 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] += x;
+        }
+        continue;
+      }
       const uint16_t* vr = c.v + (page_row(c, unit, pages.page(key >> c.page_shift)) + (key & in_page)) * kHeadDim + 4 * h;
 #pragma unroll
       for (int db = 0; db < 4; ++db)
@@ -867,9 +933,9 @@ hipError_t decode(const PagedAttnArgs& a, hipStream_t stream) {
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }
 
-template <typename T>
+template <typename T, bool FOUR>
 hipError_t extend(const PagedAttnArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_extend_kernel<T>), dim3(a.shares), dim3(kExtWaves * 64), 0, stream, a);
+  hipLaunchKernelGGL((paged_extend_kernel<T, FOUR>), dim3(a.shares), dim3(kExtWaves * 64), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_join<T>(a, stream);
 }
@@ -880,8 +946,13 @@ hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t st
   return half ? decode<_Float16>(a, stream) : decode<__bf16>(a, stream);
 }
 
-hipError_t launch_paged_extend(const PagedAttnArgs& a, bool half, hipStream_t stream) {
-  return half ? extend<_Float16>(a, stream) : extend<__bf16>(a, stream);
+hipError_t launch_paged_extend(const PagedAttnArgs& a, bool four, bool half, hipStream_t stream) {
+  if (four) return half ? extend<_Float16, true>(a, stream) : extend<__bf16, true>(a, stream);
+  return half ? extend<_Float16, false>(a, stream) : extend<__bf16, false>(a, stream);
+}
+
+hipError_t launch_paged_join(const PagedAttnArgs& a, bool half, hipStream_t stream) {
+  return half ? launch_join<_Float16>(a, stream) : launch_join<__bf16>(a, stream);
 }
 
 }  // namespace stlite

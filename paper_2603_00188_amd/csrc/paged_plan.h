@@ -176,4 +176,29 @@ struct PagedPlan {
   }
 };
 
+// The page table of one sequence as a wave reads it: 64 entries in a register,
+// one per lane, fetched by index without a memory access.
+struct PageWindow {
+  const int32_t* row;
+  int32_t n_pages, last;  // last: index of the row's last entry
+  int32_t base;           // first entry held
+  int32_t held;           // this lane's entry
+  uint64_t bad;           // entries out of range
+
+  __device__ PageWindow(const PagedDev& c, int32_t seq)
+      : row(c.page_table + int64_t(seq) * c.max_pages), n_pages(c.n_pages), last(c.max_pages - 1), base(-1), held(0), bad(0) {}
+
+  // Makes the window hold `entry` (wave-uniform).
+  __device__ void seek(int32_t entry) {
+    if ((entry & ~63) == base) return;
+    base = entry & ~63;
+    const int32_t e = row[min(base + int32_t(threadIdx.x & 63), last)];
+    const bool ok = e >= 0 && e < n_pages;
+    held = ok ? e : 0;
+    bad = __ballot(!ok);
+  }
+  __device__ int32_t page(int32_t entry) const { return __builtin_amdgcn_readlane(held, entry & 63); }
+  __device__ bool is_bad(int32_t entry) const { return (bad >> (entry & 63)) & 1; }
+};
+
 }  // namespace stlite

@@ -1,6 +1,6 @@
 // Rows into a paged cache: the compression's kept rows (a gather, as the dense
 // compaction) and the new tokens of a serving step (norm and rotation on the way).
-#include "paged.h"
+#include "paged4.h"
 #include "tile_lds.h"
 
 namespace stlite {
@@ -75,6 +75,139 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) 
   }
 }
 
+// v of lane ^ M as bits.
+template <int M>
+__device__ __forceinline__ uint32_t lane_xor_bits(uint32_t v) {
+  return __float_as_uint(lane_xor<M>(__uint_as_float(v)));
+}
+
+// Kept rows into the pages of a 4-bit pool: the same walk, sixteen lanes to a row.  Four
+// lanes hold a block: its greatest magnitude by two exchanges, then 4 bytes of codes each;
+// the row's four scale bytes meet in one lane.  The codes of consecutive rows are
+// contiguous, and are left to the caches, which put a page's lines together.
+template <typename T>
+__global__ __launch_bounds__(256) void paged4_compact_kernel(PagedCompactArgs a) {
+  constexpr int kPer = kRowsPerGroup / 16;
+  const int unit = blockIdx.y;
+  const int64_t j0 = int64_t(blockIdx.x) * kRowsPerGroup;
+  const int sub = threadIdx.x >> 4, part = threadIdx.x & 15;
+  const int64_t ubase = int64_t(unit) * a.total_tokens;
+  if (blockIdx.x == 0 && unit == 0)
+    for (int32_t s = threadIdx.x; s < a.c.n_seqs; s += 256) a.c.seq_lens[s] = a.cu_budget[s + 1] - a.cu_budget[s];
+  if (a.total_budget == 0) return;
+  const int64_t kbase = int64_t(a.kept_per_layer ? unit / a.c.n_kv_heads : unit) * a.total_budget;
+  const int32_t in_page = (1 << a.c.page_shift) - 1;
+  u32x4_t rows[2][kPer];
+  int64_t page_at[kPer];  // first byte of the page, or -1
+  int32_t row_at[kPer];
+#pragma unroll
+  for (int r = 0; r < kPer; ++r) {
+    const int64_t j = j0 + r * 16 + sub;
+    int32_t tok = -1;
+    page_at[r] = -1;
+    row_at[r] = 0;
+    if (j < a.total_budget) {
+      tok = a.kept[kbase + j];
+      const int32_t s = seq_of(a.cu_budget, a.c.n_seqs, j);
+      const int32_t at = int32_t(j - a.cu_budget[s]);
+      const int32_t entry = at >> a.c.page_shift;
+      const int32_t page = entry < a.c.max_pages ? a.c.page_table[int64_t(s) * a.c.max_pages + entry] : -1;
+      row_at[r] = at & in_page;
+      if (page >= 0 && page < a.c.n_pages) page_at[r] = page4(a.c, unit, page);
+    }
+    const bool ok = tok >= 0 && tok < a.total_tokens;
+    const int64_t src = (ubase + (ok ? tok : 0)) * kHeadDim + part * 8;
+    rows[0][r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.k + src));
+    rows[1][r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.v + src));
+    if (!ok) rows[0][r] = rows[1][r] = u32x4_t{0u, 0u, 0u, 0u};
+  }
+#pragma unroll
+  for (int r = 0; r < kPer; ++r) {
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint32_t w[4] = {rows[kv][r][0], rows[kv][r][1], rows[kv][r][2], rows[kv][r][3]};
+      uint32_t top = top_of(w);
+      top = max(top, lane_xor_bits<1>(top));
+      top = max(top, lane_xor_bits<2>(top));
+      const uint32_t byte = scale_byte<T>(Four<T>::wide(top));
+      const uint32_t code = codes_of<T>(w, byte);
+      uint32_t scales = byte << (8 * (part >> 2));
+      scales |= lane_xor_bits<4>(scales);
+      scales |= lane_xor_bits<8>(scales);
+      if (page_at[r] < 0) continue;
+      uint8_t* p = reinterpret_cast<uint8_t*>(kv ? a.c.v : a.c.k) + page_at[r];
+      *reinterpret_cast<uint32_t*>(p + row_at[r] * kCodes4 + part * 4) = code;
+      if (part == 0) *reinterpret_cast<uint32_t*>(p + (in_page + 1) * kCodes4 + row_at[r] * 4) = scales;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows out of pages
+// ---------------------------------------------------------------------------
+
+// The new tokens' rows, sixteen lanes to a row, a work-group 64 tokens of a unit.
+// HBM-bound, a row's 68 (or 256) bytes in and 256 out; as in the compaction all loads of a
+// thread are under way before its stores.
+template <typename T, bool FOUR>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
+  constexpr int kPer = kRowsPerGroup / 16;
+  const PagedDev& c = a.c;
+  const int unit = blockIdx.y, layer = unit / c.n_kv_heads, head = unit % c.n_kv_heads;
+  const int64_t i0 = (int64_t(blockIdx.z) * gridDim.x + blockIdx.x) * kRowsPerGroup;
+  const int sub = threadIdx.x >> 4, part = threadIdx.x & 15;
+  const int32_t in_page = (1 << c.page_shift) - 1;
+  u32x4_t rows[2][kPer];
+  uint32_t codes[2][kPer], scales[2][kPer];
+#pragma unroll
+  for (int r = 0; r < kPer; ++r) {
+    const int64_t i = i0 + r * 16 + sub;
+    int32_t page = -1, row = 0;
+    if (i < c.total_new) {
+      const int32_t s = seq_of(c.cu_new, c.n_seqs, i);
+      const int64_t at = int64_t(paged_len(c, s)) - c.cu_new[s + 1] + i;
+      if (at >= 0) {
+        page = c.page_table[int64_t(s) * c.max_pages + (at >> c.page_shift)];
+        row = int32_t(at) & in_page;
+      }
+    }
+    const bool ok = page >= 0 && page < c.n_pages;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      if constexpr (FOUR) {
+        codes[kv][r] = scales[kv][r] = 0u;
+        if (!ok) continue;
+        const uint8_t* p = reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + page4(c, unit, page);
+        codes[kv][r] = *reinterpret_cast<const uint32_t*>(p + row * kCodes4 + part * 4);
+        scales[kv][r] = p[(in_page + 1) * kCodes4 + row * 4 + (part >> 2)];
+      } else {
+        rows[kv][r] = u32x4_t{0u, 0u, 0u, 0u};
+        if (ok)
+          rows[kv][r] = __builtin_nontemporal_load(
+              reinterpret_cast<const u32x4_t*>((kv ? c.v : c.k) + (page_row(c, unit, page) + row) * kHeadDim + part * 8));
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kPer; ++r) {
+    const int64_t i = i0 + r * 16 + sub;
+    if (i >= c.total_new) continue;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      uint16_t* out = kv ? a.v_out : a.k_out;
+      if (!out) continue;
+      u32x4_t y = rows[kv][r];
+      if constexpr (FOUR) {
+        uint32_t w[4];
+        values_of<T>(codes[kv][r], scale_of(scales[kv][r]), w);
+        y = u32x4_t{w[0], w[1], w[2], w[3]};
+      }
+      __builtin_nontemporal_store(
+          y, reinterpret_cast<u32x4_t*>(out + ((layer * c.total_new + i) * c.n_kv_heads + head) * kHeadDim + part * 8));
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // New tokens
 // ---------------------------------------------------------------------------
@@ -87,6 +220,112 @@ constexpr int64_t kMaxBlocks = int64_t(1) << 23;  // along x
 // (3136 normed tokens of 28 layers take 298 us; without it 295.5, in 64 bits 310.)
 constexpr float kLeastSum = 0x1p-100f, kMostSum = 0x1p120f, kLeastEps = 0x1p-80f;
 
+// y in fp32 rounded to odd (toward zero, the last bit set where something was cut off): it
+// lies on the same side of every number with fewer bits as y, or is that number as y is.
+__device__ inline float odd32(double y) {
+  const float f = float(y);
+  uint32_t b = __float_as_uint(f);
+  if (double(f) != y) b = (b - (fabs(double(f)) > fabs(y) ? 1u : 0u)) | 1u;
+  return __uint_as_float(b);
+}
+
+template <int M>
+__device__ __forceinline__ double lane_xor64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = lane_xor_bits<M>(uint32_t(u)), hi = lane_xor_bits<M>(uint32_t(u >> 32));
+  return __builtin_bit_cast(double, hi << 32 | lo);
+}
+
+// A key's or a value's row into a 4-bit pool, lane c of its eight with the dimensions
+// 8 c .. and 64 + 8 c ..: blocks c / 4 and 2 + c / 4, four lanes to each.
+template <typename T>
+__device__ __forceinline__ void store4(const PagedAppendArgs& a, bool key, int layer, int h, int64_t slot, u32x4_t lo,
+                                       u32x4_t hi, const double2* cs) {
+  const PagedDev& c = a.c;
+  const int cidx = threadIdx.x & 7;
+  uint32_t code[2], byte[2];
+  if (key && (a.k_norm || a.positions)) {
+    double x[16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = elem_lo<T>(lo[j]);
+      x[2 * j + 1] = elem_hi<T>(lo[j]);
+      x[8 + 2 * j] = elem_lo<T>(hi[j]);
+      x[9 + 2 * j] = elem_hi<T>(hi[j]);
+    }
+    if (a.k_norm) {
+      double ss = 0.0;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) ss = fma(x[j], x[j], ss);
+      ss += lane_xor64<1>(ss);
+      ss += lane_xor64<2>(ss);
+      ss += lane_xor64<4>(ss);
+      const double rs = 1.0 / sqrt(ss * (1.0 / kHeadDim) + double(a.eps));
+      const uint16_t* wl = a.k_norm + layer * kHeadDim + 8 * cidx;
+      const u32x4_t w0 = *reinterpret_cast<const u32x4_t*>(wl), w1 = *reinterpret_cast<const u32x4_t*>(wl + 64);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] *= rs * elem_lo<T>(w0[j]);
+        x[2 * j + 1] *= rs * elem_hi<T>(w0[j]);
+        x[8 + 2 * j] *= rs * elem_lo<T>(w1[j]);
+        x[9 + 2 * j] *= rs * elem_hi<T>(w1[j]);
+      }
+    }
+    if (a.positions) {
+      if (a.interleaved) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const double2 t = cs[4 * cidx + (j & 3) + 32 * (j >> 2)];
+          const double y0 = x[2 * j] * t.x - x[2 * j + 1] * t.y;
+          x[2 * j + 1] = x[2 * j + 1] * t.x + x[2 * j] * t.y;
+          x[2 * j] = y0;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const double2 t = cs[8 * cidx + j];
+          const double y0 = x[j] * t.x - x[8 + j] * t.y;
+          x[8 + j] = x[8 + j] * t.x + x[j] * t.y;
+          x[j] = y0;
+        }
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float y[8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        y[j] = odd32(x[8 * b + j]);
+        top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
+      }
+      top = max(top, lane_xor_bits<1>(top));
+      top = max(top, lane_xor_bits<2>(top));
+      byte[b] = scale_byte<T>(top);
+      code[b] = codes_of(y, byte[b]);
+    }
+  } else {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const u32x4_t e = b ? hi : lo;
+      const uint32_t w[4] = {e[0], e[1], e[2], e[3]};
+      uint32_t top = top_of(w);
+      top = max(top, lane_xor_bits<1>(top));
+      top = max(top, lane_xor_bits<2>(top));
+      byte[b] = scale_byte<T>(Four<T>::wide(top));
+      code[b] = codes_of<T>(w, byte[b]);
+    }
+  }
+  uint32_t scales = (byte[0] | byte[1] << 16) << (8 * (cidx >> 2));
+  scales |= lane_xor_bits<4>(scales);
+  if (slot < 0) return;
+  const int32_t row = int32_t(slot) & ((1 << c.page_shift) - 1);
+  uint8_t* p = reinterpret_cast<uint8_t*>(key ? c.k : c.v) + page4(c, layer * c.n_kv_heads + h, int32_t(slot >> c.page_shift));
+  *reinterpret_cast<uint32_t*>(p + row * kCodes4 + 4 * cidx) = code[0];
+  *reinterpret_cast<uint32_t*>(p + row * kCodes4 + 32 + 4 * cidx) = code[1];
+  if (cidx == 0) *reinterpret_cast<uint32_t*>(p + (kCodes4 << c.page_shift) + row * 4) = scales;
+}
+
 // One (token, layer) by `WAVES` waves.  Eight lanes hold a head: lane c the
 // dimensions 8c .. 8c+7 and 64+8c .. 64+8c+7, so both members of every pair of
 // either pairing lie in one lane.  The 64 (cos, sin) of the token are formed
@@ -96,10 +335,16 @@ constexpr float kLeastSum = 0x1p-100f, kMostSum = 0x1p120f, kLeastEps = 0x1p-80f
 // HBM-bound once there are a few thousand rows: 3136 tokens of 28 layers (1.62 GB read
 // and written) take 298 us, 5.4 TB/s; 64 tokens of 28 layers (44 MB) 12.3 us, 3.6 TB/s,
 // where the chain of dependent loads (sequence, length, page, row) is half of it.
-template <typename T, int WAVES>
+//
+// FOUR: keys and values are stored in 4 bits.  Which code a key gets turns on the side of
+// a border that it lies on, so it is formed in 64 bits, which this card multiplies and adds
+// at the rate of single 32-bit operations, and the token's sines too; on the way to
+// codes it passes through fp32 rounded to odd, which keeps the side.
+template <typename T, int WAVES, bool FOUR>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   constexpr int kTok = 4 / WAVES;  // tokens per work-group
   __shared__ float2 sm_cs[kTok][64];
+  __shared__ double2 sm_cs64[FOUR ? kTok : 1][64];
   const PagedDev& c = a.c;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tl = wave / WAVES, part = wave % WAVES;
@@ -128,8 +373,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   if (a.positions && live && part == 0) {
     const int axis = (lane >= a.axis1) + (lane >= a.axis2);
     const double turn = double(a.positions[axis * c.total_new + tok]) * a.turns[lane];
-    const float r = float(turn - rint(turn));
-    sm_cs[tl][lane] = make_float2(cospif(2.0f * r), sinpif(2.0f * r));
+    if constexpr (FOUR) {
+      double sn, cs;
+      sincospi(2.0 * (turn - rint(turn)), &sn, &cs);
+      sm_cs64[tl][lane] = make_double2(cs, sn);
+      sm_cs[tl][lane] = make_float2(float(cs), float(sn));
+    } else {
+      const float r = float(turn - rint(turn));
+      sm_cs[tl][lane] = make_float2(cospif(2.0f * r), sinpif(2.0f * r));
+    }
   }
   __syncthreads();
   if (!live) return;
@@ -165,6 +417,14 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   for (int r = part * 8 + sub; r < rows; r += 8 * WAVES) {
     const u32x4_t lo = lo_next, hi = hi_next;
     if (r + 8 * WAVES < rows) load(r + 8 * WAVES);
+    if constexpr (FOUR) {
+      if (r >= nq) {  // (the lanes of a head take the same side)
+        const int h = (r - nq) % nk;
+        const bool key = r - nq < nk;
+        store4<T>(a, key, layer, h, slot, lo, hi, sm_cs64[tl]);
+        continue;
+      }
+    }
     uint16_t* dst;
     const uint16_t* w = nullptr;
     bool turn = a.positions != nullptr;
@@ -256,14 +516,36 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
 
 }  // namespace
 
-hipError_t launch_paged_compact(const PagedCompactArgs& a, hipStream_t stream) {
+hipError_t launch_paged_compact(const PagedCompactArgs& a, bool four, bool half, hipStream_t stream) {
   // (one work-group for the lengths where nothing is kept)
   const int64_t blocks = a.total_budget > 0 ? (a.total_budget + kRowsPerGroup - 1) / kRowsPerGroup : 1;
-  hipLaunchKernelGGL(paged_compact_kernel, dim3(uint32_t(blocks), a.c.n_units), dim3(256), 0, stream, a);
+  const dim3 grid(uint32_t(blocks), a.c.n_units);
+  if (!four) hipLaunchKernelGGL(paged_compact_kernel, grid, dim3(256), 0, stream, a);
+  else if (half) hipLaunchKernelGGL((paged4_compact_kernel<_Float16>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged4_compact_kernel<__bf16>), grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
-hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t stream) {
+hipError_t launch_paged_read(const PagedReadArgs& a, bool four, bool half, hipStream_t stream) {
+  const int64_t blocks = (a.c.total_new + kRowsPerGroup - 1) / kRowsPerGroup, x = blocks < kMaxBlocks ? blocks : kMaxBlocks;
+  const dim3 grid(uint32_t(x), a.c.n_units, uint32_t((blocks + x - 1) / x));
+  if (!four) hipLaunchKernelGGL((paged_read_kernel<__bf16, false>), grid, dim3(256), 0, stream, a);
+  else if (half) hipLaunchKernelGGL((paged_read_kernel<_Float16, true>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_read_kernel<__bf16, true>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+namespace {
+
+template <typename T, bool FOUR>
+void append(const PagedAppendArgs& a, bool few, dim3 grid, hipStream_t stream) {
+  if (few) hipLaunchKernelGGL((paged_append_kernel<T, 4, FOUR>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_append_kernel<T, 1, FOUR>), grid, dim3(256), 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedAppendArgs& a, bool four, bool half, hipStream_t stream) {
   // Few (token, layer) pairs: four waves each, for their latency; else a wave each, which
   // forms the angles once.  28 query heads, a wave / four waves each: 1 pair 4.7 / 3.4 us,
   // 448 pairs 6.0 / 4.7, 1024 pairs 6.9 / 5.9, 1792 pairs 9.2 / 10.1, 4096 pairs 14.3 /
@@ -273,13 +555,8 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, bool half, hipStream_t 
   // along z.
   const int64_t blocks = (a.c.total_new + (few ? 0 : 3)) / (few ? 1 : 4), x = blocks < kMaxBlocks ? blocks : kMaxBlocks;
   const dim3 grid(uint32_t(x), a.c.n_layers, uint32_t((blocks + x - 1) / x));
-  if (half) {
-    if (few) hipLaunchKernelGGL((paged_append_kernel<_Float16, 4>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged_append_kernel<_Float16, 1>), grid, dim3(256), 0, stream, a);
-  } else {
-    if (few) hipLaunchKernelGGL((paged_append_kernel<__bf16, 4>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged_append_kernel<__bf16, 1>), grid, dim3(256), 0, stream, a);
-  }
+  if (four) half ? append<_Float16, true>(a, few, grid, stream) : append<__bf16, true>(a, few, grid, stream);
+  else half ? append<_Float16, false>(a, few, grid, stream) : append<__bf16, false>(a, few, grid, stream);
   return hipGetLastError();
 }
 

@@ -7,6 +7,9 @@
     q = paged_append(cache, step, q, k, v, positions, rope)
     o = paged_attention(cache, step, q)
 
+A cache may hold its keys and values in 4 bits: ``PagedCache.alloc(..., bits=4)``, or uint8 tensors.  The same calls
+store and read it; ``paged_read`` gives rows back in 16 bits.
+
 As in ``stlite``, every function only checks and marshals its arguments; all
 arithmetic runs in the library's gfx950 kernels.  Tensors are bf16 or fp16, of
 the pool's type and on its device.  Everything runs on ``stream`` (the device's
@@ -29,7 +32,9 @@ import torch
 from .stlite import _CPaged, _CRope, _CRows, _check, load
 
 HEAD_DIM = 128
+ROW4 = 68  # bytes of a row in a 4-bit pool: 64 of codes, 4 scales
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_KV4 = 16
 
 
 def _is(t, name, shape, dtype, device):
@@ -138,16 +143,28 @@ class PagedCache(_Fixed):
     """A pool of pages [n_layers][n_kv_heads][n_pages][page_size][128], the sequences' page table
     [n_seqs][max_pages] int32 and their lengths [n_seqs] int32.  ``max_len``: no sequence grows longer.
 
+    With k and v of uint8, [n_layers][n_kv_heads][n_pages][page_size * 68], the pool holds 4 bits (a page's rows of 64
+    bytes of codes, then its rows of 4 scale bytes) and ``dtype`` is the 16-bit type of the calls' other tensors.
+
     The tensors are the cache's for good (a captured graph and the caches of single layers hold them too): other
     lengths or pages are written into them, ``cache.seq_lens.copy_(lens)``."""
 
     _fixed = ("k", "v", "page_table", "seq_lens", "tensors", "n_layers", "n_q_heads", "n_kv_heads", "n_pages", "page_size",
-              "n_seqs", "max_pages", "max_len", "dtype", "device", "_c")
+              "n_seqs", "max_pages", "max_len", "dtype", "bits", "device", "_c")
 
-    def __init__(self, k, v, page_table, seq_lens, n_q_heads: int, max_len: Optional[int] = None):
-        if k.dim() != 5 or k.shape[4] != HEAD_DIM or k.dtype not in _DTYPES:
+    def __init__(self, k, v, page_table, seq_lens, n_q_heads: int, max_len: Optional[int] = None, dtype=None):
+        four = k.dtype == torch.uint8
+        if four:
+            if k.dim() != 4 or k.shape[3] % ROW4 or not k.shape[3]:
+                raise ValueError(f"k must be [n_layers, n_kv_heads, n_pages, page_size * {ROW4}] uint8, got {tuple(k.shape)}")
+            dtype = torch.bfloat16 if dtype is None else dtype
+            if dtype not in _DTYPES:
+                raise ValueError(f"dtype must be torch.bfloat16 or torch.float16, got {dtype}")
+        elif k.dim() != 5 or k.shape[4] != HEAD_DIM or k.dtype not in _DTYPES:
             raise ValueError(f"k must be [n_layers, n_kv_heads, n_pages, page_size, {HEAD_DIM}] bf16 or fp16, got "
                              f"{k.dtype} {tuple(k.shape)}")
+        elif dtype not in (None, k.dtype):
+            raise ValueError(f"dtype {dtype} of a pool of {k.dtype}")
         if page_table.dim() != 2:
             raise ValueError("page_table must be [n_seqs, max_pages]")
         _is(k, "k", k.shape, k.dtype, k.device)
@@ -155,35 +172,40 @@ class PagedCache(_Fixed):
         _is(page_table, "page_table", page_table.shape, torch.int32, k.device)
         _is(seq_lens, "seq_lens", page_table.shape[:1], torch.int32, k.device)
         self.k, self.v, self.page_table, self.seq_lens = self.tensors = k, v, page_table, seq_lens
-        self.n_layers, self.n_kv_heads, self.n_pages, self.page_size = k.shape[:4]
+        self.n_layers, self.n_kv_heads, self.n_pages = k.shape[:3]
+        self.page_size, self.bits = (k.shape[3] // ROW4, 4) if four else (k.shape[3], 16)
         self.n_seqs, self.max_pages = page_table.shape
-        self.n_q_heads, self.dtype, self.device = int(n_q_heads), k.dtype, k.device
+        self.n_q_heads, self.dtype, self.device = int(n_q_heads), dtype if four else k.dtype, k.device
         self.max_len = self.max_pages * self.page_size if max_len is None else int(max_len)
         for name in ("n_q_heads", "max_len", "n_pages", "max_pages", "n_seqs"):
             if not -2 ** 31 <= getattr(self, name) < 2 ** 31:  # (ctypes would cut it)
                 raise ValueError(f"{name} {getattr(self, name)} does not fit in 32 bits")
-        self._c = _CPaged(self.n_layers, self.n_q_heads, self.n_kv_heads, HEAD_DIM, _DTYPES[k.dtype], self.page_size,
+        self._c = _CPaged(self.n_layers, self.n_q_heads, self.n_kv_heads, HEAD_DIM,
+                          _DTYPES[self.dtype] | (_KV4 if four else 0), self.page_size,
                           self.n_pages, self.n_seqs, self.max_pages, self.max_len, 0, k.data_ptr(), v.data_ptr(),
                           page_table.data_ptr(), seq_lens.data_ptr(), None, None)
 
     def __reduce__(self):  # a copy has addresses of its own
-        return PagedCache, (self.k, self.v, self.page_table, self.seq_lens, self.n_q_heads, self.max_len)
+        return PagedCache, (self.k, self.v, self.page_table, self.seq_lens, self.n_q_heads, self.max_len, self.dtype)
 
     @classmethod
     def alloc(cls, n_layers: int, n_q_heads: int, n_kv_heads: int, n_seqs: int, max_len: int, page_size: int = 64,
-              dtype=torch.bfloat16, device="cuda"):
+              dtype=torch.bfloat16, device="cuda", bits: int = 16):
         """A zeroed pool with room for every sequence: sequence s owns the pages s * max_pages .. of it."""
+        if bits not in (4, 16):
+            raise ValueError(f"bits must be 4 or 16, got {bits}")
         pages = -(-max_len // page_size)
-        pool = [torch.zeros((n_layers, n_kv_heads, n_seqs * pages, page_size, HEAD_DIM), dtype=dtype, device=device)
-                for _ in range(2)]
+        row, kind = ((page_size * ROW4,), torch.uint8) if bits == 4 else ((page_size, HEAD_DIM), dtype)
+        pool = [torch.zeros((n_layers, n_kv_heads, n_seqs * pages, *row), dtype=kind, device=device) for _ in range(2)]
         table = torch.arange(n_seqs * pages, dtype=torch.int32, device=device).view(n_seqs, pages)
-        return cls(*pool, table, torch.zeros(n_seqs, dtype=torch.int32, device=device), n_q_heads, max_len)
+        return cls(*pool, table, torch.zeros(n_seqs, dtype=torch.int32, device=device), n_q_heads, max_len, dtype)
 
     def layer(self, i: int) -> "PagedCache":
         """Layer i alone, on the same pages and lengths: what a model's layer loop appends to and attends over."""
         if not 0 <= i < self.n_layers:
             raise ValueError(f"layer {i} of {self.n_layers}")
-        return PagedCache(self.k[i:i + 1], self.v[i:i + 1], self.page_table, self.seq_lens, self.n_q_heads, self.max_len)
+        return PagedCache(self.k[i:i + 1], self.v[i:i + 1], self.page_table, self.seq_lens, self.n_q_heads, self.max_len,
+                          self.dtype)
 
     def _struct(self, batch: Optional[NewTokens]):
         c = _CPaged.from_buffer_copy(self._c)
@@ -327,3 +349,21 @@ def paged_attention(cache: PagedCache, batch: NewTokens, q, out=None, workspace=
                                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), on.handle),
                "stlite_paged_attention")
     return out
+
+
+def paged_read(cache: PagedCache, batch: NewTokens, k_out=None, v_out=None, stream=None):
+    """The new tokens' rows out of the pages: (k, v), [n_layers, total_new, n_kv_heads, 128] in cache.dtype.
+
+    A batch of the prefix sums of the lengths reads whole sequences."""
+    shape = (cache.n_layers, batch.total, cache.n_kv_heads, HEAD_DIM)
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is not None:
+            _is(t, name, shape, cache.dtype, cache.device)
+    with _On(cache.device, stream) as on:
+        k_out = on.new(shape, cache.dtype) if k_out is None else k_out
+        v_out = on.new(shape, cache.dtype) if v_out is None else v_out
+        if not on.own:
+            on.keep(k_out, v_out, batch.d, *cache.tensors)
+        _check(load().stlite_paged_read(ctypes.byref(cache._struct(batch)), k_out.data_ptr(), v_out.data_ptr(), on.handle),
+               "stlite_paged_read")
+    return k_out, v_out

@@ -30,7 +30,7 @@ EXPORTS = (
     "stlite_layer_mean", "stlite_tsg_rho_concat", "stlite_css_saliency_concat", "stlite_compact_kv_layer",
     "stlite_select_topk_noalloc", "stlite_mean_attention",
     "stlite_paged_validate", "stlite_paged_workspace_size", "stlite_paged_compact", "stlite_paged_append",
-    "stlite_paged_attention",
+    "stlite_paged_attention", "stlite_paged_read",
 )
 
 
@@ -120,6 +120,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "stlite_paged_compact": (st, [P, C, vp, vp, vp, ctypes.c_int32, vp]),
         "stlite_paged_append": (st, [C, ctypes.POINTER(_CRope), vp, R, R, R, vp, vp, f32, vp, vp]),
         "stlite_paged_attention": (st, [C, vp, f32, vp, vp, sz, vp]),
+        "stlite_paged_read": (st, [C, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
