@@ -89,7 +89,7 @@ hipError_t launch_paged_compact(const PagedCompactArgs& a, bool four, bool half,
 hipError_t launch_paged_read(const PagedReadArgs& a, bool four, bool half, hipStream_t stream);
 hipError_t launch_paged_append(const PagedAppendArgs& a, bool four, bool half, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
-hipError_t launch_paged4_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
+hipError_t launch_paged4_few(const PagedAttnArgs& a, bool half, hipStream_t stream);
 hipError_t launch_paged_extend(const PagedAttnArgs& a, bool four, bool half, hipStream_t stream);
 hipError_t launch_paged_join(const PagedAttnArgs& a, bool half, hipStream_t stream);
 

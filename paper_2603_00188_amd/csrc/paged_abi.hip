@@ -132,7 +132,7 @@ PagedDev device_view(const stlite_paged* c) {
 // / 743 us, a step 265 / 270 / 274, a long cache 64.6 / 63.8 / 67.5).  One token by the
 // several-token kernel: 18 us for 11, 72 for 64, 309 for 270, 806 for 729.
 struct AttnPlan {
-  bool decode;
+  bool decode;  // by the kernel of few rows
   int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows, join_groups, join_split;
   size_t bytes;
 };
@@ -146,12 +146,12 @@ AttnPlan attn_plan(const stlite_paged* c) {
     most = std::max(most, n);
     live += n > 0;
   }
-  p.decode = most <= 1;
+  p.decode = most <= 1 || (is_four(c) && most * group <= 32);
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
   if (p.decode) {
-    p.rows = group <= 16 ? 16 : 32;
+    p.tokens = int32_t(std::max<int64_t>(most, 1));
+    p.rows = p.tokens * group <= 16 ? 16 : 32;
     p.parts = int32_t(ceil_div(group, p.rows));
-    p.tokens = 1;
     p.shares = 512;
     p.min_share = 64;
     p.item_cost = 64;
@@ -179,7 +179,7 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // boundary / by item: one token behind 3 sequences of up to 79079 in 2 units 63.8 / 45.6
   // us, 4 of up to 6000 in 4 units 28.0 / 21.4, two layers of one behind 8000 24.2 / 18.4;
   // 16 of up to 1000 in 4 units 19.0 / 24.0, five drafted tokens in 16 in 8 62 / 65.
-  const int64_t item_rows = p.decode ? std::min<int64_t>(group, p.rows) : std::min<int64_t>(p.tokens, most) * group;
+  const int64_t item_rows = std::min<int64_t>(std::min<int64_t>(p.tokens, most) * group, p.rows);
   p.join_items = items < p.shares && item_rows * p.shares >= 128 * items ? int32_t(items) : 0;
   p.join_rows = p.join_items ? int32_t(ceil_div(items * item_rows, 512)) : int32_t(item_rows);
   // A boundary's work-group has 256 threads where that is few rounds of loads too, so that
@@ -419,7 +419,7 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   const bool four = is_four(c), half = is_half(c);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   return hip_status(!p.decode ? launch_paged_extend(a, four, half, s)
-                    : four    ? launch_paged4_decode(a, half, s)
+                    : four    ? launch_paged4_few(a, half, s)
                               : launch_paged_decode(a, half, s),
                     "paged_attention launch");
 }

@@ -146,66 +146,55 @@ __global__ __launch_bounds__(256) void paged4_compact_kernel(PagedCompactArgs a)
 // Rows out of pages
 // ---------------------------------------------------------------------------
 
-// The new tokens' rows, sixteen lanes to a row, a work-group 64 tokens of a unit.
-// HBM-bound, a row's 68 (or 256) bytes in and 256 out; as in the compaction all loads of a
-// thread are under way before its stores.
+constexpr int kReadRows = 16;
+
+// The new tokens' rows, sixteen lanes to a row, a work-group 16 rows in the output's order
+// (a token's heads one after another), so that what it writes is contiguous.
+// HBM-bound, a row's 68 (or 256) bytes in and 256 out: 30105 tokens of 112 units in 4 bits
+// take 545 us, 4.0 TB/s, most of it written.  (In a unit's order, whose writes are 256
+// bytes apart, 584; with 32, 64, 128 rows to a work-group 559, 559, 582; with stores that
+// go through the caches 588.)
 template <typename T, bool FOUR>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
-  constexpr int kPer = kRowsPerGroup / 16;
   const PagedDev& c = a.c;
-  const int unit = blockIdx.y, layer = unit / c.n_kv_heads, head = unit % c.n_kv_heads;
-  const int64_t i0 = (int64_t(blockIdx.z) * gridDim.x + blockIdx.x) * kRowsPerGroup;
-  const int sub = threadIdx.x >> 4, part = threadIdx.x & 15;
+  const int layer = blockIdx.y;
+  const int64_t n = c.total_new * c.n_kv_heads;
+  const int64_t i = (int64_t(blockIdx.z) * gridDim.x + blockIdx.x) * kReadRows + (threadIdx.x >> 4), tok = i / c.n_kv_heads;
+  if (i >= n) return;
+  const int part = threadIdx.x & 15, unit = layer * c.n_kv_heads + int(i - tok * c.n_kv_heads);
   const int32_t in_page = (1 << c.page_shift) - 1;
-  u32x4_t rows[2][kPer];
-  uint32_t codes[2][kPer], scales[2][kPer];
+  int32_t page = -1, row = 0;
+  const int32_t s = seq_of(c.cu_new, c.n_seqs, tok);
+  const int64_t at = int64_t(paged_len(c, s)) - c.cu_new[s + 1] + tok;
+  if (at >= 0) {
+    page = c.page_table[int64_t(s) * c.max_pages + (at >> c.page_shift)];
+    row = int32_t(at) & in_page;
+  }
+  u32x4_t rows[2] = {u32x4_t{0u, 0u, 0u, 0u}, u32x4_t{0u, 0u, 0u, 0u}};
+  if (page >= 0 && page < c.n_pages) {
+    if constexpr (FOUR) {
+      uint32_t codes[2], scales[2];
 #pragma unroll
-  for (int r = 0; r < kPer; ++r) {
-    const int64_t i = i0 + r * 16 + sub;
-    int32_t page = -1, row = 0;
-    if (i < c.total_new) {
-      const int32_t s = seq_of(c.cu_new, c.n_seqs, i);
-      const int64_t at = int64_t(paged_len(c, s)) - c.cu_new[s + 1] + i;
-      if (at >= 0) {
-        page = c.page_table[int64_t(s) * c.max_pages + (at >> c.page_shift)];
-        row = int32_t(at) & in_page;
-      }
-    }
-    const bool ok = page >= 0 && page < c.n_pages;
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      if constexpr (FOUR) {
-        codes[kv][r] = scales[kv][r] = 0u;
-        if (!ok) continue;
+      for (int kv = 0; kv < 2; ++kv) {
         const uint8_t* p = reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + page4(c, unit, page);
-        codes[kv][r] = *reinterpret_cast<const uint32_t*>(p + row * kCodes4 + part * 4);
-        scales[kv][r] = p[(in_page + 1) * kCodes4 + row * 4 + (part >> 2)];
-      } else {
-        rows[kv][r] = u32x4_t{0u, 0u, 0u, 0u};
-        if (ok)
-          rows[kv][r] = __builtin_nontemporal_load(
-              reinterpret_cast<const u32x4_t*>((kv ? c.v : c.k) + (page_row(c, unit, page) + row) * kHeadDim + part * 8));
+        codes[kv] = *reinterpret_cast<const uint32_t*>(p + row * kCodes4 + part * 4);
+        scales[kv] = p[(in_page + 1) * kCodes4 + row * 4 + (part >> 2)];
       }
-    }
-  }
 #pragma unroll
-  for (int r = 0; r < kPer; ++r) {
-    const int64_t i = i0 + r * 16 + sub;
-    if (i >= c.total_new) continue;
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      uint16_t* out = kv ? a.v_out : a.k_out;
-      if (!out) continue;
-      u32x4_t y = rows[kv][r];
-      if constexpr (FOUR) {
+      for (int kv = 0; kv < 2; ++kv) {
         uint32_t w[4];
-        values_of<T>(codes[kv][r], scale_of(scales[kv][r]), w);
-        y = u32x4_t{w[0], w[1], w[2], w[3]};
+        values_of<T>(codes[kv], scale_of(scales[kv]), w);
+        rows[kv] = u32x4_t{w[0], w[1], w[2], w[3]};
       }
-      __builtin_nontemporal_store(
-          y, reinterpret_cast<u32x4_t*>(out + ((layer * c.total_new + i) * c.n_kv_heads + head) * kHeadDim + part * 8));
+    } else {
+      const int64_t from = (page_row(c, unit, page) + row) * kHeadDim + part * 8;
+      rows[0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(c.k + from));
+      rows[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(c.v + from));
     }
   }
+  const int64_t to = (layer * n + i) * kHeadDim + part * 8;
+  if (a.k_out) __builtin_nontemporal_store(rows[0], reinterpret_cast<u32x4_t*>(a.k_out + to));
+  if (a.v_out) __builtin_nontemporal_store(rows[1], reinterpret_cast<u32x4_t*>(a.v_out + to));
 }
 
 // ---------------------------------------------------------------------------
@@ -527,8 +516,9 @@ hipError_t launch_paged_compact(const PagedCompactArgs& a, bool four, bool half,
 }
 
 hipError_t launch_paged_read(const PagedReadArgs& a, bool four, bool half, hipStream_t stream) {
-  const int64_t blocks = (a.c.total_new + kRowsPerGroup - 1) / kRowsPerGroup, x = blocks < kMaxBlocks ? blocks : kMaxBlocks;
-  const dim3 grid(uint32_t(x), a.c.n_units, uint32_t((blocks + x - 1) / x));
+  const int64_t blocks = (a.c.total_new * a.c.n_kv_heads + kReadRows - 1) / kReadRows;
+  const int64_t x = blocks < kMaxBlocks ? blocks : kMaxBlocks;
+  const dim3 grid(uint32_t(x), a.c.n_layers, uint32_t((blocks + x - 1) / x));
   if (!four) hipLaunchKernelGGL((paged_read_kernel<__bf16, false>), grid, dim3(256), 0, stream, a);
   else if (half) hipLaunchKernelGGL((paged_read_kernel<_Float16, true>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((paged_read_kernel<__bf16, true>), grid, dim3(256), 0, stream, a);
