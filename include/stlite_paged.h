@@ -206,6 +206,90 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
  */
 stlite_status stlite_paged_read(const stlite_paged* c, uint16_t* k_out, uint16_t* v_out, void* stream);
 
+/*
+ * The free pages of a pool, on the device: pages[0 .. n_free) are those that no sequence
+ * holds (the next one to be given out is the last), and held[s] counts the entries of
+ * page_table's row s, from its first, that sequence s holds a page in.  To begin with:
+ * pages every index of the pool, n_free = n_pages, held and seq_lens 0.  No page may be
+ * in the list and in a row's held entries, or in two rows', at once.
+ */
+typedef struct stlite_free_pages {
+  int32_t* pages;  /* device [n_pages] */
+  int32_t* n_free; /* device [1] */
+  int32_t* held;   /* device [n_seqs] */
+} stlite_free_pages;
+
+/*
+ * Grows every sequence by its new tokens (cu_new): seq_lens[s] += n_s, with pages from the
+ * list behind the held ones where the new length needs more.  Sequences are served in
+ * turn, the lowest first, each wholly or not at all: one whose pages, and those that the
+ * sequences before it ask for, are more than the list has, or whose length would pass
+ * max_len, is PARKED: its length becomes ~len (negative), and its pages stay as they
+ * are.  To every call a parked sequence is an idle slot (length 0): nothing of it is read
+ * or stored, its new tokens' outputs are 0.  It stays parked until a release brings it back.
+ * One that needs no page is not held up by those before it.
+ *   slots  [total_new], nullable: the row of the pool (page * page_size + row in the page)
+ *          of every new token, -1 for a parked sequence's
+ */
+stlite_status stlite_paged_grow(const stlite_paged* c, const stlite_free_pages* pages, int32_t* slots, void* stream);
+
+/*
+ * Gives back the pages behind the sequences' ends; their entries of the page table become
+ * -1.  lens [n_seqs], nullable: sequence s keeps its first min(lens[s], len) tokens, 0 to
+ * end it, and is parked no more; lens[s] < 0, or NULL, leaves its length (a parked one's
+ * pages behind ~len are given back too).  Pages return so that growing again takes the
+ * same ones in the same places.  The new tokens (total_new, cu_new, h_cu_new) are not read.
+ */
+stlite_status stlite_paged_release(const stlite_paged* c, const stlite_free_pages* pages, const int32_t* lens,
+                                   void* stream);
+
+/* Type of the probabilities of stlite_verify_drafts. */
+typedef enum stlite_prob { STLITE_PROB_BF16 = 0, STLITE_PROB_FP16 = 1, STLITE_PROB_FP32 = 2 } stlite_prob;
+
+/*
+ * Drafted tokens of a batch.  Sequence s has n_s = cu_new[s+1] - cu_new[s] rows: row t < n_s
+ * - 1 judges its drafted token t, and the last one follows them all.  (After a call of
+ * attention with n_s new tokens, a sampled one and n_s - 1 drafted ones: its rows.)
+ * Limits: n_seqs <= 65535, vocab <= 2^24, total_new < 2^31.
+ */
+typedef struct stlite_verify {
+  int32_t n_seqs;
+  int32_t vocab;
+  int32_t dtype;          /* stlite_prob, of target and draft */
+  int32_t reserved;       /* must be 0 */
+  int64_t total_new;      /* = cu_new[n_seqs] */
+  const int32_t* cu_new;  /* device [n_seqs+1], cu_new[0] = 0 */
+  const int32_t* h_cu_new;
+  const void* target;     /* device: row i, vocab probabilities, at target + i * target_stride */
+  const void* draft;      /* the same of the draft, at rows of drafted tokens; NULL: it gave each token with certainty */
+  int64_t target_stride;  /* entries, >= vocab */
+  int64_t draft_stride;
+  const int32_t* tokens;  /* device [total_new]: row i's drafted token (a sequence's last row: not read) */
+  const float* accept;    /* device [total_new]: random numbers in [0, 1), one to a drafted token */
+  const float* pick;      /* device [n_seqs]: one to a sequence */
+  int32_t* seq_lens;      /* device [n_seqs], nullable: lengths that count all n_s new tokens */
+} stlite_verify;
+
+stlite_status stlite_verify_workspace_size(const stlite_verify* v, size_t* bytes);
+
+/*
+ * Drafted token x of row i is accepted where accept_i q_i(x) < p_i(x) (draft NULL: q_i(x) =
+ * 1), compared exactly; a token outside [0, vocab) is not.  A sequence's run ends at the
+ * first one that is not, row k, and its next token comes from
+ *   w_j = max(p_k(j) - q_k(j), 0)    (draft NULL: p_k(j), and 0 for the refused token)
+ * or, where all are accepted, from w = p of its last row (and also where the other w are
+ * all 0): the least j with w_0 + .. + w_j > pick (w_0 + .. + w_{vocab-1}), in 64-bit sums;
+ * p need not add up to 1.  Entries of p and q that are negative, infinite or NaN count as
+ * 0; a row without any weight gives -1.
+ *   out    [total_new]: the accepted tokens, the next one, then -1
+ *   n_out  [n_seqs]: accepted tokens + 1; 0 where n_s = 0
+ * seq_lens[s] becomes what is right behind the accepted tokens: n_s - n_out[s] less.  A
+ * negative length (a parked sequence) stays, with n_out 0 and out -1.
+ * out, n_out, seq_lens and the workspace must not overlap one another or an input.
+ */
+stlite_status stlite_verify_drafts(const stlite_verify* v, int32_t* out, int32_t* n_out, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

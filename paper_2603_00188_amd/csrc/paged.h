@@ -35,6 +35,15 @@ struct PagedReadArgs {
   uint16_t* v_out;
 };
 
+struct PagedPagesArgs {
+  PagedDev c;
+  int32_t* free_pages;  // [n_pages]
+  int32_t* n_free;      // [1]
+  int32_t* held;        // [n_seqs]
+  int32_t* slots;       // growing: [total_new], nullable
+  const int32_t* lens;  // releasing: [n_seqs], nullable
+};
+
 struct RowsIn {
   const uint16_t* data;  // nullable (no queries)
   int64_t token_stride, layer_stride;
@@ -91,6 +100,8 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, bool four, bool half, h
 hipError_t launch_paged_decode(const PagedAttnArgs& a, bool half, hipStream_t stream);
 hipError_t launch_paged4_few(const PagedAttnArgs& a, bool half, hipStream_t stream);
 hipError_t launch_paged_extend(const PagedAttnArgs& a, bool four, bool half, hipStream_t stream);
+hipError_t launch_paged_grow(const PagedPagesArgs& a, hipStream_t stream);
+hipError_t launch_paged_release(const PagedPagesArgs& a, hipStream_t stream);
 hipError_t launch_paged_join(const PagedAttnArgs& a, bool half, hipStream_t stream);
 
 // ---------------------------------------------------------------------------

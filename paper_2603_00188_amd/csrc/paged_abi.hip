@@ -11,6 +11,7 @@
 #include "paged4.h"
 #include "stlite.h"
 #include "stlite_paged.h"
+#include "verify.h"
 
 namespace stlite {
 stlite_status report_error(stlite_status st, const char* msg);  // stlite_abi.hip
@@ -229,6 +230,66 @@ bool rows_meet(const stlite_paged* c, const stlite_rows* r, int64_t heads, const
   return false;
 }
 
+// The free pages' arrays, which the calls write: none may be another's or the cache's.
+stlite_status check_pages(const stlite_paged* c, const stlite_free_pages* f, const void* other, size_t other_bytes) {
+  if (!f || !f->pages || !f->n_free || !f->held)
+    return fail(STLITE_ERR_INVALID_ARG, "pages, n_free and held must be non-NULL");
+  const struct {
+    const void* p;
+    size_t bytes;
+  } all[] = {{f->pages, size_t(c->n_pages) * 4},
+             {f->n_free, 4},
+             {f->held, size_t(c->n_seqs) * 4},
+             {c->page_table, size_t(c->n_seqs) * c->max_pages * 4},
+             {c->seq_lens, size_t(c->n_seqs) * 4},
+             {c->cu_new, (size_t(c->n_seqs) + 1) * 4},
+             {other, other_bytes}};
+  for (const auto& x : all) {
+    for (const auto& y : all)
+      if (&x < &y && meet(x.p, x.bytes, y.p, y.bytes))
+        return fail(STLITE_ERR_INVALID_ARG, "the free pages, the page table, the lengths and the call's arrays must not overlap");
+    if (meets_pool(c, x.p, x.bytes))
+      return fail(STLITE_ERR_INVALID_ARG, "the free pages, the page table, the lengths and the call's arrays must not lie in the pool");
+  }
+  return STLITE_OK;
+}
+
+struct VerifyPlan {
+  int32_t chunk, chunks;
+  size_t bytes;
+};
+
+// About 1024 work-groups, 1024 to 8192 entries of a row each.
+VerifyPlan verify_plan(const stlite_verify* v) {
+  const int64_t even = ceil_div(int64_t(v->n_seqs) * v->vocab, 1024);
+  VerifyPlan p;
+  p.chunk = int32_t(std::min<int64_t>(std::max<int64_t>(ceil_div(even, kVerifyMinChunk) * kVerifyMinChunk, kVerifyMinChunk), kVerifyMaxChunk));
+  p.chunks = int32_t(ceil_div(v->vocab, p.chunk));
+  p.bytes = align_up(size_t(v->n_seqs) * p.chunks * sizeof(double2)) + align_up(size_t(v->n_seqs) * sizeof(int32_t));
+  return p;
+}
+
+size_t prob_size(int32_t dtype) { return dtype == STLITE_PROB_FP32 ? 4 : 2; }
+
+stlite_status check_verify(const stlite_verify* v) {
+  if (!v) return fail(STLITE_ERR_INVALID_ARG, "the batch is NULL");
+  if (v->dtype != STLITE_PROB_BF16 && v->dtype != STLITE_PROB_FP16 && v->dtype != STLITE_PROB_FP32)
+    return fail(STLITE_ERR_INVALID_ARG, "dtype must be STLITE_PROB_BF16, _FP16 or _FP32 (got %d)", v->dtype);
+  if (v->reserved != 0) return fail(STLITE_ERR_INVALID_ARG, "reserved field must be 0");
+  if (v->n_seqs < 1) return fail(STLITE_ERR_INVALID_ARG, "n_seqs must be >= 1");
+  if (v->n_seqs > 65535) return fail(STLITE_ERR_UNSUPPORTED, "n_seqs %d: at most 65535 sequences", v->n_seqs);
+  if (v->vocab < 1) return fail(STLITE_ERR_INVALID_ARG, "vocab must be >= 1");
+  if (v->vocab > (1 << 24)) return fail(STLITE_ERR_UNSUPPORTED, "vocab %d: at most 2^24 entries", v->vocab);
+  if (!v->cu_new || !v->h_cu_new) return fail(STLITE_ERR_INVALID_ARG, "cu_new and h_cu_new must be non-NULL");
+  if (v->h_cu_new[0] != 0) return fail(STLITE_ERR_INVALID_ARG, "cu_new[0] must be 0");
+  for (int32_t s = 0; s < v->n_seqs; ++s)
+    if (v->h_cu_new[s + 1] < v->h_cu_new[s])
+      return fail(STLITE_ERR_INVALID_ARG, "sequence %d has %lld rows", s, (long long)v->h_cu_new[s + 1] - v->h_cu_new[s]);
+  if (v->total_new != v->h_cu_new[v->n_seqs])
+    return fail(STLITE_ERR_INVALID_ARG, "total_new %lld != cu_new[n_seqs] %d", (long long)v->total_new, v->h_cu_new[v->n_seqs]);
+  return STLITE_OK;
+}
+
 RowsIn rows_in(const stlite_rows* r) {
   return r ? RowsIn{r->data, r->token_stride, r->layer_stride} : RowsIn{nullptr, 0, 0};
 }
@@ -438,6 +499,101 @@ stlite_status stlite_paged_read(const stlite_paged* c, uint16_t* k_out, uint16_t
   a.k_out = k_out;
   a.v_out = v_out;
   return hip_status(launch_paged_read(a, is_four(c), is_half(c), static_cast<hipStream_t>(stream)), "paged_read launch");
+}
+
+stlite_status stlite_paged_grow(const stlite_paged* c, const stlite_free_pages* pages, int32_t* slots, void* stream) {
+  stlite_status st = check_cache(c, true);
+  if (st == STLITE_OK) st = check_pages(c, pages, slots, size_t(c->total_new) * 4);
+  if (st != STLITE_OK) return st;
+  PagedPagesArgs a{};
+  a.c = device_view(c);
+  a.free_pages = pages->pages;
+  a.n_free = pages->n_free;
+  a.held = pages->held;
+  a.slots = slots;
+  return hip_status(launch_paged_grow(a, static_cast<hipStream_t>(stream)), "paged_grow launch");
+}
+
+stlite_status stlite_paged_release(const stlite_paged* c, const stlite_free_pages* pages, const int32_t* lens, void* stream) {
+  stlite_status st = check_cache(c, false);
+  if (st == STLITE_OK && !c->seq_lens) st = fail(STLITE_ERR_INVALID_ARG, "seq_lens must be non-NULL");
+  if (st == STLITE_OK) st = check_pages(c, pages, lens, size_t(c->n_seqs) * 4);
+  if (st != STLITE_OK) return st;
+  PagedPagesArgs a{};
+  a.c = device_view(c);
+  a.free_pages = pages->pages;
+  a.n_free = pages->n_free;
+  a.held = pages->held;
+  a.lens = lens;
+  return hip_status(launch_paged_release(a, static_cast<hipStream_t>(stream)), "paged_release launch");
+}
+
+stlite_status stlite_verify_workspace_size(const stlite_verify* v, size_t* bytes) {
+  if (!bytes) return fail(STLITE_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = 0;
+  const stlite_status st = check_verify(v);
+  if (st != STLITE_OK) return st;
+  if (v->total_new > 0) *bytes = verify_plan(v).bytes;
+  return ok();
+}
+
+stlite_status stlite_verify_drafts(const stlite_verify* v, int32_t* out, int32_t* n_out, void* ws, size_t ws_bytes, void* stream) {
+  const stlite_status st = check_verify(v);
+  if (st != STLITE_OK) return st;
+  if (!n_out) return fail(STLITE_ERR_INVALID_ARG, "n_out must be non-NULL");
+  if (v->total_new > 0) {
+    if (!v->target || !v->tokens || !v->accept || !v->pick || !out)
+      return fail(STLITE_ERR_INVALID_ARG, "target, tokens, accept, pick and out must be non-NULL");
+    if (v->target_stride < v->vocab || (v->draft && v->draft_stride < v->vocab))
+      return fail(STLITE_ERR_INVALID_ARG, "a row's stride is less than vocab = %d", v->vocab);
+    if (reinterpret_cast<uintptr_t>(v->target) % prob_size(v->dtype) != 0 ||
+        reinterpret_cast<uintptr_t>(v->draft) % prob_size(v->dtype) != 0)
+      return fail(STLITE_ERR_INVALID_ARG, "target and draft must be aligned to their entries");
+  }
+  const VerifyPlan p = verify_plan(v);
+  const size_t need = v->total_new > 0 ? p.bytes : 0;
+  if (need > 0 && !ws) return fail(STLITE_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
+  if (ws_bytes < need) return fail(STLITE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+  if (reinterpret_cast<uintptr_t>(ws) % 256 != 0) return fail(STLITE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const size_t rows = size_t(v->total_new), size = prob_size(v->dtype);
+  const struct {
+    const void* p;
+    size_t bytes;
+    bool written;
+  } all[] = {{out, rows * 4, true},
+             {n_out, size_t(v->n_seqs) * 4, true},
+             {ws, need, true},
+             {v->seq_lens, size_t(v->n_seqs) * 4, true},
+             {v->tokens, rows * 4, false},
+             {v->accept, rows * 4, false},
+             {v->pick, size_t(v->n_seqs) * 4, false},
+             {v->cu_new, (size_t(v->n_seqs) + 1) * 4, false},
+             {v->target, rows ? ((rows - 1) * size_t(v->target_stride) + v->vocab) * size : 0, false},
+             {v->draft, rows ? ((rows - 1) * size_t(v->draft_stride) + v->vocab) * size : 0, false}};
+  for (const auto& x : all)
+    for (const auto& y : all)
+      if (&x != &y && x.written && meet(x.p, x.bytes, y.p, y.bytes))
+        return fail(STLITE_ERR_INVALID_ARG, "out, n_out, seq_lens and the workspace must not overlap one another or an input");
+  VerifyArgs a;
+  a.n_seqs = v->n_seqs;
+  a.vocab = v->vocab;
+  a.total_new = v->total_new;
+  a.cu_new = v->cu_new;
+  a.target = v->target;
+  a.draft = v->draft;
+  a.target_stride = v->target_stride;
+  a.draft_stride = v->draft_stride;
+  a.tokens = v->tokens;
+  a.accept = v->accept;
+  a.pick = v->pick;
+  a.seq_lens = v->seq_lens;
+  a.out = out;
+  a.n_out = n_out;
+  a.sums = static_cast<double2*>(ws);
+  a.stop = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + align_up(size_t(v->n_seqs) * p.chunks * sizeof(double2)));
+  a.chunk = p.chunk;
+  a.chunks = p.chunks;
+  return hip_status(launch_verify(a, v->dtype, static_cast<hipStream_t>(stream)), "verify_drafts launch");
 }
 
 }  // extern "C"

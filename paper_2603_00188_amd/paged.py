@@ -7,6 +7,14 @@
     q = paged_append(cache, step, q, k, v, positions, rope)
     o = paged_attention(cache, step, q)
 
+Sequences that share a pool's pages as they come and go, and that draft tokens, go round
+
+    pages = FreePages.of(cache)                            # all of them free
+    paged_grow(cache, pages, step)                         # lengths, pages for the new tokens
+    q = paged_append(...); o = paged_attention(...)        # -> the target's probabilities
+    tokens, n = verify_drafts(step, p, drafted, accept, pick, draft=q, cache=cache)  # lengths go back to what is right
+    paged_release(cache, pages, lens)                      # sequences that end (0), pages behind the others' ends
+
 A cache may hold its keys and values in 4 bits: ``PagedCache.alloc(..., bits=4)``, or uint8 tensors.  The same calls
 store and read it; ``paged_read`` gives rows back in 16 bits.
 
@@ -29,11 +37,12 @@ from typing import Optional
 import numpy as np
 import torch
 
-from .stlite import _CPaged, _CRope, _CRows, _check, load
+from .stlite import _CFreePages, _CPaged, _CRope, _CRows, _CVerify, _check, load
 
 HEAD_DIM = 128
 ROW4 = 68  # bytes of a row in a 4-bit pool: 64 of codes, 4 scales
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_PROBS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _KV4 = 16
 
 
@@ -190,14 +199,19 @@ class PagedCache(_Fixed):
 
     @classmethod
     def alloc(cls, n_layers: int, n_q_heads: int, n_kv_heads: int, n_seqs: int, max_len: int, page_size: int = 64,
-              dtype=torch.bfloat16, device="cuda", bits: int = 16):
-        """A zeroed pool with room for every sequence: sequence s owns the pages s * max_pages .. of it."""
+              dtype=torch.bfloat16, device="cuda", bits: int = 16, n_pages: Optional[int] = None):
+        """A zeroed pool with room for every sequence: sequence s owns the pages s * max_pages .. of it.  With ``n_pages``,
+        a pool of so many that belong to nobody yet (FreePages.of)."""
         if bits not in (4, 16):
             raise ValueError(f"bits must be 4 or 16, got {bits}")
         pages = -(-max_len // page_size)
         row, kind = ((page_size * ROW4,), torch.uint8) if bits == 4 else ((page_size, HEAD_DIM), dtype)
-        pool = [torch.zeros((n_layers, n_kv_heads, n_seqs * pages, *row), dtype=kind, device=device) for _ in range(2)]
-        table = torch.arange(n_seqs * pages, dtype=torch.int32, device=device).view(n_seqs, pages)
+        pool = [torch.zeros((n_layers, n_kv_heads, n_seqs * pages if n_pages is None else n_pages, *row), dtype=kind,
+                            device=device) for _ in range(2)]
+        if n_pages is None:
+            table = torch.arange(n_seqs * pages, dtype=torch.int32, device=device).view(n_seqs, pages)
+        else:
+            table = torch.full((n_seqs, pages), -1, dtype=torch.int32, device=device)
         return cls(*pool, table, torch.zeros(n_seqs, dtype=torch.int32, device=device), n_q_heads, max_len, dtype)
 
     def layer(self, i: int) -> "PagedCache":
@@ -367,3 +381,132 @@ def paged_read(cache: PagedCache, batch: NewTokens, k_out=None, v_out=None, stre
         _check(load().stlite_paged_read(ctypes.byref(cache._struct(batch)), k_out.data_ptr(), v_out.data_ptr(), on.handle),
                "stlite_paged_read")
     return k_out, v_out
+
+
+class FreePages(_Fixed):
+    """The pages of a pool that no sequence holds: ``pages`` int32 [n_pages], of which the first ``n_free`` [1] are free,
+    and ``held`` [n_seqs], how many entries of its row of the page table each sequence holds."""
+
+    _fixed = ("pages", "n_free", "held", "c")
+
+    def __init__(self, pages, n_free, held):
+        if pages.dim() != 1 or held.dim() != 1:
+            raise ValueError("pages must be [n_pages], held [n_seqs]")
+        _is(pages, "pages", pages.shape, torch.int32, pages.device)
+        _is(n_free, "n_free", (1,), torch.int32, pages.device)
+        _is(held, "held", held.shape, torch.int32, pages.device)
+        self.pages, self.n_free, self.held = pages, n_free, held
+        self.c = _CFreePages(pages.data_ptr(), n_free.data_ptr(), held.data_ptr())
+
+    def __reduce__(self):  # a copy has addresses of its own
+        return FreePages, (self.pages, self.n_free, self.held)
+
+    @classmethod
+    def of(cls, cache: PagedCache) -> "FreePages":
+        """All pages of a cache whose sequences are empty, the lowest to be given out first."""
+        n, dev = cache.n_pages, cache.device
+        return cls(torch.arange(n - 1, -1, -1, dtype=torch.int32, device=dev), torch.tensor([n], dtype=torch.int32, device=dev),
+                   torch.zeros(cache.n_seqs, dtype=torch.int32, device=dev))
+
+    def _for(self, cache):
+        for t, name, shape in ((self.pages, "pages", (cache.n_pages,)), (self.held, "held", (cache.n_seqs,))):
+            if t.shape != shape or t.device != cache.device:
+                raise ValueError(f"the free pages' {name} is {tuple(t.shape)} on {t.device}, the cache's {shape} on {cache.device}")
+        return ctypes.byref(self.c)
+
+
+def paged_grow(cache: PagedCache, pages: FreePages, batch: NewTokens, slots=None, stream=None) -> None:
+    """Every sequence grows by its new tokens, with pages where it needs them; one that cannot is parked (its length
+    becomes ~len).  slots: int32 [total_new], becomes the new tokens' rows of the pool, -1 where there is none."""
+    if slots is not None:
+        _is(slots, "slots", (batch.total,), torch.int32, cache.device)
+    with _On(cache.device, stream) as on:
+        if not on.own:
+            on.keep(slots, batch.d, pages.pages, pages.n_free, pages.held, *cache.tensors)
+        _check(load().stlite_paged_grow(ctypes.byref(cache._struct(batch)), pages._for(cache),
+                                        None if slots is None else slots.data_ptr(), on.handle), "stlite_paged_grow")
+
+
+def paged_release(cache: PagedCache, pages: FreePages, lens=None, stream=None) -> None:
+    """Pages behind the sequences' ends go back.  lens: int32 [n_seqs], what each keeps of its tokens (0: it ends; negative:
+    all of them, and it stays parked if it is)."""
+    if lens is not None:
+        _is(lens, "lens", (cache.n_seqs,), torch.int32, cache.device)
+    with _On(cache.device, stream) as on:
+        if not on.own:
+            on.keep(lens, pages.pages, pages.n_free, pages.held, *cache.tensors)
+        _check(load().stlite_paged_release(ctypes.byref(cache._struct(None)), pages._for(cache),
+                                           None if lens is None else lens.data_ptr(), on.handle), "stlite_paged_release")
+
+
+def _verify(batch: NewTokens, vocab: int, dtype=0) -> _CVerify:
+    if not -2 ** 31 <= vocab < 2 ** 31:
+        raise ValueError(f"vocab {vocab} does not fit in 32 bits")
+    c = _CVerify(n_seqs=len(batch.h) - 1, vocab=vocab, dtype=dtype, total_new=batch.total)
+    c.cu_new, c.h_cu_new = batch._d, batch._h
+    return c
+
+
+def verify_workspace(batch: NewTokens, vocab: int):
+    """Workspace of verify_drafts for this batch.  Calls that share it must be ordered on one stream."""
+    n = ctypes.c_size_t(0)
+    _check(load().stlite_verify_workspace_size(ctypes.byref(_verify(batch, vocab)), ctypes.byref(n)),
+           "stlite_verify_workspace_size")
+    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=batch.d.device)
+
+
+def verify_drafts(batch: NewTokens, target, tokens, accept, pick, draft=None, cache: Optional[PagedCache] = None, out=None,
+                  n_out=None, workspace=None, stream=None):
+    """Which drafted tokens are accepted, and the next one: (out int32 [total_new], n_out int32 [n_seqs]).
+
+    A sequence of n rows in the batch has n - 1 drafted tokens, each judged by its row; the last row follows them.  target:
+    the target's probabilities [total_new, vocab], fp32, bf16 or fp16, any row stride; draft: the draft's, alike, or None
+    where it gave its tokens with certainty; tokens int32 [total_new]; accept fp32 [total_new] and pick fp32 [n_seqs]:
+    random numbers in [0, 1).  out: the accepted tokens, the next one, then -1; n_out: how many that are.  cache: its
+    lengths, which count all rows, go back to what is right."""
+    dev, n, seqs = batch.d.device, batch.total, len(batch.h) - 1
+    if target.dim() != 2 or target.dtype not in _PROBS:
+        raise ValueError(f"target must be [total_new, vocab] fp32, bf16 or fp16, got {target.dtype} {tuple(target.shape)}")
+    vocab = target.shape[1]
+    for t, name in ((target, "target"), (draft, "draft")):
+        if t is None:
+            continue
+        if t.shape != (n, vocab) or t.dtype != target.dtype or t.device != dev:
+            raise ValueError(f"{name} must be {target.dtype} {(n, vocab)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if n and vocab > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: a row's probabilities must lie one after another (strides {t.stride()})")
+        if n > 1 and t.stride(0) < vocab:
+            raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
+    _is(tokens, "tokens", (n,), torch.int32, dev)
+    _is(accept, "accept", (n,), torch.float32, dev)
+    _is(pick, "pick", (seqs,), torch.float32, dev)
+    if out is not None:
+        _is(out, "out", (n,), torch.int32, dev)
+    if n_out is not None:
+        _is(n_out, "n_out", (seqs,), torch.int32, dev)
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous and on {dev}")
+    if cache is not None and (cache.n_seqs != seqs or cache.device != dev):
+        raise ValueError(f"the batch has {seqs} sequences on {dev}, the cache {cache.n_seqs} on {cache.device}")
+    c = _verify(batch, vocab, _PROBS[target.dtype])
+    c.target, c.target_stride = target.data_ptr(), target.stride(0) if n > 1 else vocab
+    if draft is not None:
+        c.draft, c.draft_stride = draft.data_ptr(), draft.stride(0) if n > 1 else vocab
+    c.tokens, c.accept, c.pick = tokens.data_ptr(), accept.data_ptr(), pick.data_ptr()
+    if cache is not None:
+        c.seq_lens = cache.seq_lens.data_ptr()
+    with _On(dev, stream) as on:
+        if out is None:
+            out = on.new((n,), torch.int32)
+        if n_out is None:
+            n_out = on.new((seqs,), torch.int32)
+        if workspace is None:
+            size = ctypes.c_size_t(0)
+            _check(load().stlite_verify_workspace_size(ctypes.byref(c), ctypes.byref(size)), "stlite_verify_workspace_size")
+            workspace = on.new((max(size.value, 256),), torch.uint8)
+        if not on.own:
+            on.keep(target, draft, tokens, accept, pick, out, n_out, workspace, batch.d,
+                    *(cache.tensors if cache is not None else ()))
+        _check(load().stlite_verify_drafts(ctypes.byref(c), out.data_ptr(), n_out.data_ptr(), workspace.data_ptr(),
+                                           workspace.numel() * workspace.element_size(), on.handle), "stlite_verify_drafts")
+    return out, n_out

@@ -30,7 +30,8 @@ EXPORTS = (
     "stlite_layer_mean", "stlite_tsg_rho_concat", "stlite_css_saliency_concat", "stlite_compact_kv_layer",
     "stlite_select_topk_noalloc", "stlite_mean_attention",
     "stlite_paged_validate", "stlite_paged_workspace_size", "stlite_paged_compact", "stlite_paged_append",
-    "stlite_paged_attention", "stlite_paged_read",
+    "stlite_paged_attention", "stlite_paged_read", "stlite_paged_grow", "stlite_paged_release",
+    "stlite_verify_workspace_size", "stlite_verify_drafts",
 )
 
 
@@ -65,6 +66,20 @@ class _CPaged(ctypes.Structure):
     ]
 
 
+class _CFreePages(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("held", ctypes.c_void_p)]
+
+
+class _CVerify(ctypes.Structure):
+    _fields_ = [
+        ("n_seqs", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("total_new", ctypes.c_int64), ("cu_new", ctypes.c_void_p), ("h_cu_new", ctypes.c_void_p),
+        ("target", ctypes.c_void_p), ("draft", ctypes.c_void_p), ("target_stride", ctypes.c_int64),
+        ("draft_stride", ctypes.c_int64), ("tokens", ctypes.c_void_p), ("accept", ctypes.c_void_p),
+        ("pick", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+    ]
+
+
 class _CRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
 
@@ -86,6 +101,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_2603_00188_amd.build`")
     lib = ctypes.CDLL(path)
     P, C, R = ctypes.POINTER(_CProblem), ctypes.POINTER(_CPaged), ctypes.POINTER(_CRows)
+    F, V = ctypes.POINTER(_CFreePages), ctypes.POINTER(_CVerify)
     vp, sz, i64, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
     st = ctypes.c_int
     sig = {
@@ -121,6 +137,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "stlite_paged_append": (st, [C, ctypes.POINTER(_CRope), vp, R, R, R, vp, vp, f32, vp, vp]),
         "stlite_paged_attention": (st, [C, vp, f32, vp, vp, sz, vp]),
         "stlite_paged_read": (st, [C, vp, vp, vp]),
+        "stlite_paged_grow": (st, [C, F, vp, vp]),
+        "stlite_paged_release": (st, [C, F, vp, vp]),
+        "stlite_verify_workspace_size": (st, [V, ctypes.POINTER(sz)]),
+        "stlite_verify_drafts": (st, [V, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
