@@ -255,17 +255,17 @@ stlite_status check_pages(const stlite_paged* c, const stlite_free_pages* f, con
 }
 
 struct VerifyPlan {
-  int32_t chunk, chunks;
+  int32_t piece, pieces;
   size_t bytes;
 };
 
-// About 1024 work-groups, 1024 to 8192 entries of a row each.
+// About 1024 work-groups, 256 to 2048 entries of a row to each of their waves.
 VerifyPlan verify_plan(const stlite_verify* v) {
-  const int64_t even = ceil_div(int64_t(v->n_seqs) * v->vocab, 1024);
+  const int64_t even = ceil_div(int64_t(v->n_seqs) * v->vocab, 1024 * kVerifyPieces);
   VerifyPlan p;
-  p.chunk = int32_t(std::min<int64_t>(std::max<int64_t>(ceil_div(even, kVerifyMinChunk) * kVerifyMinChunk, kVerifyMinChunk), kVerifyMaxChunk));
-  p.chunks = int32_t(ceil_div(v->vocab, p.chunk));
-  p.bytes = align_up(size_t(v->n_seqs) * p.chunks * sizeof(double2)) + align_up(size_t(v->n_seqs) * sizeof(int32_t));
+  p.piece = int32_t(std::min<int64_t>(std::max<int64_t>(ceil_div(even, kVerifyMinPiece) * kVerifyMinPiece, kVerifyMinPiece), kVerifyMaxPiece));
+  p.pieces = int32_t(ceil_div(v->vocab, p.piece * kVerifyPieces) * kVerifyPieces);
+  p.bytes = align_up(size_t(v->n_seqs) * p.pieces * sizeof(double2)) + align_up(size_t(v->n_seqs) * sizeof(int32_t));
   return p;
 }
 
@@ -590,9 +590,9 @@ stlite_status stlite_verify_drafts(const stlite_verify* v, int32_t* out, int32_t
   a.out = out;
   a.n_out = n_out;
   a.sums = static_cast<double2*>(ws);
-  a.stop = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + align_up(size_t(v->n_seqs) * p.chunks * sizeof(double2)));
-  a.chunk = p.chunk;
-  a.chunks = p.chunks;
+  a.stop = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + align_up(size_t(v->n_seqs) * p.pieces * sizeof(double2)));
+  a.piece = p.piece;
+  a.pieces = p.pieces;
   return hip_status(launch_verify(a, v->dtype, static_cast<hipStream_t>(stream)), "verify_drafts launch");
 }
 

@@ -7,8 +7,6 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-// Places up to which the growing work-group writes them itself.
-constexpr int64_t kOwnSlots = 4096;
 
 // The sum of v over the threads before this one, and over all.
 __device__ inline int64_t scan(int64_t v, int64_t (&sm)[kWaves], int64_t& all) {
@@ -32,9 +30,10 @@ __device__ inline int64_t scan(int64_t v, int64_t (&sm)[kWaves], int64_t& all) {
   return sum;
 }
 
-// The thread whose pages entry f of the chunk's flat list belongs to: the last one with
-// before[t] <= f (one without pages has the next one's).
-__device__ inline int owner(const int64_t (&before)[kThreads], int64_t f) {
+// The thread whose entries entry f of the chunk's flat list is among: the last one with
+// before[t] <= f (one without entries has the next one's).
+template <typename I>
+__device__ inline int owner(const I (&before)[kThreads], I f) {
   int lo = 0, hi = kThreads;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -48,75 +47,76 @@ __device__ inline int32_t pages_of(const PagedDev& c, int64_t len) {
   return int32_t((len + (int64_t(1) << c.page_shift) - 1) >> c.page_shift);
 }
 
-__device__ inline int32_t slot_of(const PagedDev& c, int32_t s, int64_t i) {
-  const int32_t len = c.seq_lens[s];
-  const int64_t at = int64_t(len) - c.cu_new[s + 1] + i;
-  if (len < 0 || len > c.max_len || at < 0) return -1;
-  const int32_t page = c.page_table[int64_t(s) * c.max_pages + (at >> c.page_shift)];
-  return page >= 0 && page < c.n_pages ? (page << c.page_shift) + int32_t(at & ((1 << c.page_shift) - 1)) : -1;
-}
-
-__device__ inline int32_t seq_of(const int32_t* cu, int32_t n, int64_t j) {
-  int32_t lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int32_t mid = (lo + hi) >> 1;
-    if (cu[mid] <= j) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
-
 // One work-group, since every sequence's pages lie behind those of the sequences before
-// it: a scan of what 1024 sequences at a time need, then their pages as one flat list, a
-// thread each.  Latency-bound: three loads, a scan, a load and a store one after another.
+// it: a scan of what 1024 sequences at a time need, then their pages as one flat list and
+// their new tokens as another, a thread each.  With many of those, kLists writes them by
+// many work-groups, each with the scan of its own, and a second launch of one, kState, what
+// the scans read.  Latency-bound: three loads, a scan, a load and a store one after another.
+enum { kAll, kLists, kState };
+template <int PART>
 __global__ __launch_bounds__(kThreads) void paged_grow_kernel(PagedPagesArgs a) {
   __shared__ int64_t sm_wave[kWaves], sm_before[kThreads];
-  __shared__ int32_t sm_held[kThreads];
+  __shared__ int32_t sm_held[kThreads], sm_len[kThreads], sm_cu[kThreads];
   const PagedDev& c = a.c;
+  const int64_t first = int64_t(blockIdx.x) * kThreads + threadIdx.x, stride = int64_t(gridDim.x) * kThreads;
   const int32_t n_free = min(max(*a.n_free, 0), c.n_pages);
   int64_t carry = 0;  // pages that the sequences before this chunk need
   int64_t taken = 0;  // pages given out
   for (int32_t base = 0; base < c.n_seqs; base += kThreads) {
     const int32_t s = base + int32_t(threadIdx.x);
-    int32_t len = 0, held = 0;
+    int32_t len = 0, held = 0, cu = INT32_MAX;
     int64_t grown = 0, need = 0;
     bool fits = false;
     if (s < c.n_seqs) {
-      const int32_t now = c.seq_lens[s], n = c.cu_new[s + 1] - c.cu_new[s];
+      const int32_t now = c.seq_lens[s];
+      cu = c.cu_new[s];
       held = min(max(a.held[s], 0), c.max_pages);
       len = now < 0 ? now : min(now, c.max_len);
-      grown = int64_t(len) + n;
+      grown = int64_t(len) + (c.cu_new[s + 1] - cu);
       fits = len >= 0 && grown <= c.max_len;
       if (fits) need = max(pages_of(c, grown) - held, 0);
     }
     int64_t all;
     const int64_t before = scan(need, sm_wave, all);
     const bool granted = fits && (need == 0 || carry + before + need <= n_free);
-    sm_before[threadIdx.x] = before;
-    sm_held[threadIdx.x] = held;
-    if (s < c.n_seqs) {
+    if (PART != kLists && s < c.n_seqs) {
       c.seq_lens[s] = granted ? int32_t(grown) : len < 0 ? len : ~len;
       if (granted) a.held[s] = held + int32_t(need);
     }
     int64_t here;  // what this chunk takes: the needs of a first part of its sequences
     scan(granted ? need : 0, sm_wave, here);
-    __syncthreads();
-    for (int64_t f = threadIdx.x; f < here; f += kThreads) {
-      const int t = owner(sm_before, f);
-      c.page_table[int64_t(base + t) * c.max_pages + sm_held[t] + (f - sm_before[t])] = a.free_pages[n_free - 1 - (carry + f)];
+    if (PART != kState) {
+      sm_before[threadIdx.x] = before;
+      sm_held[threadIdx.x] = held;
+      sm_len[threadIdx.x] = granted ? len : -1;
+      sm_cu[threadIdx.x] = cu;
+      __syncthreads();
+      for (int64_t f = first; f < here; f += stride) {
+        const int t = owner(sm_before, f);
+        c.page_table[int64_t(base + t) * c.max_pages + sm_held[t] + (f - sm_before[t])] = a.free_pages[n_free - 1 - (carry + f)];
+      }
+      if (a.slots) {
+        const int32_t end = c.cu_new[min(base + kThreads, c.n_seqs)];
+        for (int64_t i = sm_cu[0] + first; i < end; i += stride) {
+          const int t = owner(sm_cu, int32_t(i));
+          const int64_t at = int64_t(sm_len[t]) + (i - sm_cu[t]);
+          const int32_t entry = int32_t(at >> c.page_shift), more = entry - sm_held[t];
+          int32_t page = -1;
+          if (sm_len[t] >= 0)
+            page = more < 0 ? c.page_table[int64_t(base + t) * c.max_pages + entry]
+                            : a.free_pages[n_free - 1 - (carry + sm_before[t] + more)];
+          a.slots[i] = page >= 0 && page < c.n_pages ? (page << c.page_shift) + int32_t(at & ((1 << c.page_shift) - 1)) : -1;
+        }
+      }
+      __syncthreads();  // the lists have been read
     }
     carry += all;
     taken += here;
   }
-  __syncthreads();
-  if (threadIdx.x == 0) *a.n_free = n_free - int32_t(taken);
-  if (a.slots && c.total_new <= kOwnSlots)
-    for (int64_t i = threadIdx.x; i < c.total_new; i += kThreads) a.slots[i] = slot_of(c, seq_of(c.cu_new, c.n_seqs, i), i);
-}
-
-__global__ __launch_bounds__(256) void paged_slots_kernel(PagedPagesArgs a) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (i < a.c.total_new) a.slots[i] = slot_of(a.c, seq_of(a.c.cu_new, a.c.n_seqs, i), i);
+  if (PART != kLists) {
+    __syncthreads();
+    if (threadIdx.x == 0) *a.n_free = n_free - int32_t(taken);
+  }
 }
 
 // The pages behind every sequence's new end, as one flat list (sequences in turn, entries
@@ -171,9 +171,17 @@ __global__ __launch_bounds__(kThreads) void paged_release_kernel(PagedPagesArgs 
 }  // namespace
 
 hipError_t launch_paged_grow(const PagedPagesArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(paged_grow_kernel, dim3(1), dim3(kThreads), 0, stream, a);
-  if (a.slots && a.c.total_new > kOwnSlots)
-    hipLaunchKernelGGL(paged_slots_kernel, dim3(uint32_t((a.c.total_new + 255) / 256)), dim3(256), 0, stream, a);
+  // 1000 sequences of up to 2999 new tokens (90000 pages, 1.5 million places) take 19 us by
+  // 256 work-groups and a second launch (14 and 6), 61 by one and a launch for the places;
+  // 64 of one token 6 us by one.
+  if (a.c.total_new <= 4096) {
+    hipLaunchKernelGGL((paged_grow_kernel<kAll>), dim3(1), dim3(kThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((paged_grow_kernel<kLists>), dim3(256), dim3(kThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((paged_grow_kernel<kState>), dim3(1), dim3(kThreads), 0, stream, a);
+  }
   return hipGetLastError();
 }
 

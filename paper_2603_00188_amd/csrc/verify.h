@@ -18,12 +18,12 @@ struct VerifyArgs {
   int32_t* seq_lens;       // [n_seqs], nullable
   int32_t* out;            // [total_new]
   int32_t* n_out;          // [n_seqs]
-  double2* sums;           // workspace [n_seqs][chunks]
+  double2* sums;           // workspace [n_seqs][pieces]
   int32_t* stop;           // workspace [n_seqs]
-  int32_t chunk, chunks;   // entries of a row per work-group, a multiple of 1024; their number
+  int32_t piece, pieces;   // entries of a row per wave, a multiple of 256; their number, of whole work-groups
 };
 
-constexpr int32_t kVerifyMinChunk = 1024, kVerifyMaxChunk = 8192;
+constexpr int32_t kVerifyMinPiece = 256, kVerifyMaxPiece = 2048, kVerifyPieces = 4;  // (pieces of a work-group)
 
 // type: 0 bf16, 1 fp16, 2 fp32
 hipError_t launch_verify(const VerifyArgs& a, int type, hipStream_t stream);

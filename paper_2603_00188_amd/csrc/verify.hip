@@ -92,20 +92,24 @@ __device__ inline int32_t stop_of(const VerifyArgs& a, int32_t row0, int32_t n, 
   return sm_stop;
 }
 
-// One chunk of one sequence's deciding row: the sums of its weights and of its p.
+// One chunk of one sequence's deciding row, a piece of it to each wave: the sums of its
+// weights and of its p.  HBM-bound: 64 rows of 131072 fp32 of both sides (67 MB) take 10 us,
+// 6.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void verify_sum_kernel(VerifyArgs a) {
   __shared__ int32_t sm_stop;
-  __shared__ double sm[2][kWaves];
   const int32_t s = blockIdx.y, row0 = a.cu_new[s], n = a.cu_new[s + 1] - row0;
   if (n <= 0 || (a.seq_lens && a.seq_lens[s] < 0)) return;
   const int32_t stop = stop_of<T>(a, row0, n, sm_stop);
   const Row<T> row(a, row0, n, stop);
   typedef typename Probs<T>::vec vec;
   constexpr int kPer = Probs<T>::kPer;
-  const int32_t j0 = int32_t(blockIdx.x) * a.chunk, j1 = min(j0 + a.chunk, a.vocab);
+  const int lane = threadIdx.x & 63;
+  const int32_t piece = int32_t(blockIdx.x) * kWaves + int32_t(threadIdx.x >> 6), j0 = piece * a.piece;
+  const int32_t j1 = min(j0 + a.piece, a.vocab);
   double rest = 0.0, full = 0.0;
-  for (int32_t j = j0 + int32_t(threadIdx.x) * kPer; j < j1; j += kThreads * kPer) {
+#pragma unroll 4
+  for (int32_t j = j0 + lane * kPer; j < j1; j += 64 * kPer) {
     if (j + kPer <= j1) {
       const vec p = *reinterpret_cast<const vec*>(row.p + j);
       vec q = {};
@@ -128,25 +132,18 @@ __global__ __launch_bounds__(kThreads) void verify_sum_kernel(VerifyArgs a) {
     rest += __shfl_xor(rest, d);
     full += __shfl_xor(full, d);
   }
-  if ((threadIdx.x & 63) == 0) {
-    sm[0][threadIdx.x >> 6] = rest;
-    sm[1][threadIdx.x >> 6] = full;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    a.sums[int64_t(s) * a.chunks + blockIdx.x] = make_double2((sm[0][0] + sm[0][1]) + (sm[0][2] + sm[0][3]),
-                                                              (sm[1][0] + sm[1][1]) + (sm[1][2] + sm[1][3]));
-    if (blockIdx.x == 0) a.stop[s] = stop;
-  }
+  if (lane == 0) a.sums[int64_t(s) * a.pieces + piece] = make_double2(rest, full);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.stop[s] = stop;
 }
 
-// A sequence's next token: the chunk that the threshold falls into, and the entry in it.
+// A sequence's next token: the piece that the threshold falls into, and the entry in it.
 // Where rounding, or a number that is not below one, leaves no entry behind the threshold,
-// the last one with any weight.
+// the last one with any weight.  Latency-bound: the sums, a scan, a piece's entries, another.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
-  __shared__ double sm[kWaves], sm_before;
-  __shared__ int32_t sm_first, sm_last;
+  constexpr int kEach = kVerifyMaxPiece / kThreads;  // entries of a thread
+  __shared__ double sm[2][kWaves], sm_before;
+  __shared__ int32_t sm_first[2][kWaves], sm_last[2][kWaves];
   const int32_t s = blockIdx.x, row0 = a.cu_new[s], n = a.cu_new[s + 1] - row0;
   if (n <= 0 || (a.seq_lens && a.seq_lens[s] < 0)) {  // idle
     for (int32_t t = threadIdx.x; t < n; t += kThreads) a.out[int64_t(row0) + t] = -1;
@@ -155,57 +152,70 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
   }
   const int32_t stop = a.stop[s];
   const Row<T> row(a, row0, n, stop);
-  const double2* sums = a.sums + int64_t(s) * a.chunks;
-  const int32_t per = (a.chunks + kThreads - 1) / kThreads;
-  const int32_t c0 = min(int32_t(threadIdx.x) * per, a.chunks), c1 = min(c0 + per, a.chunks);
+  const double2* sums = a.sums + int64_t(s) * a.pieces;
+  const int32_t per = (a.pieces + kThreads - 1) / kThreads;
+  const int32_t c0 = min(int32_t(threadIdx.x) * per, a.pieces), c1 = min(c0 + per, a.pieces);
   double rest = 0.0, full = 0.0, total;
   for (int32_t i = c0; i < c1; ++i) {
     rest += sums[i].x;
     full += sums[i].y;
   }
-  double before = scan(rest, sm, total);
+  double before = scan(rest, sm[0], total);
   const bool some = total > 0.0;
-  if (!some) before = scan(full, sm, total);  // nothing is left over: p itself decides
+  if (!some) before = scan(full, sm[1], total);  // nothing is left over: p itself decides
   const double threshold = double(a.pick[s]) * total;
-  auto begin = [&]() {
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      sm_first = INT32_MAX;
-      sm_last = -1;
+  // One entry (a piece, then a token) of weight w behind `sum`: of this thread's, which lie
+  // in order, the first that passes the threshold and the last with any weight.
+  int32_t first = INT32_MAX, last = -1;
+  auto walk = [&](int32_t at, double w, double& sum) {
+    if (!(w > 0.0)) return;
+    last = at;
+    sum += w;
+    if (sum > threshold) first = min(first, at);
+  };
+  // Of all threads', in their order, the first that passes, else the last; -1: no weight.
+  auto found = [&](int k) {
+    const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
+    const int32_t lo = __shfl(first, f ? __builtin_ctzll(f) : 0), hi = __shfl(last, l ? 63 - __builtin_clzll(l) : 0);
+    if ((threadIdx.x & 63) == 0) {
+      sm_first[k][threadIdx.x >> 6] = lo;
+      sm_last[k][threadIdx.x >> 6] = hi;
     }
     __syncthreads();
+    int32_t at = INT32_MAX, end = -1;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      at = min(at, sm_first[k][w]);
+      end = max(end, sm_last[k][w]);
+    }
+    first = INT32_MAX;
+    last = -1;
+    return min(at, end);
   };
-  // One entry (a chunk, then a token) of weight w behind `sum`: whether it passes the threshold.
-  auto passes = [&](int32_t at, double w, double& sum) {
-    if (!(w > 0.0)) return false;
-    atomicMax(&sm_last, at);
-    sum += w;
-    if (sum > threshold) atomicMin(&sm_first, at);
-    return sum > threshold;
-  };
-  begin();
   double sum = before;
-  for (int32_t i = c0; i < c1; ++i)
-    if (passes(i, some ? sums[i].x : sums[i].y, sum)) break;
-  __syncthreads();
-  const int32_t chunk = min(sm_first, sm_last);  // (sm_last is an entry at or behind sm_first, if there is any)
-  sum = before;
-  for (int32_t i = c0; i < c1; ++i) {
-    if (i == chunk) sm_before = sum;
-    sum += some ? sums[i].x : sums[i].y;
+  for (int32_t i = c0; i < c1; ++i) walk(i, some ? sums[i].x : sums[i].y, sum);
+  const int32_t piece = found(0);
+  int32_t token = -1;
+  if (piece >= 0) {
+    const int32_t each = a.piece / kThreads, j0 = piece * a.piece + int32_t(threadIdx.x) * each;
+    double w[kEach], mine = 0.0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      w[i] = 0.0;
+      if (i < each && j0 + i < a.vocab) w[i] = some ? row.rest_at(j0 + i) : double(weight(float(row.p[j0 + i])));
+    }
+    sum = before;
+    for (int32_t i = c0; i < c1 && i <= piece; ++i) {
+      if (i == piece) sm_before = sum;
+      sum += some ? sums[i].x : sums[i].y;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine += w[i];
+    sum = scan(mine, sm[0], all) + sm_before;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) walk(j0 + i, w[i], sum);
+    token = found(1);
   }
-  begin();
-  if (chunk >= 0) {
-    const int32_t each = a.chunk / kThreads, j0 = chunk * a.chunk + int32_t(threadIdx.x) * each;
-    const int32_t j1 = min(j0 + each, a.vocab);
-    double mine = 0.0, all;
-    for (int32_t j = j0; j < j1; ++j) mine += some ? row.rest_at(j) : double(weight(float(row.p[j])));
-    sum = scan(mine, sm, all) + sm_before;
-    for (int32_t j = j0; j < j1; ++j)
-      if (passes(j, some ? row.rest_at(j) : double(weight(float(row.p[j]))), sum)) break;
-    __syncthreads();
-  }
-  const int32_t token = min(sm_first, sm_last);  // (-1: no entry of p has any weight)
   for (int32_t t = threadIdx.x; t < n; t += kThreads)
     a.out[int64_t(row0) + t] = t < stop ? a.tokens[int64_t(row0) + t] : t == stop ? token : -1;
   if (threadIdx.x == 0) {
@@ -216,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
 
 template <typename T>
 hipError_t verify(const VerifyArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((verify_sum_kernel<T>), dim3(a.chunks, a.n_seqs), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((verify_sum_kernel<T>), dim3(a.pieces / kWaves, a.n_seqs), dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((verify_pick_kernel<T>), dim3(a.n_seqs), dim3(kThreads), 0, stream, a);
