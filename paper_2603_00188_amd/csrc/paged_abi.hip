@@ -153,10 +153,19 @@ AttnPlan attn_plan(const stlite_paged* c) {
     p.tokens = int32_t(std::max<int64_t>(most, 1));
     p.rows = p.tokens * group <= 16 ? 16 : 32;
     p.parts = int32_t(ceil_div(group, p.rows));
-    p.shares = 512;
-    p.min_share = 64;
-    p.item_cost = 64;
     items *= p.parts * live;
+    // Over a 4-bit pool a share's round is 256 keys and a key takes a quarter of the time.
+    // With fewer items than CUs one work-group to each, 256 / 512 shares: a step over 30105
+    // tokens (112 items) 80.3 / 82.3 us, one layer over 150528 (4) 25.6 / 27.7, four drafted
+    // tokens in each of 16 sequences in 8 units (128) 36.9 / 40.0; with more, two, which
+    // begin and end at different times: 64 sequences of up to 8000 in 32 units (2048) 229 /
+    // 209, drafted tokens in 16 in 16 (256) 59.7 / 54.2.  min_share 64 / 256: 678 keys of a
+    // layer 12.7 / 11.8, a layer over 30105 21 / 17.8.  item_cost 128 / 256 / 512: one layer
+    // over 150528 29.4 / 28.7 / 27.6, the 2048 items 214 / 212 / 210.
+    const bool four = is_four(c);
+    p.shares = four && items < 256 ? 256 : 512;
+    p.min_share = four ? 256 : 64;
+    p.item_cost = four ? 512 : 64;
   } else {
     p.parts = 1;
     p.rows = kExtRows;
