@@ -46,7 +46,7 @@ constexpr int kKeys = 16 * kRuns;  // of a tile
 // chunk, or four rows' 4 apart, take all banks.  Then the scales, run by run.
 constexpr int kKPart = 1024 + 16, kVPart = 1024 + 64;
 constexpr int kVAt = 4 * kKPart, kScalesAt = kVAt + 4 * kVPart, kSlot = kScalesAt + 2 * kKeys * 4;
-constexpr int kDepth = 2;
+constexpr int kDmas = 10;     // instructions of a tile
 constexpr int kWindow = 512;  // entries of the page table that a wave holds
 constexpr float kLazy = 8.0f, kFar = 960.0f;
 
@@ -64,11 +64,13 @@ __device__ inline V lds_read(uint32_t at) {
   return *reinterpret_cast<const __attribute__((address_space(3))) V*>((uintptr_t)at);
 }
 
-template <typename T, int NG>  // 16 NG rows to an item
-__global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArgs a) {
+// 16 NG rows to an item.  Of 48 or 64 rows the sums and queries take more registers than two
+// waves of a SIMD have; one wave has three tiles under way instead of one.
+template <typename T, int NG>
+__global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
-  constexpr int NT = kWaves * 64, kRows = 16 * NG;
+  constexpr int NT = kWaves * 64, kRows = 16 * NG, kDepth = NG <= 2 ? 2 : 4;
   __shared__ float sm_m[kWaves][kRows], sm_l[kWaves][kRows];
   __shared__ __align__(1024) uint8_t sm_ring[kWaves][kDepth][kSlot];  // (the waves' sums, once an item is done)
   __shared__ int32_t sm_pages[kWaves][kWindow];
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArg
     const int32_t* const table = c.page_table + int64_t(it.seq) * c.max_pages;
     const uint8_t* const unit_at = reinterpret_cast<const uint8_t*>(
         PagedPlan<NT>::uniform(reinterpret_cast<int64_t>(reinterpret_cast<const uint8_t*>(c.k) + page4(c, unit, 0))));
-    uint64_t bad = 0, bad_next = 0;  // lanes whose run's page is none, of the current tile and the next
+    bool bad = false;  // a page was none
     // Tile i.  Where a page is none, what page 0 holds is read, and left out; rows past the
     // sequence's end lie in its last page, whatever they hold, or in what the table has behind it.
     auto fetch = [&](int32_t i) {
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArg
       const uint32_t to = ring + (i & (kDepth - 1)) * kSlot;
       uint32_t page = *reinterpret_cast<const volatile __attribute__((address_space(3))) uint32_t*>(
           (uintptr_t)(window + ((uint32_t(entry) & (kWindow - 1)) + entry_from) * 4));
-      bad_next = __ballot(page >= uint32_t(c.n_pages));
+      bad |= __ballot(page >= uint32_t(c.n_pages)) != 0;
       page = page < uint32_t(c.n_pages) ? page : 0;
       const uint8_t* const at = unit_at + uint64_t(page) * page_bytes;
       const uint8_t* const codes = at + (uint32_t(j0 & in_page) * kCodes4 + codes_from);
@@ -151,7 +153,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArg
       for (int d = 0; d < 4; ++d) dma16_each(codes + v_off + d * 4 * kCodes4, to + kVAt + d * kVPart);
       dma4_each(scales + v_off, to + kScalesAt + kKeys * 4);
     };
-    if (steps > 0) fetch(0);
+#pragma unroll 1
+    for (int i = 0; i < min(steps, kDepth - 1); ++i) fetch(i);
 
     x8 qb[NG][4];     // dimensions 32 quad + 8 kk ..
     int32_t sees[NG];  // keys that this lane's rows see
@@ -176,10 +179,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArg
     bool odd = false;  // blocks that some rows do not see were NaN
 
     auto step = [&](int32_t j0, uint32_t at) {
-      const bool ends = bad != 0 || j0 + kKeys > min(k1, sees_first);  // keys are left out, for some rows or all
+      uint64_t none = 0;  // lanes whose run's page is none
+      if (bad) none = __ballot(uint32_t(table[min((j0 >> c.page_shift) + int32_t(entry_from), c.max_pages - 1)]) >= uint32_t(c.n_pages));
+      const bool ends = none != 0 || j0 + kKeys > min(k1, sees_first);  // keys are left out, for some rows or all
       // Key i of run r, of the four of this lane, and the first that is left out for all rows.
       auto key = [&](int r, int i) { return j0 + 16 * r + 4 * quad + i; };
-      auto end = [&](int r) { return bad >> (16 * r) & 1 ? 0 : k1; };
+      auto end = [&](int r) { return none >> (16 * r) & 1 ? 0 : k1; };
       u32x4_t kc[kRuns];
       uint32_t ks[kRuns];
 #pragma unroll
@@ -313,9 +318,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArg
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) asm volatile("" : "+v"(qb[ng][kk]));
     for (int32_t i = 0; i < steps; ++i) {
-      wait_vmcnt<0>();  // tile i has landed
-      bad = bad_next;
-      if (i + 1 < steps) fetch(i + 1);  // in place of tile i - 1, whose values have been used
+      // tile i has landed: all but the kDepth - 2 behind it (near the end: all)
+      if (i + kDepth - 1 <= steps) wait_vmcnt<kDmas * (kDepth - 2)>();
+      else wait_vmcnt<0>();
+      if (i + kDepth - 1 < steps) fetch(i + kDepth - 1);  // in place of tile i - 1, whose values have been used
       step(first + i * (kKeys * kWaves), ring + (i & (kDepth - 1)) * kSlot);
     }
     if (__ballot(odd)) {
@@ -390,8 +396,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void paged4_few_kernel(PagedAttnArg
 
 template <typename T>
 hipError_t few(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.rows == 16) hipLaunchKernelGGL((paged4_few_kernel<T, 1>), dim3(a.shares), dim3(kWaves * 64), 0, stream, a);
-  else hipLaunchKernelGGL((paged4_few_kernel<T, 2>), dim3(a.shares), dim3(kWaves * 64), 0, stream, a);
+  const dim3 grid(a.shares), block(kWaves * 64);
+  if (a.rows == 16) hipLaunchKernelGGL((paged4_few_kernel<T, 1>), grid, block, 0, stream, a);
+  else if (a.rows == 32) hipLaunchKernelGGL((paged4_few_kernel<T, 2>), grid, block, 0, stream, a);
+  else if (a.rows == 48) hipLaunchKernelGGL((paged4_few_kernel<T, 3>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((paged4_few_kernel<T, 4>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -43,6 +43,7 @@ size_t align_up(size_t x) { return (x + 255) & ~size_t(255); }
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int32_t kMaxGroup = 128;
+
 constexpr int64_t kMaxLen = int64_t(1) << 28;
 constexpr int64_t kIntRows = (int64_t(1) << 31) - 1;
 
@@ -147,11 +148,21 @@ AttnPlan attn_plan(const stlite_paged* c) {
     most = std::max(most, n);
     live += n > 0;
   }
-  p.decode = most <= 1 || (is_four(c) && most * group <= 32);
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
+  // A few tokens over a 4-bit pool by the kernel of one: up to 32 rows always, up to 48 or
+  // 64, which leave one wave to a SIMD, where the sequences may have keys enough.  Several
+  // tokens' kernel / this, 28 heads over 4, 16 sequences in 2 layers: 5 tokens (35 rows)
+  // behind up to 6000 keys 55 / 51 us, 40000 310 / 187; 9 (63) 58 / 62, 16000 136 / 118; 8
+  // of 16 heads over 2 (64) behind up to 40000 170 / 135; one sequence in 8 units behind
+  // 3000, 40 rows 21 / 23, 60 22 / 27.  One token of 40 heads of a kv head, two parts of
+  // 32 / one of 48: 16 sequences of 60000 72 / 67, 8 of 8000 28 / 30; of 64 heads 72 / 79.
+  const bool four = is_four(c);
+  const int64_t few_rows = std::max<int64_t>(most, 1) * group, keys = items * live * c->max_len;
+  const int64_t most_rows = !four || keys < (1 << 18) ? 32 : keys < (1 << 20) || most <= 1 ? 48 : 64;
+  p.decode = most <= 1 || (four && few_rows <= most_rows);
   if (p.decode) {
     p.tokens = int32_t(std::max<int64_t>(most, 1));
-    p.rows = p.tokens * group <= 16 ? 16 : 32;
+    p.rows = int32_t(few_rows <= 16 ? 16 : few_rows <= 32 || few_rows > most_rows ? 32 : ceil_div(few_rows, 16) * 16);
     p.parts = int32_t(ceil_div(group, p.rows));
     items *= p.parts * live;
     // Over a 4-bit pool a share's round is 256 keys and a key takes a quarter of the time.
@@ -162,8 +173,8 @@ AttnPlan attn_plan(const stlite_paged* c) {
     // 209, drafted tokens in 16 in 16 (256) 59.7 / 54.2.  min_share 64 / 256: 678 keys of a
     // layer 12.7 / 11.8, a layer over 30105 21 / 17.8.  item_cost 128 / 256 / 512: one layer
     // over 150528 29.4 / 28.7 / 27.6, the 2048 items 214 / 212 / 210.
-    const bool four = is_four(c);
-    p.shares = four && items < 256 ? 256 : 512;
+    // (Of 48 and 64 rows one work-group is all that a CU holds.)
+    p.shares = four && (items < 256 || p.rows > 32) ? 256 : 512;
     p.min_share = four ? 256 : 64;
     p.item_cost = four ? 512 : 64;
   } else {

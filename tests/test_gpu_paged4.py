@@ -307,6 +307,50 @@ def test_extend_of_few_and_many_tiles(torch_cuda, tiles):
         f.compare(q, f.attend(q))
 
 
+def _room(f, keys):
+    """A table for sequences of so many keys, of which the cache's have few: what a program that serves long ones has."""
+    wide = np.full((len(f.lens), -(-keys // f.page)), -1, np.int32)
+    wide[:, :f.table.shape[1]] = f.table
+    f.table, f.max_len = wide, keys
+    f.rebuild()
+    return f
+
+
+@pytest.mark.parametrize("group,tokens", [(11, 3), (7, 6), (48, 1), (33, 1), (40, 1), (64, 1), (12, 4), (16, 3), (7, 7), (7, 9), (16, 4), (1, 64), (1, 50), (32, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_few_rows(torch_cuda, group, tokens, dtype):
+    """33 to 64 rows to an item, in the kernel that takes them where sequences may be long: masks, ends, idle sequences,
+    pages that are none, values that are NaN in a later token's row, and sequences cut into parts."""
+    import torch
+    lens = (1, tokens, 63 + tokens, 64, 300, 0, 5, 2000, 131)
+    new = [min(tokens, max(n, 0)) for n in lens]
+    new[6], new[4] = 0, max(tokens - 1, 1)
+    f = _room(Served4(lens, new, 32, dtype, 1, 2 * group, 2, seed=51, fill=float("nan")), 1 << 17)
+    f.table[7, 3], f.table[7, 40] = -1, f.n_pages
+    f.rebuild()
+    q = f.randn((1, f.total, 2 * group, D), 1.5)
+    out = f.attend(q)
+    _log(f"few rows {group} x {tokens} {dtype}: worst error / tolerance {f.compare(q, out):.3g}")
+    assert np.array_equal(_bits(f.attend(q)), _bits(out)), "two calls differ"
+    s, j = 4, lens[4] - max(new[4] // 2, 1)  # a new token's own row, in the middle
+    f.v.view(1, 2, -1, D)[0, 1, OP.place(f.table, s, j, 32, f.n_pages), 70] = float("nan")
+    f.k.view(1, 2, -1, D)[0, 0, OP.place(f.table, 7, 1990, 32, f.n_pages), 70] = float("nan")
+    f.rebuild()
+    got = f.attend(q)
+    want = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    want[0, int(f.cu[s]) + j - (lens[s] - new[s]):f.cu[s + 1], group:, 64:96] = True
+    want[0, int(f.cu[7]) + max(1990 - (2000 - tokens), 0):f.cu[8], :group] = True
+    assert torch.equal(torch.isnan(got), want) and torch.equal(got[~want], out[~want])
+
+
+def test_few_rows_of_long_sequences(torch_cuda):
+    """Many parts to an item, ring slots used again, a page table beyond the entries that a wave holds."""
+    for page, group, tokens in ((16, 7, 6), (16, 7, 9), (64, 7, 4), (16, 7, 1)):
+        f = _room(Served4((20000, 9000, 16384 + tokens), (tokens,) * 3, page, "bf16", 1, group, 1, seed=52), 1 << 19)
+        q = f.randn((1, f.total, group, D), 1.5)
+        f.compare(q, f.attend(q))
+
+
 @pytest.mark.parametrize("new", [1, 4, 150])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_rising_and_extreme_logits(torch_cuda, new, dtype):
