@@ -83,8 +83,10 @@ __device__ __forceinline__ uint32_t lane_xor_bits(uint32_t v) {
 
 // Kept rows into the pages of a 4-bit pool: the same walk, sixteen lanes to a row.  Four
 // lanes hold a block: its greatest magnitude by two exchanges, then 4 bytes of codes each;
-// the row's four scale bytes meet in one lane.  The codes of consecutive rows are
-// contiguous, and are left to the caches, which put a page's lines together.
+// the row's four scale bytes meet in one lane.
+// HBM-bound: 30105 rows of 112 units (1.73 GB in, 0.46 out) take 390 us, 5.6 TB/s; 678 rows
+// 15.  (With codes stored past the caches 369, but what reads them next then takes more
+// than that longer.)
 template <typename T>
 __global__ __launch_bounds__(256) void paged4_compact_kernel(PagedCompactArgs a) {
   constexpr int kPer = kRowsPerGroup / 16;
@@ -151,10 +153,12 @@ constexpr int kReadRows = 16;
 // The new tokens' rows, sixteen lanes to a row, a work-group 16 rows in the output's order
 // (a token's heads one after another), so that what it writes is contiguous.
 // HBM-bound, a row's 68 (or 256) bytes in and 256 out: 30105 tokens of 112 units in 4 bits
-// take 545 us, 4.0 TB/s, most of it written.  (In a unit's order, whose writes are 256
-// bytes apart, 584; with 32, 64, 128 rows to a work-group 559, 559, 582; with stores that
-// go through the caches 588.)
-template <typename T, bool FOUR>
+// (2.2 GB, four fifths of it written) take 410 us behind the compaction, 5.3 TB/s, with the
+// codes past the caches, 475 through them; 678 tokens 8.6 through them and 9.9 past, so
+// PAST where the rows are more than the caches hold.
+// (In a unit's order, whose writes are 256 bytes apart, 584; with 32, 64, 128 rows to a
+// work-group 14, 14 and 37 more; with stores that go through the caches 30 more.)
+template <typename T, bool FOUR, bool PAST>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
   const PagedDev& c = a.c;
   const int layer = blockIdx.y;
@@ -177,7 +181,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         const uint8_t* p = reinterpret_cast<const uint8_t*>(kv ? c.v : c.k) + page4(c, unit, page);
-        codes[kv] = *reinterpret_cast<const uint32_t*>(p + row * kCodes4 + part * 4);
+        const uint32_t* const from = reinterpret_cast<const uint32_t*>(p + row * kCodes4 + part * 4);
+        codes[kv] = PAST ? __builtin_nontemporal_load(from) : *from;
         scales[kv] = p[(in_page + 1) * kCodes4 + row * 4 + (part >> 2)];
       }
 #pragma unroll
@@ -330,7 +335,7 @@ __device__ __forceinline__ void store4(const PagedAppendArgs& a, bool key, int l
 // at the rate of single 32-bit operations, and the token's sines too; on the way to
 // codes it passes through fp32 rounded to odd, which keeps the side.
 template <typename T, int WAVES, bool FOUR>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
+__global__ __launch_bounds__(256, FOUR ? 4 : 1) void paged_append_kernel(PagedAppendArgs a) {
   constexpr int kTok = 4 / WAVES;  // tokens per work-group
   __shared__ float2 sm_cs[kTok][64];
   __shared__ double2 sm_cs64[FOUR ? kTok : 1][64];
@@ -515,13 +520,19 @@ hipError_t launch_paged_compact(const PagedCompactArgs& a, bool four, bool half,
   return hipGetLastError();
 }
 
+template <typename T>
+static void read4(const PagedReadArgs& a, dim3 grid, hipStream_t stream) {
+  const bool past = 2 * a.c.total_new * a.c.n_units * kRow4 > (int64_t(128) << 20);
+  if (past) hipLaunchKernelGGL((paged_read_kernel<T, true, true>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_read_kernel<T, true, false>), grid, dim3(256), 0, stream, a);
+}
+
 hipError_t launch_paged_read(const PagedReadArgs& a, bool four, bool half, hipStream_t stream) {
   const int64_t blocks = (a.c.total_new * a.c.n_kv_heads + kReadRows - 1) / kReadRows;
   const int64_t x = blocks < kMaxBlocks ? blocks : kMaxBlocks;
   const dim3 grid(uint32_t(x), a.c.n_layers, uint32_t((blocks + x - 1) / x));
-  if (!four) hipLaunchKernelGGL((paged_read_kernel<__bf16, false>), grid, dim3(256), 0, stream, a);
-  else if (half) hipLaunchKernelGGL((paged_read_kernel<_Float16, true>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((paged_read_kernel<__bf16, true>), grid, dim3(256), 0, stream, a);
+  if (!four) hipLaunchKernelGGL((paged_read_kernel<__bf16, false, false>), grid, dim3(256), 0, stream, a);
+  else half ? read4<_Float16>(a, grid, stream) : read4<__bf16>(a, grid, stream);
   return hipGetLastError();
 }
 

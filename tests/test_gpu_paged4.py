@@ -527,3 +527,32 @@ def test_pool_of_more_than_4_gib(torch_cuda, new):
     assert torch.equal(big.v[:, :, -used:], f.vb[:, :, f.table[0, :used]])
     for a, b in zip(P.paged_read(big, f.batch), P.paged_read(f.cache, f.batch)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_rows_past_the_caches(torch_cuda, dtype):
+    """More rows than the caches hold, into pages and back: the first, the last and rows between as the oracle's, the rest as
+    a smaller call's."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    n, layers, hk = 33000, 8, 2
+    p = T._problem((n,), layers, hk, (1, 1))
+    cache = P.PagedCache.alloc(layers, 4, hk, 1, n, page_size=64, dtype={"bf16": torch.bfloat16, "fp16": torch.float16}[dtype], bits=4)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(53)
+    k, v = (torch.randn((layers * hk, n, D), generator=gen, device="cuda").to(cache.dtype) for _ in range(2))
+    kept = torch.arange(n, dtype=torch.int32, device="cuda").repeat(layers * hk, 1)
+    P.paged_compact(cache, p, k, v, kept)
+    out = P.paged_read(cache, P.NewTokens([0, n]))
+    for x, src in zip(out, (k, v)):
+        for layer in range(layers):  # a layer at a time is a small call
+            one = cache.layer(layer)
+            assert torch.equal(P.paged_read(one, P.NewTokens([0, n]))[0 if x is out[0] else 1][0], x[layer])
+        at = [0, 1, 63, 64, 15999, n - 1]
+        want = O4.decode(*O4.encode(_f64(src.view(layers, hk, n, D)[:, :, at]), dtype))
+        assert np.array_equal(_f64(x[:, at]), want.transpose(0, 2, 1, 3))
+    small = P.PagedCache.alloc(layers, 4, hk, 1, 1000, page_size=64, dtype=cache.dtype, bits=4)
+    ps = T._problem((1000,), layers, hk, (1, 1))
+    P.paged_compact(small, ps, k[:, 5000:6000].contiguous(), v[:, 5000:6000].contiguous(), kept[:, :1000].contiguous())
+    for x, y in zip(P.paged_read(small, P.NewTokens([0, 1000])), out):
+        assert torch.equal(x, y[:, 5000:6000])
