@@ -556,3 +556,108 @@ def test_rows_past_the_caches(torch_cuda, dtype):
     P.paged_compact(small, ps, k[:, 5000:6000].contiguous(), v[:, 5000:6000].contiguous(), kept[:, :1000].contiguous())
     for x, y in zip(P.paged_read(small, P.NewTokens([0, 1000])), out):
         assert torch.equal(x, y[:, 5000:6000])
+
+
+# ---------------------------------------------------------------------------
+# Together, as a program serves
+# ---------------------------------------------------------------------------
+
+def test_compress_into_4_bits(torch_cuda):
+    """The compression pass straight into 4-bit pages: the codes of the rows that the dense compaction keeps."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    from paper_2603_00188_amd import stlite as S
+    from tests import gpu_harness as H
+    from tests.test_gpu_parity import SMALL
+    case = H.Case(SMALL["ragged"])
+    w, prob, res = case.w, case.prob, case.run()
+    cache = P.PagedCache.alloc(case.n_layers, w.n_q_heads, w.n_kv_heads, prob.n_seqs, int(np.diff(case.cu_budget).max()) + 9,
+                               page_size=16, bits=4)
+    S.compress(prob, case.dq, case.dk, case.dv, case.out, alpha=w.alpha, cache=cache)
+    k, v = P.paged_read(cache, P.NewTokens(case.cu_budget))
+    torch.cuda.synchronize()
+    assert cache.seq_lens.tolist() == np.diff(case.cu_budget).tolist()
+    for x, rows in ((k, res["k_out"]), (v, res["v_out"])):
+        bits = torch.from_numpy(np.ascontiguousarray(rows).view(np.int16)).view(torch.bfloat16)
+        want = O4.decode(*O4.encode(_f64(bits), "bf16")).reshape(case.n_layers, w.n_kv_heads, -1, D)
+        assert np.array_equal(_f64(x), want.transpose(0, 2, 1, 3))
+
+
+def test_layers_one_by_one(torch_cuda):
+    """What a model does: layer after layer, each on its own slice of the cache."""
+    import torch
+    for new in (1, 6, 40):
+        f = Served4((500, 120, 77), (new,) * 3, 32, "bf16", 4, 8, 2, seed=17)
+        q, k, v = (f.randn((4, f.total, h, D)) for h in (8, 2, 2))
+        pos = torch.arange(f.total, dtype=torch.int32, device="cuda").view(1, -1)
+        qs = []
+        for layer in range(4):
+            one, at = f.cache.layer(layer), slice(layer, layer + 1)
+            qs.append(f.P.paged_append(one, f.batch, q[at], k[at], v[at], positions=pos, rope=f.P.Rope()))
+        outs = torch.cat([f.P.paged_attention(f.cache.layer(i), f.batch, qs[i]) for i in range(4)])
+        pools = f.kb.clone(), f.vb.clone()
+        whole = f.P.paged_append(f.cache, f.batch, q, k, v, positions=pos, rope=f.P.Rope())
+        torch.cuda.synchronize()
+        assert torch.equal(torch.cat(qs), whole) and torch.equal(pools[0], f.kb) and torch.equal(pools[1], f.vb)
+        for x, b in ((f.k, f.kb), (f.v, f.vb)):
+            x.copy_(torch.from_numpy(O4.decode(*O4.rows(b.cpu().numpy(), 32))))
+        f.compare(whole, outs)
+        f.compare(whole, f.attend(whole))
+
+
+@pytest.mark.parametrize("new", [1, 4, 40])
+def test_streams_and_two_calls_at_once(torch_cuda, new):
+    """On busy streams that are not the current one, two workspaces, tensors that are dropped at once."""
+    import torch
+    f = Served4((3000, 240, 700), (new,) * 3, 32, "bf16", 2, 8, 2, seed=27)
+    n = 3 * new
+    rows = [f.randn((2, n, h, D)) for h in (8, 2, 2)]
+    want_q = f.P.paged_append(f.cache, f.batch, *rows)
+    want = f.P.paged_attention(f.cache, f.batch, want_q)
+    pools = f.kb.clone(), f.vb.clone()
+    busy = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for side in sides:
+        with torch.cuda.stream(side):
+            for _ in range(10):
+                torch.mm(busy, busy)
+        q = f.P.paged_append(f.cache, f.P.NewTokens(f.cu), *(x.clone() for x in rows), stream=side)
+        got.append((q, f.P.paged_attention(f.cache, f.P.NewTokens(f.cu), q, stream=side)))
+        junk = [torch.full_like(x, 9.0) for x in rows for _ in range(4)]
+    torch.cuda.synchronize()
+    for q, o in got:
+        assert torch.equal(q, want_q) and torch.equal(o, want) and len(junk) == 12
+    assert torch.equal(f.kb, pools[0]) and torch.equal(f.vb, pools[1])
+
+
+@pytest.mark.parametrize("layers,seqs,hq,extra", [(2, 65535, 64, 0), (65535, 2, 2, 1), (2, 65535, 128, 1)])
+def test_limits_of_a_call(torch_cuda, layers, seqs, hq, extra):
+    """As many sequences, or layers, as a call may have.  Every token sees one key, so that its output is that key's value,
+    but for the second token of the last sequence, which sees two equal keys with equal values."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(32)
+    new = torch.ones(seqs, dtype=torch.int64)
+    new[-1] += extra
+    batch = P.NewTokens(torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)]))
+    n = batch.total
+    table = torch.randperm(seqs, generator=gen, device="cuda").to(torch.int32).view(seqs, 1)
+    pool = [torch.full((layers, 1, seqs, 16 * 68), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = P.PagedCache(*pool, table, new.to(torch.int32).cuda(), hq)
+    k, v = (torch.randn((layers, n, 1, D), generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    if extra:
+        k[:, -1], v[:, -1] = k[:, -2], v[:, -2]
+    P.paged_append(cache, batch, None, k, v)
+    rk, rv = P.paged_read(cache, batch)
+    for x, y in ((rk, k), (rv, v)):
+        for layer in range(0, layers, max(layers // 8, 1)):
+            at = torch.randint(0, n, (256,), device="cuda")
+            assert np.array_equal(_f64(x[layer, at, 0]), O4.decode(*O4.encode(_f64(y[layer, at, 0]), "bf16")))
+    q = torch.randn((1, n, hq, D), generator=gen, device="cuda", dtype=torch.bfloat16).expand(layers, -1, -1, -1).contiguous()
+    out = P.paged_attention(cache, batch, q)
+    for layer in range(0, layers, max(layers // 64, 1)):
+        # (a weight rounded to 1, over a sum of it: exact; of two equal ones too)
+        assert torch.equal(out[layer], rv[layer].expand(-1, hq, -1)), layer

@@ -449,3 +449,33 @@ def test_streams(torch_cuda):
         torch.cuda.synchronize()
         assert (out.tolist(), n_out.tolist()) == want and len(junk) == 8
         assert torch.equal(got[0], rows[0]) and torch.equal(got[1], rows[1])
+
+
+def test_limits_of_the_calls(torch_cuda):
+    """65535 sequences."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    rng = np.random.default_rng(6)
+    f = Pages(65535, 16, 100000, 64)
+    f.grow(rng.integers(0, 34, 65535).tolist())
+    f.grow(rng.integers(0, 3, 65535).tolist())
+    f.release(rng.integers(-1, 20, 65535).tolist())
+    f.release([0] * 65535)
+    counts = rng.integers(0, 4, 65535)
+    counts[-3:] = 2
+    p, q, x, u, r = _drafts(counts.tolist(), 60, seed=4)
+    out, n_out = _verify(counts.tolist(), p, q, x, u, r)
+    cu = np.concatenate([[0], np.cumsum(counts)])
+    for s in list(range(0, 65535, 997)) + [65532, 65533, 65534]:
+        a, n = int(cu[s]), int(counts[s])
+        if n == 0:
+            assert n_out[s] == 0
+            continue
+        rows = [t[a:a + n].double().cpu().numpy() for t in (p, q)]
+        want = OS.verify(*rows, x[a:a + n].tolist(), u[a:a + n].tolist(), float(r[s]))
+        assert out[a:a + n] == want + [-1] * (n - len(want)) and n_out[s] == len(want)
+    p = torch.zeros((2, 1 << 24), device="cuda")
+    p[0, (1 << 24) - 1], p[1, (1 << 24) - 2] = 1.0, 1.0
+    x = torch.tensor([(1 << 24) - 1, 0], dtype=torch.int32, device="cuda")
+    z = torch.zeros(2, device="cuda")
+    assert _verify((2,), p, None, x, z, z[:1]) == ([(1 << 24) - 1, (1 << 24) - 2], [2])
