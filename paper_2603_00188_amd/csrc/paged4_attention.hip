@@ -46,8 +46,6 @@ constexpr int kKeys = 16 * kRuns;  // of a tile
 // chunk, or four rows' 4 apart, take all banks.  Then the scales, run by run.
 constexpr int kKPart = 1024 + 16, kVPart = 1024 + 64;
 constexpr int kVAt = 4 * kKPart, kScalesAt = kVAt + 4 * kVPart, kSlot = kScalesAt + 2 * kKeys * 4;
-constexpr int kDmas = 10;     // instructions of a tile
-constexpr int kWindow = 512;  // entries of the page table that a wave holds
 constexpr float kLazy = 8.0f, kFar = 960.0f;
 
 // 16 or 4 bytes per lane, each from an address of its own, to LDS address `to` + 16 lane or
@@ -64,16 +62,21 @@ __device__ inline V lds_read(uint32_t at) {
   return *reinterpret_cast<const __attribute__((address_space(3))) V*>((uintptr_t)at);
 }
 
-// 16 NG rows to an item.  Of 48 or 64 rows the sums and queries take more registers than two
-// waves of a SIMD have; one wave has three tiles under way instead of one.
-template <typename T, int NG>
-__global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kernel(PagedAttnArgs a) {
+// 16 NG HALVES rows to an item.  Of more than 32 rows the sums and queries take more
+// registers than two waves of a SIMD have: with HALVES = 2 the two waves of a SIMD, w and
+// w + 4, take half of the rows each of the same tiles, one of them fetching K and the other
+// V, with three tiles under way.  (One wave with all of them, products and vector work in
+// turn, took 187 us where this takes BOTH.)
+template <typename T, int NG, int HALVES>
+__global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
-  constexpr int NT = kWaves * 64, kRows = 16 * NG, kDepth = NG <= 2 ? 2 : 4;
+  constexpr int NT = kWaves * 64 * HALVES, kRows = 16 * NG * HALVES, kDepth = HALVES == 1 ? 2 : 4;
+  constexpr int kDmas = HALVES == 1 ? 10 : 5;        // instructions of a wave to a tile
+  constexpr int kWindow = HALVES == 1 ? 512 : 256;  // entries of the page table that a wave holds
   __shared__ float sm_m[kWaves][kRows], sm_l[kWaves][kRows];
   __shared__ __align__(1024) uint8_t sm_ring[kWaves][kDepth][kSlot];  // (the waves' sums, once an item is done)
-  __shared__ int32_t sm_pages[kWaves][kWindow];
+  __shared__ int32_t sm_pages[kWaves * HALVES][kWindow];
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
   static_assert(sizeof(sm_ring) >= sizeof(float) * kWaves * 16 * kHeadDim);
   const PagedDev& c = a.c;
@@ -84,12 +87,13 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
   PagedItem it = plan.find(x);
   if (it.start >= y) return;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = wave8 % kWaves, half = HALVES == 1 ? 0 : wave8 / kWaves;
   const int col = lane & 15, quad = lane >> 4;
   const int32_t in_page = (1 << c.page_shift) - 1, scales_at = (in_page + 1) * kCodes4;
   const uint32_t page_bytes = uint32_t(in_page + 1) * kRow4;
   const uint32_t ring = uint32_t(reinterpret_cast<uintptr_t>(sm_ring[wave]));
-  const uint32_t window = uint32_t(reinterpret_cast<uintptr_t>(sm_pages[wave]));
+  const uint32_t window = uint32_t(reinterpret_cast<uintptr_t>(sm_pages[wave8]));
   const int64_t v_off = reinterpret_cast<int64_t>(c.v) - reinterpret_cast<int64_t>(c.k);
   // DMA: lane l has run l / 16, row 4 d + l / 4 % 4 of it and chunk l % 4, or its scales' row l % 16.
   const uint32_t codes_from = uint32_t((16 * quad & in_page) + (lane >> 2 & 3)) * kCodes4 + (lane & 3) * 16;
@@ -118,6 +122,8 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
     };
     const int32_t first = __builtin_amdgcn_readfirstlane(k0 + kKeys * wave);  // this wave's first key
     const int32_t steps = first < k1 ? (k1 - first + kKeys * kWaves - 1) / (kKeys * kWaves) : 0;
+    // (the waves of HALVES = 2 go in step)
+    const int32_t rounds = HALVES == 1 ? steps : __builtin_amdgcn_readfirstlane(max((k1 - k0 + kKeys * kWaves - 1) / (kKeys * kWaves), 0));
 
     // --- tiles into the ring ---
     int32_t held = -kWindow;  // first entry in the window
@@ -146,12 +152,16 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
       const uint8_t* const at = unit_at + uint64_t(page) * page_bytes;
       const uint8_t* const codes = at + (uint32_t(j0 & in_page) * kCodes4 + codes_from);
       const uint8_t* const scales = at + (uint32_t(j0 & in_page) * 4 + scales_from);
+      if (HALVES == 1 || half == 0) {
 #pragma unroll
-      for (int d = 0; d < 4; ++d) dma16_each(codes + d * 4 * kCodes4, to + d * kKPart);
-      dma4_each(scales, to + kScalesAt);
+        for (int d = 0; d < 4; ++d) dma16_each(codes + d * 4 * kCodes4, to + d * kKPart);
+        dma4_each(scales, to + kScalesAt);
+      }
+      if (HALVES == 1 || half == 1) {
 #pragma unroll
-      for (int d = 0; d < 4; ++d) dma16_each(codes + v_off + d * 4 * kCodes4, to + kVAt + d * kVPart);
-      dma4_each(scales + v_off, to + kScalesAt + kKeys * 4);
+        for (int d = 0; d < 4; ++d) dma16_each(codes + v_off + d * 4 * kCodes4, to + kVAt + d * kVPart);
+        dma4_each(scales + v_off, to + kScalesAt + kKeys * 4);
+      }
     };
 #pragma unroll 1
     for (int i = 0; i < min(steps, kDepth - 1); ++i) fetch(i);
@@ -160,7 +170,7 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
     int32_t sees[NG];  // keys that this lane's rows see
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
-      const int32_t r = min(16 * ng + col, rows - 1);
+      const int32_t r = min(16 * (NG * half + ng) + col, rows - 1);
       const uint16_t* p = a.q + place(r) * kHeadDim;
       sees[ng] = it.cached + tok0 + 1 + (a.parts > 1 ? 0 : r / c.group);
 #pragma unroll
@@ -168,7 +178,7 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
     }
     float m_ref[NG];
     f32x4_t l[NG];     // sums of the weights of rows 4 quad + r, on every column
-    f32x4_t o[NG][8];  // O[row 16 ng + 4 quad + r][dimension 8 col + db]
+    f32x4_t o[NG][8];  // O[row 16 (NG half + ng) + 4 quad + r][dimension 8 col + db]
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
       m_ref[ng] = -FLT_MAX;  // (finite: no difference of infinities while no key was seen)
@@ -317,10 +327,12 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
     for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) asm volatile("" : "+v"(qb[ng][kk]));
-    for (int32_t i = 0; i < steps; ++i) {
-      // tile i has landed: all but the kDepth - 2 behind it (near the end: all)
+    for (int32_t i = 0; i < rounds; ++i) {
+      // this wave's part of tile i has landed: all but the kDepth - 2 behind it (near the end: all)
       if (i + kDepth - 1 <= steps) wait_vmcnt<kDmas * (kDepth - 2)>();
       else wait_vmcnt<0>();
+      if (HALVES == 2) barrier_lds();  // and the other wave's, which is done with tile i - 1
+      if (HALVES == 2 && i >= steps) continue;
       if (i + kDepth - 1 < steps) fetch(i + kDepth - 1);  // in place of tile i - 1, whose values have been used
       step(first + i * (kKeys * kWaves), ring + (i & (kDepth - 1)) * kSlot);
     }
@@ -343,26 +355,28 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
     }
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
-      if (lane < 16) sm_m[wave][16 * ng + lane] = m_ref[ng];
+      const int row = 16 * (NG * half + ng);
+      if (lane < 16) sm_m[wave][row + lane] = m_ref[ng];
       if (col == 0)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sm_l[wave][16 * ng + 4 * quad + r] = l[ng][r];
+        for (int r = 0; r < 4; ++r) sm_l[wave][row + 4 * quad + r] = l[ng][r];
     }
 
     // Merge the waves, sixteen rows at a time (a wave that saw no key has weights of 0).
     float(&sm_o)[kWaves][16][kHeadDim] = *reinterpret_cast<float(*)[kWaves][16][kHeadDim]>(&sm_ring[0][0][0]);
     const int64_t slot = paged_slot(blockIdx.x, plan.share, it.start) * kRows;
 #pragma unroll
-    for (int ng = 0; ng < NG; ++ng) {
-      if (16 * ng >= rows) break;
+    for (int block = 0; block < NG * HALVES; ++block) {
+      if (16 * block >= rows) break;
       __syncthreads();  // the rings, or the last rows' sums, have been read
+      if (half == block / NG)
 #pragma unroll
-      for (int db = 0; db < 8; ++db)
+        for (int db = 0; db < 8; ++db)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sm_o[wave][4 * quad + r][col * 8 + db] = o[ng][db][r];
+          for (int r = 0; r < 4; ++r) sm_o[wave][4 * quad + r][col * 8 + db] = o[block % NG][db][r];
       __syncthreads();
-      for (int e = threadIdx.x; e < min(rows - 16 * ng, 16) * (kHeadDim / 2); e += NT) {
-        const int h = e / (kHeadDim / 2), dim = e % (kHeadDim / 2) * 2, row = 16 * ng + h;
+      for (int e = threadIdx.x; e < min(rows - 16 * block, 16) * (kHeadDim / 2); e += NT) {
+        const int h = e / (kHeadDim / 2), dim = e % (kHeadDim / 2) * 2, row = 16 * block + h;
         float M = -FLT_MAX;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w][row]);
@@ -396,11 +410,9 @@ __global__ __launch_bounds__(kWaves * 64, NG <= 2 ? 2 : 1) void paged4_few_kerne
 
 template <typename T>
 hipError_t few(const PagedAttnArgs& a, hipStream_t stream) {
-  const dim3 grid(a.shares), block(kWaves * 64);
-  if (a.rows == 16) hipLaunchKernelGGL((paged4_few_kernel<T, 1>), grid, block, 0, stream, a);
-  else if (a.rows == 32) hipLaunchKernelGGL((paged4_few_kernel<T, 2>), grid, block, 0, stream, a);
-  else if (a.rows == 48) hipLaunchKernelGGL((paged4_few_kernel<T, 3>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((paged4_few_kernel<T, 4>), grid, block, 0, stream, a);
+  if (a.rows == 16) hipLaunchKernelGGL((paged4_few_kernel<T, 1, 1>), dim3(a.shares), dim3(kWaves * 64), 0, stream, a);
+  else if (a.rows == 32) hipLaunchKernelGGL((paged4_few_kernel<T, 2, 1>), dim3(a.shares), dim3(kWaves * 64), 0, stream, a);
+  else hipLaunchKernelGGL((paged4_few_kernel<T, 2, 2>), dim3(a.shares), dim3(kWaves * 128), 0, stream, a);
   return hipGetLastError();
 }
 

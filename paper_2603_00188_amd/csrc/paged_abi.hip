@@ -162,7 +162,7 @@ AttnPlan attn_plan(const stlite_paged* c) {
   p.decode = most <= 1 || (four && few_rows <= most_rows);
   if (p.decode) {
     p.tokens = int32_t(std::max<int64_t>(most, 1));
-    p.rows = int32_t(few_rows <= 16 ? 16 : few_rows <= 32 || few_rows > most_rows ? 32 : ceil_div(few_rows, 16) * 16);
+    p.rows = int32_t(few_rows <= 16 ? 16 : few_rows <= 32 || few_rows > most_rows ? 32 : 64);
     p.parts = int32_t(ceil_div(group, p.rows));
     items *= p.parts * live;
     // Over a 4-bit pool a share's round is 256 keys and a key takes a quarter of the time.
