@@ -149,16 +149,16 @@ AttnPlan attn_plan(const stlite_paged* c) {
     live += n > 0;
   }
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
-  // A few tokens over a 4-bit pool by the kernel of one: up to 32 rows always, up to 48 or
-  // 64, which leave one wave to a SIMD, where the sequences may have keys enough.  Several
-  // tokens' kernel / this, 28 heads over 4, 16 sequences in 2 layers: 5 tokens (35 rows)
-  // behind up to 6000 keys 55 / 51 us, 40000 310 / 187; 9 (63) 58 / 62, 16000 136 / 118; 8
-  // of 16 heads over 2 (64) behind up to 40000 170 / 135; one sequence in 8 units behind
-  // 3000, 40 rows 21 / 23, 60 22 / 27.  One token of 40 heads of a kv head, two parts of
-  // 32 / one of 48: 16 sequences of 60000 72 / 67, 8 of 8000 28 / 30; of 64 heads 72 / 79.
+  // A few tokens over a 4-bit pool by the kernel of one: up to 32 rows always, up to 64,
+  // whose queries and sums take two waves of a SIMD, where the sequences may have keys
+  // enough.  Several tokens' kernel / this, 28 heads over 4, 16 sequences in 2 layers: 5
+  // tokens (35 rows) behind up to 6000 keys 55 / 47 us, 40000 310 / 180; 9 (63) 58 / 52,
+  // 16000 135 / 96; 8 of 16 heads over 2 (64) behind 40000 170 / 109; one sequence in 8
+  // units behind 3000, 40 rows 21 / 22, 60 22 / 24.  One token of 40 heads of a kv head, two
+  // parts of 32 / one: 8 sequences of 8000 27.5 / 28.8, 16 of 60000 73 / 63; of 64 heads 73 / 65.
   const bool four = is_four(c);
   const int64_t few_rows = std::max<int64_t>(most, 1) * group, keys = items * live * c->max_len;
-  const int64_t most_rows = !four || keys < (1 << 18) ? 32 : keys < (1 << 20) || most <= 1 ? 48 : 64;
+  const int64_t most_rows = four && keys >= (1 << 18) ? 64 : 32;
   p.decode = most <= 1 || (four && few_rows <= most_rows);
   if (p.decode) {
     p.tokens = int32_t(std::max<int64_t>(most, 1));
@@ -168,13 +168,16 @@ AttnPlan attn_plan(const stlite_paged* c) {
     // Over a 4-bit pool a share's round is 256 keys and a key takes a quarter of the time.
     // With fewer items than CUs one work-group to each, 256 / 512 shares: a step over 30105
     // tokens (112 items) 80.3 / 82.3 us, one layer over 150528 (4) 25.6 / 27.7, four drafted
-    // tokens in each of 16 sequences in 8 units (128) 36.9 / 40.0; with more, two, which
-    // begin and end at different times: 64 sequences of up to 8000 in 32 units (2048) 229 /
-    // 209, drafted tokens in 16 in 16 (256) 59.7 / 54.2.  min_share 64 / 256: 678 keys of a
-    // layer 12.7 / 11.8, a layer over 30105 21 / 17.8.  item_cost 128 / 256 / 512: one layer
-    // over 150528 29.4 / 28.7 / 27.6, the 2048 items 214 / 212 / 210.
-    // (Of 48 and 64 rows one work-group is all that a CU holds.)
-    p.shares = four && (items < 256 || p.rows > 32) ? 256 : 512;
+    // tokens in each of 16 sequences of up to 6000 in 8 units (128) 36.9 / 40.0; with more,
+    // two, which begin and end at different times: 64 sequences of up to 8000 in 32 units
+    // (2048) 229 / 209, drafted tokens in 16 in 16 (256) 59.7 / 54.2.  Two also where 32
+    // rows have many keys, since one's products run under the other's vector work: the
+    // drafted tokens behind up to 40000 130 / 121.  (Of 64 rows a CU holds no more than
+    // one.)  min_share 64 / 256: 678 keys of a layer 12.7 / 11.8, a layer over 30105 21 /
+    // 17.8.  item_cost 128 / 256 / 512: one layer over 150528 29.4 / 28.7 / 27.6, the 2048
+    // items 214 / 212 / 210.
+    const bool one = p.rows > 32 || (items < 256 && (p.rows < 32 || keys < (1 << 20)));
+    p.shares = four && one ? 256 : 512;
     p.min_share = four ? 256 : 64;
     p.item_cost = four ? 512 : 64;
   } else {

@@ -64,7 +64,8 @@ class Pages:
 
 @pytest.mark.parametrize("seqs,page,n_pages,max_len,most", [
     (1, 16, 3, 40, 25), (3, 16, 40, 300, 100), (64, 16, 500, 400, 90), (64, 256, 30, 2000, 300), (1000, 16, 3000, 160, 60),
-    (1023, 32, 400, 90, 20), (1024, 16, 5000, 300, 40), (1025, 16, 700, 100, 3), (2500, 16, 9000, 256, 70)])
+    (1023, 32, 400, 90, 20), (1024, 16, 5000, 300, 40), (1025, 16, 700, 100, 3), (2500, 16, 9000, 256, 70),
+    (40, 16, 65537, 20000, 2000), (1500, 16, 70000, 3000, 700)])
 def test_pages(torch_cuda, seqs, page, n_pages, max_len, most):
     """Rounds of growing, ending, cutting and resuming, with enough pages and with too few."""
     _log(f"pages: {seqs} sequences, {n_pages} pages of {page}")
