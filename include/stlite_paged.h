@@ -91,7 +91,7 @@ typedef struct stlite_paged {
   int64_t total_new;         /* = cu_new[n_seqs] */
   void* k;                   /* the pools, 16-byte aligned */
   void* v;
-  int32_t* page_table;       /* device [n_seqs][max_pages]; only grow and release write it */
+  const int32_t* page_table; /* device [n_seqs][max_pages] */
   int32_t* seq_lens;         /* device [n_seqs]; compact, grow, release and verify write it */
   const int32_t* cu_new;     /* device [n_seqs+1], prefix sums of the new tokens, cu_new[0] = 0 */
   const int32_t* h_cu_new;   /* host mirror of cu_new */
@@ -211,12 +211,14 @@ stlite_status stlite_paged_read(const stlite_paged* c, uint16_t* k_out, uint16_t
  * holds (the next one to be given out is the last), and held[s] counts the entries of
  * page_table's row s, from its first, that sequence s holds a page in.  To begin with:
  * pages every index of the pool, n_free = n_pages, held and seq_lens 0.  No page may be
- * in the list and in a row's held entries, or in two rows', at once.
+ * in the list and in a row's held entries, or in two rows', at once.  page_table is the
+ * cache's, which grow and release write.
  */
 typedef struct stlite_free_pages {
   int32_t* pages;  /* device [n_pages] */
   int32_t* n_free; /* device [1] */
   int32_t* held;   /* device [n_seqs] */
+  int32_t* page_table; /* = the cache's page_table */
 } stlite_free_pages;
 
 /*

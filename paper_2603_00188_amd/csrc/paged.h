@@ -10,7 +10,7 @@ namespace stlite {
 struct PagedDev {
   uint16_t* k;  // [units][n_pages][page][d]; of a 4-bit pool: [units][n_pages][page * 68 bytes]
   uint16_t* v;
-  int32_t* page_table;  // [n_seqs][max_pages]; only growing and releasing write it
+  const int32_t* page_table;  // [n_seqs][max_pages]
   int32_t* seq_lens;          // [n_seqs], new tokens included
   const int32_t* cu_new;      // [n_seqs + 1]
   int32_t n_layers, n_q_heads, n_kv_heads, n_units, group;
@@ -40,6 +40,7 @@ struct PagedPagesArgs {
   int32_t* free_pages;  // [n_pages]
   int32_t* n_free;      // [1]
   int32_t* held;        // [n_seqs]
+  int32_t* page_table;  // the cache's
   int32_t* slots;       // growing: [total_new], nullable
   const int32_t* lens;  // releasing: [n_seqs], nullable
 };

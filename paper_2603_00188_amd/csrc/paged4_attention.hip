@@ -65,13 +65,14 @@ __device__ inline V lds_read(uint32_t at) {
 // 16 NG HALVES rows to an item.  Of more than 32 rows the sums and queries take more
 // registers than two waves of a SIMD have: with HALVES = 2 the two waves of a SIMD, w and
 // w + 4, take half of the rows each of the same tiles, one of them fetching K and the other
-// V, with three tiles under way.  (One wave with all of them, products and vector work in
-// turn, took 134 us where this takes 109.)
+// V.  (One wave with all of them, products and vector work in turn, took 134 us where this
+// takes 106.)  One tile is under way while another is worked on: with three 81 us became 91
+// for 16 rows, 106 became 109 for 64.
 template <typename T, int NG, int HALVES>
 __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(PagedAttnArgs a) {
   typedef Elem<T> E;
   typedef typename E::x8 x8;
-  constexpr int NT = kWaves * 64 * HALVES, kRows = 16 * NG * HALVES, kDepth = HALVES == 1 ? 2 : 4;
+  constexpr int NT = kWaves * 64 * HALVES, kRows = 16 * NG * HALVES, kDepth = 2;
   constexpr int kDmas = HALVES == 1 ? 10 : 5;        // instructions of a wave to a tile
   constexpr int kWindow = HALVES == 1 ? 512 : 256;  // entries of the page table that a wave holds
   __shared__ float sm_m[kWaves][kRows], sm_l[kWaves][kRows];

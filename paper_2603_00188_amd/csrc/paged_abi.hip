@@ -152,10 +152,10 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // A few tokens over a 4-bit pool by the kernel of one: up to 32 rows always, up to 64,
   // whose queries and sums take two waves of a SIMD, where the sequences may have keys
   // enough.  Several tokens' kernel / this, 28 heads over 4, 16 sequences in 2 layers: 5
-  // tokens (35 rows) behind up to 6000 keys 55 / 47 us, 40000 310 / 180; 9 (63) 58 / 52,
-  // 16000 135 / 96; 8 of 16 heads over 2 (64) behind 40000 170 / 109; one sequence in 8
+  // tokens (35 rows) behind up to 6000 keys 55 / 45 us, 40000 310 / 176; 9 (63) 58 / 49,
+  // 16000 135 / 91; 8 of 16 heads over 2 (64) behind 40000 170 / 106; one sequence in 8
   // units behind 3000, 40 rows 21 / 22, 60 22 / 24.  One token of 40 heads of a kv head, two
-  // parts of 32 / one: 8 sequences of 8000 27.5 / 28.8, 16 of 60000 73 / 63; of 64 heads 73 / 65.
+  // parts of 32 / one: 8 sequences of 8000 27.5 / 28.8, 16 of 60000 73 / 61; of 64 heads 73 / 65.
   const bool four = is_four(c);
   const int64_t few_rows = std::max<int64_t>(most, 1) * group, keys = items * live * c->max_len;
   const int64_t most_rows = four && keys >= (1 << 18) ? 64 : 32;
@@ -257,6 +257,7 @@ bool rows_meet(const stlite_paged* c, const stlite_rows* r, int64_t heads, const
 stlite_status check_pages(const stlite_paged* c, const stlite_free_pages* f, const void* other, size_t other_bytes) {
   if (!f || !f->pages || !f->n_free || !f->held)
     return fail(STLITE_ERR_INVALID_ARG, "pages, n_free and held must be non-NULL");
+  if (f->page_table != c->page_table) return fail(STLITE_ERR_INVALID_ARG, "page_table is not the cache's");
   const struct {
     const void* p;
     size_t bytes;
@@ -533,6 +534,7 @@ stlite_status stlite_paged_grow(const stlite_paged* c, const stlite_free_pages* 
   a.free_pages = pages->pages;
   a.n_free = pages->n_free;
   a.held = pages->held;
+  a.page_table = pages->page_table;
   a.slots = slots;
   return hip_status(launch_paged_grow(a, static_cast<hipStream_t>(stream)), "paged_grow launch");
 }
@@ -547,6 +549,7 @@ stlite_status stlite_paged_release(const stlite_paged* c, const stlite_free_page
   a.free_pages = pages->pages;
   a.n_free = pages->n_free;
   a.held = pages->held;
+  a.page_table = pages->page_table;
   a.lens = lens;
   return hip_status(launch_paged_release(a, static_cast<hipStream_t>(stream)), "paged_release launch");
 }

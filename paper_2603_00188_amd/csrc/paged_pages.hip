@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void paged_grow_kernel(PagedPagesArgs a) 
       __syncthreads();
       for (int64_t f = first; f < here; f += stride) {
         const int t = owner(sm_before, f);
-        c.page_table[int64_t(base + t) * c.max_pages + sm_held[t] + (f - sm_before[t])] = a.free_pages[n_free - 1 - (carry + f)];
+        a.page_table[int64_t(base + t) * c.max_pages + sm_held[t] + (f - sm_before[t])] = a.free_pages[n_free - 1 - (carry + f)];
       }
       if (a.slots) {
         const int32_t end = c.cu_new[min(base + kThreads, c.n_seqs)];
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void paged_grow_kernel(PagedPagesArgs a) 
           const int32_t entry = int32_t(at >> c.page_shift), more = entry - sm_held[t];
           int32_t page = -1;
           if (sm_len[t] >= 0)
-            page = more < 0 ? c.page_table[int64_t(base + t) * c.max_pages + entry]
+            page = more < 0 ? a.page_table[int64_t(base + t) * c.max_pages + entry]
                             : a.free_pages[n_free - 1 - (carry + sm_before[t] + more)];
           a.slots[i] = page >= 0 && page < c.n_pages ? (page << c.page_shift) + int32_t(at & ((1 << c.page_shift) - 1)) : -1;
         }
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(kThreads) void paged_release_kernel(PagedPagesArgs 
     __syncthreads();
     for (int64_t f = int64_t(blockIdx.x) * kThreads + threadIdx.x; f < all; f += int64_t(gridDim.x) * kThreads) {
       const int t = owner(sm_before, f);
-      int32_t* entry = c.page_table + int64_t(base + t) * c.max_pages + sm_kept[t] + (f - sm_before[t]);
+      int32_t* entry = a.page_table + int64_t(base + t) * c.max_pages + sm_kept[t] + (f - sm_before[t]);
       const int64_t to = n_free + total - 1 - (carry + f);
       if (to < c.n_pages) a.free_pages[to] = *entry;  // (more than there are pages: the list is full)
       *entry = -1;

@@ -387,7 +387,7 @@ class FreePages(_Fixed):
     """The pages of a pool that no sequence holds: ``pages`` int32 [n_pages], of which the first ``n_free`` [1] are free,
     and ``held`` [n_seqs], how many entries of its row of the page table each sequence holds."""
 
-    _fixed = ("pages", "n_free", "held", "c")
+    _fixed = ("pages", "n_free", "held", "_c")
 
     def __init__(self, pages, n_free, held):
         if pages.dim() != 1 or held.dim() != 1:
@@ -396,7 +396,7 @@ class FreePages(_Fixed):
         _is(n_free, "n_free", (1,), torch.int32, pages.device)
         _is(held, "held", held.shape, torch.int32, pages.device)
         self.pages, self.n_free, self.held = pages, n_free, held
-        self.c = _CFreePages(pages.data_ptr(), n_free.data_ptr(), held.data_ptr())
+        self._c = _CFreePages(pages.data_ptr(), n_free.data_ptr(), held.data_ptr(), None)
 
     def __reduce__(self):  # a copy has addresses of its own
         return FreePages, (self.pages, self.n_free, self.held)
@@ -412,7 +412,9 @@ class FreePages(_Fixed):
         for t, name, shape in ((self.pages, "pages", (cache.n_pages,)), (self.held, "held", (cache.n_seqs,))):
             if t.shape != shape or t.device != cache.device:
                 raise ValueError(f"the free pages' {name} is {tuple(t.shape)} on {t.device}, the cache's {shape} on {cache.device}")
-        return ctypes.byref(self.c)
+        c = _CFreePages.from_buffer_copy(self._c)
+        c.page_table = cache.page_table.data_ptr()
+        return ctypes.byref(c)
 
 
 def paged_grow(cache: PagedCache, pages: FreePages, batch: NewTokens, slots=None, stream=None) -> None:

@@ -67,7 +67,8 @@ class _CPaged(ctypes.Structure):
 
 
 class _CFreePages(ctypes.Structure):
-    _fields_ = [("pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("held", ctypes.c_void_p)]
+    _fields_ = [("pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p)]
 
 
 class _CVerify(ctypes.Structure):

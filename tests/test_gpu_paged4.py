@@ -267,7 +267,16 @@ def test_decode_many_short_sequences(torch_cuda):
     f.compare(q, f.attend(q))
 
 
-@pytest.mark.parametrize("lens,new,page,dtype,layers,hq,hk", EXTEND)
+# More rows than the kernel of few rows takes, where that of several tokens may go wrong too.
+MANY_ROWS = [
+    ((3, 0, 2), (5, 3, 9), 16, "bf16", 1, 20, 1),              # shorter than their new tokens
+    ((37, 64, 65), (5, 1, 0), 16, "fp16", 2, 40, 2),           # a plain step and an idle sequence beside
+    ((9000, 40, 3000, 10), (3, 0, 40, 1), 32, "bf16", 1, 28, 1),  # few items, each in many parts
+    ((6000,), (3,), 16, "fp16", 1, 128, 4),                    # few rows over a long cache: joined
+]
+
+
+@pytest.mark.parametrize("lens,new,page,dtype,layers,hq,hk", EXTEND + MANY_ROWS)
 def test_extend(torch_cuda, lens, new, page, dtype, layers, hq, hk):
     _log(f"paged extend, 4 bits, lens {lens} new {new} page {page} {dtype} {layers} x {hq}/{hk}")
     f = Served4(lens, new, page, dtype, layers, hq, hk, seed=3, fill=float("nan"))
@@ -293,17 +302,18 @@ def test_extend_many_sequences(torch_cuda):
     rng = np.random.default_rng(4)
     new = rng.integers(0, 4, 1100)
     lens = [int(n + rng.integers(0, 90)) for n in new]
-    f = Served4(lens, new.tolist(), 16, "fp16", 1, 2, 1, fill=float("nan"))
-    q = f.randn((1, f.total, 2, D))
-    f.compare(q, f.attend(q))
+    for heads in (2, 24):
+        f = Served4(lens, new.tolist(), 16, "fp16", 1, heads, 1, fill=float("nan"))
+        q = f.randn((1, f.total, heads, D))
+        f.compare(q, f.attend(q))
 
 
 @pytest.mark.parametrize("tiles", [1, 2, 7, 8, 9, 10, 11, 17, 25])
 def test_extend_of_few_and_many_tiles(torch_cuda, tiles):
     """Caches around the eight tiles that are fetched ahead, in pages that end inside a tile and behind it."""
-    for page in (16, 128):
-        f = Served4((64 * tiles - 3, 64 * tiles, 64 * tiles + 1), (2, 3, 2), page, "bf16", 1, 7, 1, seed=46, fill=float("nan"))
-        q = f.randn((1, f.total, 7, D), 1.5)
+    for page, heads in ((16, 7), (128, 7), (16, 40), (128, 40)):
+        f = Served4((64 * tiles - 3, 64 * tiles, 64 * tiles + 1), (2, 3, 2), page, "bf16", 1, heads, 1, seed=46, fill=float("nan"))
+        q = f.randn((1, f.total, heads, D), 1.5)
         f.compare(q, f.attend(q))
 
 
@@ -489,7 +499,7 @@ def test_pages_out_of_range_are_left_out(torch_cuda, new, dtype):
 
 
 def test_lengths_are_cut_to_the_bounds(torch_cuda):
-    for new in (1, 4):
+    for new in (1, 4, 30):
         f = Served4((64, 48, 30), (new,) * 3, 16, "bf16", 1, 4, 1, seed=8)
         q = f.randn((1, f.total, 4, D))
         f.lens = [64, 2 ** 31 - 1, -7]

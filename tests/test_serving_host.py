@@ -116,7 +116,7 @@ def test_drafts_follow_the_target():
 # ---------------------------------------------------------------------------
 
 def _pages(**kw):
-    f = dict(pages=BIG, n_free=BIG + 4096, held=BIG + 8192)
+    f = dict(pages=BIG, n_free=BIG + 4096, held=BIG + 8192, page_table=FAKE)
     f.update(kw)
     return ctypes.byref(S._CFreePages(**f))
 
@@ -160,18 +160,24 @@ def test_aliases_of_a_4_bit_pool():
 
 @needs_lib
 def test_free_pages_rejections():
-    lib, f = S.load(), Fake(page_table=BIG + (1 << 20), seq_lens=BIG + (1 << 21), cu_new=BIG + (1 << 22))
+    lib, table = S.load(), BIG + (1 << 20)
+    f = Fake(page_table=table, seq_lens=BIG + (1 << 21), cu_new=BIG + (1 << 22))
     for bad in (dict(pages=None), dict(n_free=None), dict(held=None)):
-        assert lib.stlite_paged_grow(f.ref, _pages(**bad), None, None) == S.ERR_INVALID_ARG and "non-NULL" in _err()
-        assert lib.stlite_paged_release(f.ref, _pages(**bad), None, None) == S.ERR_INVALID_ARG
+        assert lib.stlite_paged_grow(f.ref, _pages(page_table=table, **bad), None, None) == S.ERR_INVALID_ARG and "non-NULL" in _err()
+        assert lib.stlite_paged_release(f.ref, _pages(page_table=table, **bad), None, None) == S.ERR_INVALID_ARG
     assert lib.stlite_paged_grow(f.ref, None, None, None) == S.ERR_INVALID_ARG
-    for bad in (dict(n_free=BIG + 76), dict(held=BIG + 4096), dict(pages=BIG + (1 << 20) + 36), dict(held=BIG + (1 << 21)),
+    for other in (None, table + 4):
+        assert lib.stlite_paged_grow(f.ref, _pages(page_table=other), None, None) == S.ERR_INVALID_ARG and "page_table" in _err()
+        assert lib.stlite_paged_release(f.ref, _pages(page_table=other), None, None) == S.ERR_INVALID_ARG and "page_table" in _err()
+    for bad in (dict(n_free=BIG + 76), dict(held=BIG + 4096), dict(pages=table + 36), dict(held=BIG + (1 << 21)),
                 dict(n_free=BIG + (1 << 22) + 8)):
-        assert lib.stlite_paged_grow(f.ref, _pages(**bad), None, None) == S.ERR_INVALID_ARG and "overlap" in _err()
-        assert lib.stlite_paged_release(f.ref, _pages(**bad), None, None) == S.ERR_INVALID_ARG and "overlap" in _err()
-    assert lib.stlite_paged_grow(f.ref, _pages(), BIG + 8192 + 4, None) == S.ERR_INVALID_ARG and "overlap" in _err()
-    assert lib.stlite_paged_release(f.ref, _pages(), BIG + (1 << 21) + 4, None) == S.ERR_INVALID_ARG and "overlap" in _err()
-    assert lib.stlite_paged_grow(f.ref, _pages(held=FAKE + 64), None, None) == S.ERR_INVALID_ARG and "pool" in _err()
+        p = _pages(page_table=table, **bad)
+        assert lib.stlite_paged_grow(f.ref, p, None, None) == S.ERR_INVALID_ARG and "overlap" in _err()
+        assert lib.stlite_paged_release(f.ref, p, None, None) == S.ERR_INVALID_ARG and "overlap" in _err()
+    p = _pages(page_table=table)
+    assert lib.stlite_paged_grow(f.ref, p, BIG + 8192 + 4, None) == S.ERR_INVALID_ARG and "overlap" in _err()
+    assert lib.stlite_paged_release(f.ref, p, BIG + (1 << 21) + 4, None) == S.ERR_INVALID_ARG and "overlap" in _err()
+    assert lib.stlite_paged_grow(f.ref, _pages(page_table=table, held=FAKE + 64), None, None) == S.ERR_INVALID_ARG and "pool" in _err()
 
 
 class Drafts:
@@ -278,7 +284,7 @@ def test_binding_refusals():
         P.paged_read(c, b)
     f = P.FreePages.of(c)
     assert f.pages.tolist() == [4, 3, 2, 1, 0] and f.n_free.tolist() == [5] and f.held.tolist() == [0, 0, 0]
-    assert copy.deepcopy(f).c.pages != f.c.pages
+    assert copy.deepcopy(f)._c.pages != f._c.pages
     with pytest.raises(AttributeError):
         f.pages = f.pages.clone()
     for bad in ((f.pages.long(), f.n_free, f.held), (f.pages, f.n_free[0], f.held), (f.pages, f.n_free, f.held.float()),
