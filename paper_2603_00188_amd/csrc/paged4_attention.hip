@@ -79,7 +79,6 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
   __shared__ __align__(1024) uint8_t sm_ring[kWaves][kDepth][kSlot];  // (the waves' sums, once an item is done)
   __shared__ int32_t sm_pages[kWaves * HALVES][kWindow];
   __shared__ typename PagedPlan<NT>::Shared sm_plan;
-  static_assert(sizeof(sm_ring) >= sizeof(float) * kWaves * 16 * kHeadDim);
   const PagedDev& c = a.c;
   PagedPlan<NT> plan(a, sm_plan);
   int64_t x = int64_t(blockIdx.x) * plan.share;
@@ -363,21 +362,30 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
         for (int r = 0; r < 4; ++r) sm_l[wave][row + 4 * quad + r] = l[ng][r];
     }
 
-    // Merge the waves, sixteen rows at a time (a wave that saw no key has weights of 0).
-    float(&sm_o)[kWaves][16][kHeadDim] = *reinterpret_cast<float(*)[kWaves][16][kHeadDim]>(&sm_ring[0][0][0]);
+    // Merge the waves, as many rows at a time as their rings hold (a wave that saw no key has
+    // weights of 0).
+    constexpr int kAtOnce = 16 * (NG * HALVES < 2 ? 1 : 2);
+    static_assert(sizeof(sm_ring[0]) >= sizeof(float) * kAtOnce * kHeadDim && sizeof(sm_ring[0]) % sizeof(float) == 0);
+    const auto sum_at = [&](int w, int row, int dim) -> float& {
+      return *reinterpret_cast<float*>(&sm_ring[w][0][0] + (row * kHeadDim + dim) * int(sizeof(float)));
+    };
     const int64_t slot = paged_slot(blockIdx.x, plan.share, it.start) * kRows;
 #pragma unroll
-    for (int block = 0; block < NG * HALVES; ++block) {
-      if (16 * block >= rows) break;
+    for (int row0 = 0; row0 < kRows; row0 += kAtOnce) {
+      if (row0 >= rows) break;
       __syncthreads();  // the rings, or the last rows' sums, have been read
-      if (half == block / NG)
+      if (half == row0 / (16 * NG))
 #pragma unroll
-        for (int db = 0; db < 8; ++db)
+        for (int ng = 0; ng < kAtOnce / 16; ++ng)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) sm_o[wave][4 * quad + r][col * 8 + db] = o[block % NG][db][r];
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int db = 0; db < 8; db += 4)
+              *reinterpret_cast<f32x4_t*>(&sum_at(wave, 16 * ng + 4 * quad + r, col * 8 + db)) =
+                  f32x4_t{o[ng][db][r], o[ng][db + 1][r], o[ng][db + 2][r], o[ng][db + 3][r]};
       __syncthreads();
-      for (int e = threadIdx.x; e < min(rows - 16 * block, 16) * (kHeadDim / 2); e += NT) {
-        const int h = e / (kHeadDim / 2), dim = e % (kHeadDim / 2) * 2, row = 16 * block + h;
+      for (int e = threadIdx.x; e < min(rows - row0, kAtOnce) * (kHeadDim / 2); e += NT) {
+        const int h = e / (kHeadDim / 2), dim = e % (kHeadDim / 2) * 2, row = row0 + h;
         float M = -FLT_MAX;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w][row]);
@@ -385,9 +393,10 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
           const float wt = __builtin_amdgcn_exp2f(sm_m[w][row] - M);
+          const float2 part = *reinterpret_cast<const float2*>(&sum_at(w, h, dim));
           L += wt * sm_l[w][row];
-          O0 += wt * sm_o[w][h][dim];
-          O1 += wt * sm_o[w][h][dim + 1];
+          O0 += wt * part.x;
+          O1 += wt * part.y;
         }
         if (whole) {
           const float inv = L == 0.0f ? 0.0f : 1.0f / L;
