@@ -369,7 +369,7 @@ __device__ inline void dma4(i32x4_t rsrc, uint32_t to, uint32_t at, uint32_t fro
 // (a wave's sixteen keys of a tile are one run of codes and one of scales), and the wave
 // that fetched them turns them into 16-bit tiles in the vector half of its step, a block of
 // 32 values to a lane: K(t+2) in place of K(t), V(t+2) in place of V(t), so rings of two do.
-constexpr int kAhead4 = 8;
+constexpr int kAhead4 = 2;  // (eight, which a short item has to issue before its first product: 72, not 66 us)
 constexpr int kRaw4 = 16 * kCodes4 + 256;  // a wave's part of a tile: codes, and a row's scales for each lane
 
 template <typename T, bool FOUR>
@@ -427,6 +427,12 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   const uint32_t raw_lds = uint32_t(reinterpret_cast<uintptr_t>(sm_raw)) + wave * (kAhead4 * kRaw4);
   const uint32_t write4 = dma_lds + lane4 * 256 + (((lane & 3) << 2 ^ (group ? 4 * (lane4 & 3) + (lane4 >> 2) : lane4)) << 4);
 
+  // The token of an item's row (below 256: the product's error is less than 1 / group), and
+  // where its query lies behind the item's first one.
+  const uint32_t per_row = 65535u / uint32_t(c.group) + 1u;
+  auto token_of = [&](int32_t row) { return int32_t(uint32_t(row) * per_row >> 16); };
+  auto query_of = [&](int32_t row) { return token_of(row) * (c.n_q_heads - c.group) + row; };
+
   for (;;) {
     const int unit = it.unit;
     const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
@@ -439,14 +445,13 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     const int32_t t0 = __builtin_amdgcn_readfirstlane(span.t0);
     const int32_t t1 = __builtin_amdgcn_readfirstlane(min(span.t1, (seen + kPagedTile - 1) / kPagedTile));
     // This lane's query (a row past the item's repeats the last one).
-    const int32_t row = min(wave * 32 + col, rows - 1), tok = row / c.group;
-    const int64_t qrow = (int64_t(layer) * c.total_new + it.row0 + tok0 + tok) * c.n_q_heads + int64_t(kv) * c.group +
-                         (row - tok * c.group);
-    const int32_t limit = it.cached + tok0 + tok;  // last key that it sees
+    const int32_t row = min(wave * 32 + col, rows - 1);
+    const int64_t qrow0 = (int64_t(layer) * c.total_new + it.row0 + tok0) * c.n_q_heads + int64_t(kv) * c.group;
+    const int32_t limit = it.cached + tok0 + token_of(row);  // last key that it sees
     x8 qf[8];
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk)
-      qf[kk] = __builtin_bit_cast(x8, *reinterpret_cast<const u32x4_t*>(a.q + qrow * kHeadDim + kk * 16 + h * 8));
+      qf[kk] = __builtin_bit_cast(x8, *reinterpret_cast<const u32x4_t*>(a.q + (qrow0 + query_of(row)) * kHeadDim + kk * 16 + h * 8));
     const int32_t limit_lo = __builtin_amdgcn_readfirstlane(limit);
     // last tile of this wave; none where its rows are past the item's
     const int32_t t_last =
@@ -500,7 +505,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     auto slot = [&](int32_t t) { return uint32_t((t - t0) & (kSlots - 1)) * kTileBytes; };
     // FOUR: this wave's part of tile t on its way (rows past the sequence's end lie in its
     // last page, whatever they hold), and its sixteen keys' bad groups.
-    auto fetch4 = [&](int32_t t) {
+    auto fetch4 = [&](int32_t t) {  // returns them
       const uint64_t from = uint64_t(PagedPlan<NT>::uniform(
           reinterpret_cast<int64_t>(reinterpret_cast<const uint8_t*>(pool) + page4(c, unit, __builtin_amdgcn_readfirstlane(ahead)))));
       const i32x4_t rsrc = {int32_t(uint32_t(from)), int32_t(uint32_t(from >> 32) & 0xffffu), (in_page + 1) * kRow4, kBufferFlags};
@@ -508,10 +513,10 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       const uint32_t to = __builtin_amdgcn_readfirstlane(raw_lds + ((t - t0) & (kAhead4 - 1)) * kRaw4);
       dma16(rsrc, to, lane * 16, row * kCodes4);
       dma4(rsrc, to + 16 * kCodes4, lane4 * 4, (in_page + 1) * kCodes4 + row * 4);
-      uint64_t m = 0;
+      uint32_t m = 0;
       if (pages.bad)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) m |= uint64_t(pages.is_bad(entry_of(t, 16 * g))) << g;
+        for (int g = 0; g < 4; ++g) m |= uint32_t(pages.is_bad(entry_of(t, 16 * g))) << g;
       look(t + 1);
       return m;
     };
@@ -655,15 +660,16 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       l_run += sum[0] + sum[1];
     };
 
-    __syncthreads();  // the last item's tiles have been read
+    barrier_lds();  // the last item's outputs are out of the tiles' memory (its stores may be under way)
     if (t0 < t1) {
       look(t0);
       // (the queries have come with the page: no later wait for them drains the DMA)
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));
       // K(t0), K(t0+1), K(t0+2) and V(t0), V(t0+1); then a step fetches one of each
-      std::conditional_t<FOUR, uint64_t, uint32_t> bad = 0;  // bad 16-key groups of tiles t, t + 1, ..: four bits each
+      uint32_t bad = 0;  // bad 16-key groups of tiles t, t + 1, ..: four bits each
       if constexpr (FOUR) {
+#pragma unroll
         for (int i = 0; i < kAhead4; ++i) bad |= fetch4(t0 + i) << (4 * (i + 1));
         convert4(t0, (bad >> 4) & 15);
         bad |= fetch4(t0 + kAhead4) << (4 * (kAhead4 + 1));
@@ -752,10 +758,21 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     float other = l_run;
     swap32(l_run, other);
     l_run += other;
-    if (wave * 32 + col < rows) {
+    // Rows of 256 bytes through this wave's part of the tiles, which nobody reads any more,
+    // so that a store takes four whole rows, not 16 bytes of each of 32 (28 layers x 28 heads,
+    // 256 tokens: 72 to 64 us): chunk q of row r at slot q ^ (r & 15).
+    int out_lane = lane;  // (addresses from here on are not kept in registers across the loop)
+    asm volatile("" : "+v"(out_lane));
+    const uint32_t out_lds = lds0 + wave * (32 * 256);
+    const uint32_t to = out_lds + (out_lane & 31) * 256, swizzle = (out_lane & 15) << 4;
+    const int r0 = out_lane >> 4, chunk = out_lane & 15;
+    auto row_out = [&](int j) {  // chunk `chunk` of row 4 j + r0
+      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t*>((uintptr_t)(out_lds + (4 * j + r0) * 256 + ((chunk ^ ((4 * j + r0) & 15)) << 4)));
+    };
+    const int left = rows - wave * 32;
+    if (left > 0) {
       if (whole) {
         const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-        uint16_t* p = a.out + qrow * kHeadDim + 4 * h;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -763,20 +780,34 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
             u32x2_t e;
             e[0] = elem_pack<T>(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
             e[1] = elem_pack<T>(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
-            *reinterpret_cast<u32x2_t*>(p + 32 * db + 8 * g) = e;
+            *reinterpret_cast<__attribute__((address_space(3))) u32x2_t*>((uintptr_t)(to + ((4 * db + g) << 4 ^ swizzle) + (out_lane >> 5) * 8)) = e;
           }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int32_t at = query_of(wave * 32 + 4 * j + r0);
+          const u32x4_t e = row_out(j);
+          if (4 * j + r0 < left) *reinterpret_cast<u32x4_t*>(a.out + (qrow0 + at) * kHeadDim + chunk * 8) = e;
+        }
       } else {
-        const int64_t at = paged_slot(this_share, share, it.start) * kExtRows + wave * 32 + col;
-        float* p = a.po + at * kHeadDim + 4 * h;
+        const int64_t at = paged_slot(this_share, share, it.start) * kExtRows + wave * 32;
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
+        for (int p = 0; p < 2; ++p) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4_t*>(p + 32 * db + 8 * g) =
-                f32x4_t{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
-        if (h == 0) {
-          a.pm[at] = m_ref;
-          a.pl[at] = l_run;
+          for (int db = 0; db < 2; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              *reinterpret_cast<__attribute__((address_space(3))) f32x4_t*>((uintptr_t)(to + ((8 * db + 2 * g) << 4 ^ (out_lane >> 5 << 4) ^ swizzle))) =
+                  f32x4_t{o[2 * p + db][4 * g], o[2 * p + db][4 * g + 1], o[2 * p + db][4 * g + 2], o[2 * p + db][4 * g + 3]};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const u32x4_t e = row_out(j);
+            if (4 * j + r0 < left)
+              *reinterpret_cast<u32x4_t*>(a.po + (at + 4 * j + r0) * kHeadDim + p * 64 + chunk * 4) = e;
+          }
+        }
+        if (h == 0 && col < left) {
+          a.pm[at + col] = m_ref;
+          a.pl[at + col] = l_run;
         }
       }
     }
