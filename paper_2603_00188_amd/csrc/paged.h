@@ -85,6 +85,8 @@ struct PagedAttnArgs {
   int32_t shares;     // work-groups
   int32_t min_share;  // places
   int32_t item_cost;  // places that beginning an item takes
+  int32_t keep;       // items of up to so many keys are not cut
+  bool joins;          // items may be cut
   int32_t join_items;  // joining by item: their number; 0: by boundary
   int32_t join_rows;  // rows of an item per joining work-group
   int32_t join_groups;  // rows that a joining work-group takes at once, 8 or 32

@@ -135,7 +135,8 @@ PagedDev device_view(const stlite_paged* c) {
 // several-token kernel: 18 us for 11, 72 for 64, 309 for 270, 806 for 729.
 struct AttnPlan {
   bool decode;  // by the kernel of few rows
-  int32_t parts, tokens, rows, shares, min_share, item_cost, join_items, join_rows, join_groups, join_split;
+  int32_t parts, tokens, rows, shares, min_share, item_cost, keep, join_items, join_rows, join_groups, join_split;
+  bool joins;
   size_t bytes;
 };
 
@@ -192,6 +193,15 @@ AttnPlan attn_plan(const stlite_paged* c) {
     items *= blocks;
   }
   if (items == 1) p.item_cost = 0;  // nothing to balance
+  // Where every CU has an item, short ones of several tokens over a 4-bit pool stay in one
+  // share: a cut costs 128 KB a part to write and to read, some 25 us where every share has
+  // one, a share of too much less than an item's time.  Items cut / kept up to 256 / 512 /
+  // 1024 keys, us: 896 of up to 256 keys 66 / 58 / 58 / 58, 128 tokens in 112 units 37 / 27 /
+  // 27 / 27, 512 in them 127 / 128 / 118 / 118, 600 behind 300 in two sequences 59 / 60 / 61 /
+  // 53, 60 behind 1000 in 40 sequences of 4 units 75.0 / 76.4 / 76.8 / 76.1; to 2048, prompts
+  // of 2000 tokens 193 / 205.  (A 16-bit pool's sums keep the order that they had.)
+  p.keep = four && !p.decode && items >= p.shares ? 1024 : 0;
+  p.joins = c->max_len > p.keep;  // (an item's keys: max_len at most, as a sequence's new tokens)
   // (no more shares than the longest possible range fills)
   const double range = double(items) * (double(c->max_len) + p.item_cost);
   p.shares = int32_t(std::max(1.0, std::min(double(p.shares), std::ceil(range / p.min_share))));
@@ -493,6 +503,8 @@ stlite_status stlite_paged_attention(const stlite_paged* c, const uint16_t* q, f
   a.shares = p.shares;
   a.min_share = p.min_share;
   a.item_cost = p.item_cost;
+  a.keep = p.keep;
+  a.joins = p.joins;
   a.join_items = p.join_items;
   a.join_rows = p.join_rows;
   a.join_groups = p.join_groups;

@@ -390,8 +390,8 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   // screen behind 30k tokens 1362 to 1353).
   const int32_t per_die = a.shares / 8, at_die = blockIdx.x / 8;
   const int32_t this_share = at_die < per_die ? int32_t(blockIdx.x % 8) * per_die + at_die : int32_t(blockIdx.x);
-  int64_t x = int64_t(this_share) * plan.share;
-  const int64_t y = min(x + plan.share, plan.total);
+  int64_t x = plan.begin(int64_t(this_share) * plan.share);
+  const int64_t y = plan.begin((int64_t(this_share) + 1) * plan.share);
   if (x >= y) return;
   PagedItem it = plan.find(x);
   if (it.start >= y) return;
@@ -863,7 +863,7 @@ __global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a
     const int64_t cut = (int64_t(blockIdx.x) + 1) * plan.share;
     if (cut >= plan.total) return;
     it = plan.find(cut);
-    if (it.start >= cut || it.start / plan.share != int64_t(blockIdx.x)) return;
+    if (it.keys <= a.keep || it.start >= cut || it.start / plan.share != int64_t(blockIdx.x)) return;
   }
   const int32_t w0 = int32_t(it.start / plan.share), w1 = int32_t((it.start + it.keys - 1) / plan.share);
   if (w0 == w1) return;
@@ -949,7 +949,7 @@ __global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a
 
 template <typename T>
 hipError_t launch_join(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.shares < 2) return hipSuccess;
+  if (a.shares < 2 || !a.joins) return hipSuccess;
   const dim3 grid(a.join_items ? a.join_items : a.shares - 1, a.join_split);
   if (a.join_groups == 8) hipLaunchKernelGGL((paged_join_kernel<T, 8>), grid, dim3(8 * 32), 0, stream, a);
   else hipLaunchKernelGGL((paged_join_kernel<T, 32>), grid, dim3(32 * 32), 0, stream, a);

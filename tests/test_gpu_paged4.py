@@ -297,6 +297,21 @@ def test_extend_at_the_ends_of_blocks(torch_cuda, group, tokens):
     f.compare(q, f.attend(q))
 
 
+@pytest.mark.parametrize("lens,new,page,dtype,layers,hq,hk", [
+    ((900, 1700, 1030), (900, 200, 0), 16, "bf16", 4, 16, 2),    # 288 items: short ones stay whole, those of the second may be cut
+    ((1024, 1025, 5), (513, 600, 5), 64, "fp16", 4, 16, 2),      # keys around the longest that stays whole
+    ((900,), (900,), 32, "bf16", 8, 16, 2),                      # one sequence, nothing to join
+    ((1100, 700, 3), (900, 1050, 9), 16, "fp16", 4, 16, 2),      # shorter than their new tokens
+])
+def test_extend_items_that_stay_whole(torch_cuda, lens, new, page, dtype, layers, hq, hk):
+    """More items than CUs, some of them short: shares that begin and end where an item does, and within one."""
+    f = Served4(lens, new, page, dtype, layers, hq, hk, seed=37, fill=float("nan"))
+    q = f.randn((layers, f.total, hq, D), 1.5)
+    out = f.attend(q)
+    f.compare(q, out)
+    assert np.array_equal(_bits(f.attend(q)), _bits(out)), "two calls differ"
+
+
 def test_extend_many_sequences(torch_cuda):
     """More sequences than threads look them up, idle ones among them."""
     rng = np.random.default_rng(4)
@@ -310,7 +325,7 @@ def test_extend_many_sequences(torch_cuda):
 
 @pytest.mark.parametrize("tiles", [1, 2, 7, 8, 9, 10, 11, 17, 25])
 def test_extend_of_few_and_many_tiles(torch_cuda, tiles):
-    """Caches around the eight tiles that are fetched ahead, in pages that end inside a tile and behind it."""
+    """Caches around the tiles that are fetched ahead, in pages that end inside a tile and behind it."""
     for page, heads in ((16, 7), (128, 7), (16, 40), (128, 40)):
         f = Served4((64 * tiles - 3, 64 * tiles, 64 * tiles + 1), (2, 3, 2), page, "bf16", 1, heads, 1, seed=46, fill=float("nan"))
         q = f.randn((1, f.total, heads, D), 1.5)
