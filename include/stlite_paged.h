@@ -75,7 +75,7 @@ typedef enum stlite_dtype {
  * Limits: head_dim == 128; n_q_heads % n_kv_heads == 0, at most 128 query heads
  * per kv head; page_size 16, 32, 64, 128 or 256; n_layers * n_kv_heads <= 65535;
  * n_seqs <= 65535; 1 <= max_len <= min(2^28, max_pages * page_size); n_s <=
- * max_len; n_pages * page_size < 2^31; total_new < 2^31.
+ * max_len (in stlite_paged_grow any number); n_pages * page_size < 2^31; total_new < 2^31.
  */
 typedef struct stlite_paged {
   int32_t n_layers;

@@ -48,7 +48,7 @@ constexpr int64_t kMaxLen = int64_t(1) << 28;
 constexpr int64_t kIntRows = (int64_t(1) << 31) - 1;
 
 // The pool and its tables; `batch`: the new tokens too.
-stlite_status check_cache(const stlite_paged* c, bool batch) {
+stlite_status check_cache(const stlite_paged* c, bool batch, int64_t most_new = -1) {  // of a sequence; -1: max_len
   if (!c) return fail(STLITE_ERR_INVALID_ARG, "the cache is NULL");
   if (c->n_layers < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1)
     return fail(STLITE_ERR_INVALID_ARG, "n_layers, n_q_heads and n_kv_heads must be >= 1");
@@ -84,9 +84,10 @@ stlite_status check_cache(const stlite_paged* c, bool batch) {
   if (!c->seq_lens || !c->cu_new || !c->h_cu_new)
     return fail(STLITE_ERR_INVALID_ARG, "seq_lens, cu_new and h_cu_new must be non-NULL");
   if (c->h_cu_new[0] != 0) return fail(STLITE_ERR_INVALID_ARG, "cu_new[0] must be 0");
+  if (most_new < 0) most_new = c->max_len;
   for (int32_t s = 0; s < c->n_seqs; ++s) {
     const int64_t n = int64_t(c->h_cu_new[s + 1]) - c->h_cu_new[s];
-    if (n < 0 || n > c->max_len)
+    if (n < 0 || n > most_new)
       return fail(STLITE_ERR_INVALID_ARG, "sequence %d has %lld new tokens, outside [0, max_len = %d]", s, (long long)n,
                   c->max_len);
   }
@@ -538,7 +539,7 @@ stlite_status stlite_paged_read(const stlite_paged* c, uint16_t* k_out, uint16_t
 }
 
 stlite_status stlite_paged_grow(const stlite_paged* c, const stlite_free_pages* pages, int32_t* slots, void* stream) {
-  stlite_status st = check_cache(c, true);
+  stlite_status st = check_cache(c, true, INT32_MAX);  // (more than max_len: parked)
   if (st == STLITE_OK) st = check_pages(c, pages, slots, size_t(c->total_new) * 4);
   if (st != STLITE_OK) return st;
   PagedPagesArgs a{};

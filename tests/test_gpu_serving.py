@@ -104,6 +104,16 @@ def test_slots_of_many_tokens(torch_cuda, total):
     f.grow(np.diff(np.concatenate([[0], cut, [total]])).tolist())
 
 
+@pytest.mark.parametrize("most", [50, 5000])
+def test_more_new_tokens_than_a_sequence_may_have(torch_cuda, most):
+    """By itself more than max_len: parked as any other that does not fit, the others are served."""
+    f = Pages(5, 16, 40, 48)
+    f.grow([3, most, 0, 48, 49])
+    assert f.o.lens == [3, ~0, 0, 48, ~0]
+    f.release([3, 0, 0, 48, 0])
+    f.grow([1, 48, most, 0, most])
+
+
 def test_slots_are_where_rows_go(torch_cuda):
     """The place that an append writes a token's row to."""
     import torch
