@@ -125,8 +125,9 @@ def _pages(**kw):
 @pytest.mark.parametrize("change, status, text", BAD + BAD_BATCH)
 def test_cache_rejections(change, status, text):
     lib, f = S.load(), Fake(**change)
-    calls = [lambda: lib.stlite_paged_read(f.ref, BIG, BIG + (1 << 30), None),
-             lambda: lib.stlite_paged_grow(f.ref, _pages(), BIG + 16384, None)]
+    calls = [lambda: lib.stlite_paged_read(f.ref, BIG, BIG + (1 << 30), None)]
+    if change != {"max_len": 1}:  # growing takes more new tokens than that, and parks the sequence
+        calls.append(lambda: lib.stlite_paged_grow(f.ref, _pages(), BIG + 16384, None))
     if (change, status, text) in BAD:
         calls.append(lambda: lib.stlite_paged_release(f.ref, _pages(), BIG + 16384, None))
     for call in calls:
