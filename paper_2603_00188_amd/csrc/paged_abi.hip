@@ -197,10 +197,10 @@ AttnPlan attn_plan(const stlite_paged* c) {
   // Where every CU has an item, short ones of several tokens over a 4-bit pool stay in one
   // share: a cut costs 128 KB a part to write and to read, some 25 us where every share has
   // one, a share of too much less than an item's time.  Items cut / kept up to 256 / 512 /
-  // 1024 keys, us: 896 of up to 256 keys 66 / 58 / 58 / 58, 128 tokens in 112 units 37 / 27 /
-  // 27 / 27, 512 in them 127 / 128 / 118 / 118, 600 behind 300 in two sequences 59 / 60 / 61 /
-  // 53, 60 behind 1000 in 40 sequences of 4 units 75.0 / 76.4 / 76.8 / 76.1; to 2048, prompts
-  // of 2000 tokens 193 / 205.  (A 16-bit pool's sums keep the order that they had.)
+  // 1024 / 2048 keys, us: 896 of up to 256 keys 66 / 57, 128 tokens in 112 units 38 / 26.5,
+  // 512 in them 127 / 128 / 118 / 118 / 118, 1024 324 / 324 / 323 / 314 / 314, 600 behind 300
+  // in two sequences of 8 units 59 / 59 / 59 / 50 / 50, prompts of 2000 189 / 189 / 188 / 186
+  // / 203.  (A 16-bit pool's sums keep the order that they had.)
   p.keep = four && !p.decode && items >= p.shares ? 1024 : 0;
   p.joins = c->max_len > p.keep;  // (an item's keys: max_len at most, as a sequence's new tokens)
   // (no more shares than the longest possible range fills)

@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void paged_decode_kernel(PagedAt
 // about 1420 of a half's 1840 cycles.  3136 tokens x 28 heads behind 30105 tokens take 1.38 ms, 1.03 PFLOP/s, at
 // the 1.8 GHz that the power leaves; five tokens in each of 16 sequences 60 us, where the
 // cache (225 MB) comes at 5.9 TB/s once the first tiles have; prompts of 131 to 2999
-// tokens 206 us, 0.73 PFLOP/s.
+// tokens 204 us, 0.73 PFLOP/s.
 
 constexpr float kLazy = 8.0f;
 constexpr float kFar = 960.0f;  // 960 + 28 has 10 bits before the point
@@ -390,11 +390,20 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   // screen behind 30k tokens 1362 to 1353).
   const int32_t per_die = a.shares / 8, at_die = blockIdx.x / 8;
   const int32_t this_share = at_die < per_die ? int32_t(blockIdx.x % 8) * per_die + at_die : int32_t(blockIdx.x);
-  int64_t x = plan.begin(int64_t(this_share) * plan.share);
-  const int64_t y = plan.begin((int64_t(this_share) + 1) * plan.share);
+  int64_t x = int64_t(this_share) * plan.share;
+  const int64_t y = min(x + plan.share, plan.total);
   if (x >= y) return;
   PagedItem it = plan.find(x);
-  if (it.start >= y) return;
+  // An item that is not cut is whole in the share that its middle lies in.
+  auto kept = [&] { return FOUR && it.keys <= a.keep; };
+  auto middle2 = [&] { return 2 * it.start + it.keys - a.item_cost; };
+  auto ours = [&] { return kept() ? middle2() <= 2 * y : it.start < y; };
+  if (kept() && middle2() <= 2 * x) {
+    x = it.start + it.keys;
+    if (x >= y) return;
+    plan.next(it);
+  }
+  if (!ours()) return;
   const int64_t share = plan.share;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -436,7 +445,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   for (;;) {
     const int unit = it.unit;
     const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
-    const PagedPart span = paged_part(x, y, it.start, it.keys);
+    const PagedPart span = kept() ? paged_part(it.start, it.start + it.keys, it.start, it.keys) : paged_part(x, y, it.start, it.keys);
     const bool whole = span.whole;
     const int32_t tok0 = it.index * a.tokens, toks = min(it.n - tok0, a.tokens);
     const int32_t rows = toks * c.group;
@@ -814,7 +823,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     x = span.end;
     if (x >= y) break;
     plan.next(it);
-    if (it.start >= y) break;
+    if (!ours()) break;
   }
 }
 

@@ -115,16 +115,6 @@ struct PagedPlan {
     return it;
   }
 
-  // Where the share that would begin at place b of the range begins: an item that is not
-  // cut goes to the share with more of it (the whole work-group calls).
-  __device__ int64_t begin(int64_t b) {
-    if (a.keep == 0 || b <= 0 || b >= total) return min(b, total);
-    const PagedItem it = find(b);
-    if (it.keys > a.keep) return b;
-    const int64_t from = it.start - a.item_cost, to = it.start + it.keys;
-    return b - from < to - b ? from : to;
-  }
-
   // Item i of the call's join_items (the whole work-group calls).
   __device__ PagedItem item(int32_t i) {
     const int32_t per = a.join_items / (a.c.n_units * a.parts);
