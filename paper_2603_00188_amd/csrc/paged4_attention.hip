@@ -78,14 +78,14 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
   __shared__ float sm_m[kWaves][kRows], sm_l[kWaves][kRows];
   __shared__ __align__(1024) uint8_t sm_ring[kWaves][kDepth][kSlot];  // (the waves' sums, once an item is done)
   __shared__ int32_t sm_pages[kWaves * HALVES][kWindow];
-  __shared__ typename PagedPlan<NT>::Shared sm_plan;
+  typedef PagedPlan<NT, true> Plan;
+  __shared__ typename Plan::Shared sm_plan;
   const PagedDev& c = a.c;
-  PagedPlan<NT> plan(a, sm_plan);
+  Plan plan(a, sm_plan);
   int64_t x = int64_t(blockIdx.x) * plan.share;
   const int64_t y = min(x + plan.share, plan.total);
-  if (x >= y) return;
-  PagedItem it = plan.find(x);
-  if (it.start >= y) return;
+  PagedItem it;
+  if (!plan.first(x, y, it)) return;
 
   const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave = wave8 % kWaves, half = HALVES == 1 ? 0 : wave8 / kWaves;
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
     const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
     const int32_t tok0 = it.index * a.tokens, toks = min(it.n - tok0, a.tokens);
     const int32_t rows = a.parts > 1 ? min(c.group - part * kRows, kRows) : toks * c.group;
-    const PagedPart span = paged_part(x, y, it.start, it.keys);
+    const PagedPart span = plan.part(x, y, it);
     const bool whole = span.whole;
     const int32_t sees_first = __builtin_amdgcn_readfirstlane(max(it.cached + tok0 + 1, 0));  // keys that every row sees
     const int32_t k0 = span.t0 * kPagedTile;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
     int32_t held = -kWindow;  // first entry in the window
     const int32_t* const table = c.page_table + int64_t(it.seq) * c.max_pages;
     const uint8_t* const unit_at = reinterpret_cast<const uint8_t*>(
-        PagedPlan<NT>::uniform(reinterpret_cast<int64_t>(reinterpret_cast<const uint8_t*>(c.k) + page4(c, unit, 0))));
+        Plan::uniform(reinterpret_cast<int64_t>(reinterpret_cast<const uint8_t*>(c.k) + page4(c, unit, 0))));
     bool bad = false;  // a page was none
     // Tile i.  Where a page is none, what page 0 holds is read, and left out; rows past the
     // sequence's end lie in its last page, whatever they hold, or in what the table has behind it.
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
     x = span.end;
     if (x >= y) break;
     plan.next(it);
-    if (it.start >= y) break;
+    if (!plan.ours(it, y)) break;
     __syncthreads();  // the sums have been read
   }
 }

@@ -194,14 +194,18 @@ AttnPlan attn_plan(const stlite_paged* c) {
     items *= blocks;
   }
   if (items == 1) p.item_cost = 0;  // nothing to balance
-  // Where every CU has an item, short ones of several tokens over a 4-bit pool stay in one
-  // share: a cut costs 128 KB a part to write and to read, some 25 us where every share has
-  // one, a share of too much less than an item's time.  Items cut / kept up to 256 / 512 /
-  // 1024 / 2048 keys, us: 896 of up to 256 keys 66 / 57, 128 tokens in 112 units 38 / 26.5,
-  // 512 in them 127 / 128 / 118 / 118 / 118, 1024 324 / 324 / 323 / 314 / 314, 600 behind 300
-  // in two sequences of 8 units 59 / 59 / 59 / 50 / 50, prompts of 2000 189 / 189 / 188 / 186
-  // / 203.  (A 16-bit pool's sums keep the order that they had.)
-  p.keep = four && !p.decode && items >= p.shares ? 1024 : 0;
+  // Short items over a 4-bit pool stay in one share.  Of several tokens a cut costs 128 KB a
+  // part to write and to read and where nothing is cut the joining launch goes; a share of
+  // too much costs less than an item's time.  Items cut / kept up to 256 / 512 / 1024 / 2048
+  // keys, us: 896 of up to 256 keys 66 / 57, 128 tokens in 112 units 38 / 26.5, 512 in them
+  // 127 / 128 / 118 / 118 / 118, 1024 324 / 324 / 323 / 314 / 314, 600 behind 300 in two
+  // sequences of 8 units 59 / 59 / 59 / 50 / 50, prompts of 2000 189 / 189 / 188 / 186 / 203.
+  // With fewer items than shares a cut also puts idle CUs to work, the more the fewer items:
+  // cut / whole, 64 items of 530 keys 37 / 27, 56 of up to 500 31 / 24, 192 of 348 38 / 21,
+  // 64 of 1220 39 / 41, 8 of 742 24 / 30.  A few tokens: one layer behind 677 11.7 / 10.1, 1500
+  // 12.5 / 13.2; 28 behind 1000 15.5 / 11.7; 4 in each of 4 sequences of 900 24 / 17; 24 of up
+  // to 6000, kept to 1024 / 1536, 23 / 26.8.  (A 16-bit pool's sums keep the order that they had.)
+  p.keep = !four ? 0 : p.decode || items >= p.shares ? 1024 : int32_t(std::min<int64_t>(1024, 448 * p.shares / (p.shares - items)));
   p.joins = c->max_len > p.keep;  // (an item's keys: max_len at most, as a sequence's new tokens)
   // (no more shares than the longest possible range fills)
   const double range = double(items) * (double(c->max_len) + p.item_cost);

@@ -380,11 +380,12 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   constexpr int kSlots = FOUR ? 2 : kRing;
   __shared__ __align__(1024) uint16_t sm_tiles[2 * kSlots * kTileBytes / 2];  // K, then V: [slot][64][128]
   __shared__ __align__(1024) uint8_t sm_raw[FOUR ? kExtWaves * kAhead4 * kRaw4 : 16];
-  __shared__ typename PagedPlan<NT>::Shared sm_plan;
+  typedef PagedPlan<NT, FOUR> Plan;
+  __shared__ typename Plan::Shared sm_plan;
   __shared__ int32_t sm_pages[kExtWaves][64];
   __shared__ int2 sm_odd[kExtWaves];
   const PagedDev& c = a.c;
-  PagedPlan<NT> plan(a, sm_plan);
+  Plan plan(a, sm_plan);
   // Work-groups go round the eight dies; the shares of a die lie one after another, so
   // that items of one kv head read its cache through one L2 (prompts 215 to 204 us, a
   // screen behind 30k tokens 1362 to 1353).
@@ -392,18 +393,8 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   const int32_t this_share = at_die < per_die ? int32_t(blockIdx.x % 8) * per_die + at_die : int32_t(blockIdx.x);
   int64_t x = int64_t(this_share) * plan.share;
   const int64_t y = min(x + plan.share, plan.total);
-  if (x >= y) return;
-  PagedItem it = plan.find(x);
-  // An item that is not cut is whole in the share that its middle lies in.
-  auto kept = [&] { return FOUR && it.keys <= a.keep; };
-  auto middle2 = [&] { return 2 * it.start + it.keys - a.item_cost; };
-  auto ours = [&] { return kept() ? middle2() <= 2 * y : it.start < y; };
-  if (kept() && middle2() <= 2 * x) {
-    x = it.start + it.keys;
-    if (x >= y) return;
-    plan.next(it);
-  }
-  if (!ours()) return;
+  PagedItem it;
+  if (!plan.first(x, y, it)) return;
   const int64_t share = plan.share;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -445,7 +436,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
   for (;;) {
     const int unit = it.unit;
     const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
-    const PagedPart span = kept() ? paged_part(it.start, it.start + it.keys, it.start, it.keys) : paged_part(x, y, it.start, it.keys);
+    const PagedPart span = plan.part(x, y, it);
     const bool whole = span.whole;
     const int32_t tok0 = it.index * a.tokens, toks = min(it.n - tok0, a.tokens);
     const int32_t rows = toks * c.group;
@@ -486,7 +477,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     };
     auto fetch = [&](int32_t t) {  // returns the tile's bad 16-key groups
       const uint64_t from =
-          uint64_t(PagedPlan<NT>::uniform(reinterpret_cast<int64_t>(pool + page_row(c, unit, __builtin_amdgcn_readfirstlane(ahead)) * kHeadDim)));
+          uint64_t(Plan::uniform(reinterpret_cast<int64_t>(pool + page_row(c, unit, __builtin_amdgcn_readfirstlane(ahead)) * kHeadDim)));
       const i32x4_t rsrc = {int32_t(uint32_t(from)), int32_t(uint32_t(from >> 32) & 0xffffu), (in_page + 1) * (kHeadDim * 2), kBufferFlags};
       const int32_t key = min(t, last) * kPagedTile + key0;
       const uint32_t to = __builtin_amdgcn_readfirstlane(dma_lds + ((t - t0) & (kRing - 1)) * kTileBytes);
@@ -515,7 +506,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     // FOUR: this wave's part of tile t on its way (rows past the sequence's end lie in its
     // last page, whatever they hold), and its sixteen keys' bad groups.
     auto fetch4 = [&](int32_t t) {  // returns them
-      const uint64_t from = uint64_t(PagedPlan<NT>::uniform(
+      const uint64_t from = uint64_t(Plan::uniform(
           reinterpret_cast<int64_t>(reinterpret_cast<const uint8_t*>(pool) + page4(c, unit, __builtin_amdgcn_readfirstlane(ahead)))));
       const i32x4_t rsrc = {int32_t(uint32_t(from)), int32_t(uint32_t(from >> 32) & 0xffffu), (in_page + 1) * kRow4, kBufferFlags};
       const uint32_t row = __builtin_amdgcn_readfirstlane(uint32_t((min(t, last) * kPagedTile + key0) & in_page));
@@ -823,7 +814,7 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
     x = span.end;
     if (x >= y) break;
     plan.next(it);
-    if (!ours()) break;
+    if (!plan.ours(it, y)) break;
   }
 }
 
@@ -872,10 +863,10 @@ __global__ __launch_bounds__(GROUPS * 32) void paged_join_kernel(PagedAttnArgs a
     const int64_t cut = (int64_t(blockIdx.x) + 1) * plan.share;
     if (cut >= plan.total) return;
     it = plan.find(cut);
-    if (it.keys <= a.keep || it.start >= cut || it.start / plan.share != int64_t(blockIdx.x)) return;
+    if (it.start >= cut || it.start / plan.share != int64_t(blockIdx.x)) return;
   }
   const int32_t w0 = int32_t(it.start / plan.share), w1 = int32_t((it.start + it.keys - 1) / plan.share);
-  if (w0 == w1) return;
+  if (w0 == w1 || it.keys <= a.keep) return;
   const int unit = it.unit / a.parts, part = it.unit % a.parts;
   const int layer = unit / c.n_kv_heads, kv = unit % c.n_kv_heads;
   const int32_t tok0 = it.index * a.tokens;

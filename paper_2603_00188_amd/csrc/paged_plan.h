@@ -14,7 +14,9 @@ struct PagedItem {
   int64_t start, keys;       // place of its first key in the flat range
 };
 
-template <int NT>  // threads of the work-group, a multiple of 64
+// NT: threads of the work-group, a multiple of 64; KEEPS: items of up to a.keep keys are
+// not cut, but whole in the share that their middle lies in.
+template <int NT, bool KEEPS = false>
 struct PagedPlan {
   struct Shared {
     int64_t wave[NT / 64];
@@ -114,6 +116,25 @@ struct PagedPlan {
     set_keys(it);
     return it;
   }
+
+  // The first item of the share [x, y), if it has one (the whole work-group calls).
+  __device__ bool first(int64_t& x, int64_t y, PagedItem& it) {
+    if (x >= y) return false;
+    it = find(x);
+    if (kept(it) && middle2(it) <= 2 * x) {  // the share before has it
+      x = it.start + it.keys;
+      if (x >= y) return false;
+      next(it);
+    }
+    return ours(it, y);
+  }
+  // Whether the item, not one of an earlier share, is this one's, which ends at y.
+  __device__ bool ours(const PagedItem& it, int64_t y) const { return kept(it) ? middle2(it) <= 2 * y : it.start < y; }
+  __device__ PagedPart part(int64_t x, int64_t y, const PagedItem& it) const {
+    return kept(it) ? paged_part(it.start, it.start + it.keys, it.start, it.keys) : paged_part(x, y, it.start, it.keys);
+  }
+  __device__ bool kept(const PagedItem& it) const { return KEEPS && it.keys <= a.keep; }
+  __device__ int64_t middle2(const PagedItem& it) const { return 2 * it.start + it.keys - a.item_cost; }
 
   // Item i of the call's join_items (the whole work-group calls).
   __device__ PagedItem item(int32_t i) {

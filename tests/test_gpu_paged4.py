@@ -301,10 +301,15 @@ def test_extend_at_the_ends_of_blocks(torch_cuda, group, tokens):
     ((900, 1700, 1030), (900, 200, 0), 16, "bf16", 4, 16, 2),    # 288 items: short ones stay whole, those of the second may be cut
     ((1024, 1025, 5), (513, 600, 5), 64, "fp16", 4, 16, 2),      # keys around the longest that stays whole
     ((900,), (900,), 32, "bf16", 8, 16, 2),                      # one sequence, nothing to join
+    ((1023, 1024, 1025, 3000, 1, 0), (1, 1, 1, 1, 1, 0), 16, "bf16", 2, 28, 4),   # one token
+    ((1024, 1024, 1000), (1, 1, 1), 256, "fp16", 1, 20, 1),      # one token, nothing to join
+    ((1026, 1024, 500, 5000, 3), (4, 3, 4, 4, 3), 64, "bf16", 2, 28, 4),          # a few
+    ((463, 461, 462, 40, 2000), (9, 36, 37, 40, 100), 16, "bf16", 1, 7, 1),       # fewer items than CUs
+    ((300, 448), (200, 41), 128, "fp16", 1, 14, 2),              # the same, nothing to join
     ((1100, 700, 3), (900, 1050, 9), 16, "fp16", 4, 16, 2),      # shorter than their new tokens
 ])
-def test_extend_items_that_stay_whole(torch_cuda, lens, new, page, dtype, layers, hq, hk):
-    """More items than CUs, some of them short: shares that begin and end where an item does, and within one."""
+def test_items_that_stay_whole(torch_cuda, lens, new, page, dtype, layers, hq, hk):
+    """Short items, which are not cut: shares that begin and end where an item does, and within one."""
     f = Served4(lens, new, page, dtype, layers, hq, hk, seed=37, fill=float("nan"))
     q = f.randn((layers, f.total, hq, D), 1.5)
     out = f.attend(q)
