@@ -153,14 +153,15 @@ AttnPlan attn_plan(const stlite_paged* c) {
   int64_t items = int64_t(c->n_layers) * c->n_kv_heads;
   // A few tokens over a 4-bit pool by the kernel of one: up to 32 rows always, up to 64,
   // whose queries and sums take two waves of a SIMD, where the sequences may have keys
-  // enough.  Several tokens' kernel / this, 28 heads over 4, 16 sequences in 2 layers: 5
-  // tokens (35 rows) behind up to 6000 keys 55 / 45 us, 40000 310 / 176; 9 (63) 58 / 49,
-  // 16000 135 / 91; 8 of 16 heads over 2 (64) behind 40000 170 / 106; one sequence in 8
-  // units behind 3000, 40 rows 21 / 22, 60 22 / 24.  One token of 40 heads of a kv head, two
-  // parts of 32 / one: 8 sequences of 8000 27.5 / 28.8, 16 of 60000 73 / 61; of 64 heads 73 / 65.
+  // enough.  Several tokens' kernel / this, 28 heads over 4, 5 tokens (35 rows) and 9 (63):
+  // 16 sequences behind 900 in 16 units 28.5 / 22.2 and 29 / 24, one behind 600 in 112 20.8 /
+  // 18.3 and 20.9 / 20.4, 16 of up to 40000 in 8 310 / 176; with fewer keys, 4 behind 300 in
+  // 32 15.8 / 16.9 and 16.1 / 18.7, one behind 900 in 4 16.7 / 20.3 and 16.9 / 21.9.  One token
+  // of 40 heads of a kv head, two parts of 32 / one: 16 sequences of 1200 in 4 layers 23.6 /
+  // 28.5, of 8000 in one 31.0 / 31.5, of 60000 73 / 61; of 64 heads there 73 / 65.
   const bool four = is_four(c);
   const int64_t few_rows = std::max<int64_t>(most, 1) * group, keys = items * live * c->max_len;
-  const int64_t most_rows = four && keys >= (1 << 18) ? 64 : 32;
+  const int64_t most_rows = four && keys >= (most > 1 ? 1 << 16 : 1 << 18) ? 64 : 32;
   p.decode = most <= 1 || (four && few_rows <= most_rows);
   if (p.decode) {
     p.tokens = int32_t(std::max<int64_t>(most, 1));
