@@ -59,7 +59,7 @@ class _On:
         if device.type != "cuda":
             raise ValueError(f"the cache is on {device}: the kernels run on a GPU")
         if stream is None:
-            self.stream = torch.cuda.current_stream(device)
+            self.stream = torch.cuda.current_stream(device.index)  # (by the device: 0.6 us more)
             self.handle, self.own = self.stream.cuda_stream, True
         else:
             at = getattr(stream, "device", device)  # (a handle does not know)
