@@ -144,9 +144,12 @@ stlite_status stlite_paged_workspace_size(const stlite_paged* c, size_t* bytes);
  * j < B_s, row kept[u][cu_budget[s] + j] of k and v (the layout of
  * stlite_compact_kv) becomes token j of sequence s.  Exact row copies of 16-bit
  * patterns, which must be of the pool's type (the compression pass knows bf16 alone:
- * its rows belong in a bf16 pool); into a 4-bit pool, their codes.  seq_lens[s] becomes B_s.  p and c must agree in
- * n_layers, n_kv_heads and n_seqs, and every B_s must be at most c->max_len; the
- * new tokens (total_new, cu_new, h_cu_new) are not read.  per_layer != 0: one
+ * its rows belong in a bf16 pool); into a 4-bit pool, their codes.  seq_lens[s] becomes B_s.
+ * A parked sequence (stlite_paged_grow) stays parked, and nothing is stored for it; an empty one
+ * (-1) that holds pages for all of B_s takes them instead, and is parked no more.  (In a row of
+ * the table that no call has grown, -1 with a page in the first entry is as good as 0.)
+ * p and c must agree in n_layers, n_kv_heads and n_seqs, and every B_s must be at most
+ * c->max_len; the new tokens (total_new, cu_new, h_cu_new) are not read.  per_layer != 0: one
  * kept list per layer, as in stlite_compact_kv_layer.  A kept index outside
  * [0, total_tokens) stores zeros.  k and v must not alias the pool.
  */
@@ -227,8 +230,9 @@ typedef struct stlite_free_pages {
  * turn, the lowest first, each wholly or not at all: one whose pages, and those that the
  * sequences before it ask for, are more than the list has, or whose length would pass
  * max_len, is PARKED: its length becomes ~len (negative), and its pages stay as they
- * are.  To every call a parked sequence is an idle slot (length 0): nothing of it is read
- * or stored, its new tokens' outputs are 0.  It stays parked until a release brings it back.
+ * are (behind those of an empty one its row gets a -2).  To every call a parked sequence is
+ * an idle slot (length 0): nothing of it is read or stored, its new tokens' outputs are 0.
+ * It stays parked until a release brings it back.
  * One that needs no page is not held up by those before it.
  *   slots  [total_new], nullable: the row of the pool (page * page_size + row in the page)
  *          of every new token, -1 for a parked sequence's

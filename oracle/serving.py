@@ -6,6 +6,9 @@ from fractions import Fraction
 import math
 
 
+ENDS = -2  # in a page table: where the pages of an empty sequence end that was parked
+
+
 class Pool:
     """A page table, lengths, and the pages that nobody holds."""
 
@@ -27,6 +30,8 @@ class Pool:
             else:
                 granted = False
             if not granted:
+                if len0 == 0 < self.held[s] < len(self.table[s]):
+                    self.table[s][self.held[s]] = ENDS
                 self.lens[s] = len0 if len0 < 0 else ~len0
                 slots += [-1] * n
                 continue
@@ -36,6 +41,16 @@ class Pool:
             self.lens[s] = len0 + n
             slots += [self.table[s][j // self.page] * self.page + j % self.page for j in range(len0, len0 + n)]
         return slots
+
+    def compact(self, budgets):
+        """Lengths; and of every sequence, whether its rows are stored: not where it is parked, but for an empty one with pages."""
+        taken = []
+        for s, n in enumerate(budgets):
+            row = self.table[s][:max(-(-n // self.page), 1)]
+            taken.append(self.lens[s] >= 0 or (self.lens[s] == -1 and row[0] >= 0 and ENDS not in row))
+            if taken[s]:
+                self.lens[s] = n
+        return taken
 
     def release(self, lens=None):
         back = []

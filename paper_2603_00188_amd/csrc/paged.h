@@ -194,6 +194,23 @@ __device__ inline float base2(float s, float scale2) {
 
 __device__ inline int32_t paged_len(const PagedDev& c, int32_t s) { return min(max(c.seq_lens[s], 0), c.max_len); }
 
+// What growing writes behind the pages of an empty sequence that it parks.
+constexpr int32_t kPagesEnd = -2;
+
+// Whether a compaction of `keeps` rows leaves sequence s of length `len` as it is: it is
+// parked, and not an empty one whose row of the table has pages for them.  A length of -1 that
+// no call has written is told from an empty parked sequence's by that row: without pages its
+// first entry is none, with some growing has marked where they end.
+__device__ inline bool stays_parked(const PagedDev& c, int32_t s, int32_t len, int32_t keeps) {
+  if (len >= 0) return false;
+  if (len < -1) return true;
+  const int32_t* row = c.page_table + int64_t(s) * c.max_pages;
+  bool parked = uint32_t(row[0]) >= uint32_t(c.n_pages);
+  const int32_t last = min((keeps - 1) >> c.page_shift, c.max_pages - 1);
+  for (int32_t e = 1; e <= last; ++e) parked |= row[e] == kPagesEnd;
+  return parked;
+}
+
 // First row of page `page` of a unit, in rows of the pool.
 __device__ inline int64_t page_row(const PagedDev& c, int32_t unit, int32_t page) {
   return ((int64_t(unit) * c.n_pages + page) << c.page_shift);

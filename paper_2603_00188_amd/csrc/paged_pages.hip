@@ -82,6 +82,7 @@ __global__ __launch_bounds__(kThreads) void paged_grow_kernel(PagedPagesArgs a) 
     if (PART != kLists && s < c.n_seqs) {
       c.seq_lens[s] = granted ? int32_t(grown) : len < 0 ? len : ~len;
       if (granted) a.held[s] = held + int32_t(need);
+      else if (len == 0 && held > 0 && held < c.max_pages) a.page_table[int64_t(s) * c.max_pages + held] = kPagesEnd;
     }
     int64_t here;  // what this chunk takes: the needs of a first part of its sequences
     scan(granted ? need : 0, sm_wave, here);

@@ -25,6 +25,15 @@ __device__ inline int32_t seq_of(const int32_t* cu, int32_t n, int64_t j) {
   return lo;
 }
 
+// A compaction's lengths, by one work-group.  (The others may read a length before or after:
+// it is negative and stays, is not and remains so, or is -1 and its row of the table says.)
+__device__ inline void set_lengths(const PagedCompactArgs& a) {
+  for (int32_t s = threadIdx.x; s < a.c.n_seqs; s += 256) {
+    const int32_t keeps = a.cu_budget[s + 1] - a.cu_budget[s];
+    if (!stays_parked(a.c, s, a.c.seq_lens[s], keeps)) a.c.seq_lens[s] = keeps;
+  }
+}
+
 // Sixteen lanes move one 256-byte row of K and one of V; a work-group 64 rows of
 // a unit.  HBM-bound: all of a thread's loads are issued before its stores, and
 // both bypass the caches (each byte is touched once).  3.47 GB (a trajectory of 150528
@@ -35,8 +44,7 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) 
   const int64_t j0 = int64_t(blockIdx.x) * kRowsPerGroup;
   const int sub = threadIdx.x >> 4, part = threadIdx.x & 15;
   const int64_t ubase = int64_t(unit) * a.total_tokens;
-  if (blockIdx.x == 0 && unit == 0)
-    for (int32_t s = threadIdx.x; s < a.c.n_seqs; s += 256) a.c.seq_lens[s] = a.cu_budget[s + 1] - a.cu_budget[s];
+  if (blockIdx.x == 0 && unit == 0) set_lengths(a);
   const int64_t kbase = int64_t(a.kept_per_layer ? unit / a.c.n_kv_heads : unit) * a.total_budget;
   int32_t tok[kPer];
   int64_t dst[kPer];  // row of the pool, or -1
@@ -48,10 +56,11 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(PagedCompactArgs a) 
     if (j < a.total_budget) {
       tok[r] = a.kept[kbase + j];
       const int32_t s = seq_of(a.cu_budget, a.c.n_seqs, j);
-      const int32_t at = int32_t(j - a.cu_budget[s]);
+      const int32_t at = int32_t(j - a.cu_budget[s]), keeps = a.cu_budget[s + 1] - a.cu_budget[s], len = a.c.seq_lens[s];
       const int32_t entry = at >> a.c.page_shift;
       const int32_t page = entry < a.c.max_pages ? a.c.page_table[int64_t(s) * a.c.max_pages + entry] : -1;
-      if (page >= 0 && page < a.c.n_pages) dst[r] = page_row(a.c, unit, page) + (at & ((1 << a.c.page_shift) - 1));
+      if (page >= 0 && page < a.c.n_pages && !stays_parked(a.c, s, len, keeps))
+        dst[r] = page_row(a.c, unit, page) + (at & ((1 << a.c.page_shift) - 1));
     }
   }
   if (a.total_budget == 0) return;
@@ -94,8 +103,7 @@ __global__ __launch_bounds__(256) void paged4_compact_kernel(PagedCompactArgs a)
   const int64_t j0 = int64_t(blockIdx.x) * kRowsPerGroup;
   const int sub = threadIdx.x >> 4, part = threadIdx.x & 15;
   const int64_t ubase = int64_t(unit) * a.total_tokens;
-  if (blockIdx.x == 0 && unit == 0)
-    for (int32_t s = threadIdx.x; s < a.c.n_seqs; s += 256) a.c.seq_lens[s] = a.cu_budget[s + 1] - a.cu_budget[s];
+  if (blockIdx.x == 0 && unit == 0) set_lengths(a);
   if (a.total_budget == 0) return;
   const int64_t kbase = int64_t(a.kept_per_layer ? unit / a.c.n_kv_heads : unit) * a.total_budget;
   const int32_t in_page = (1 << a.c.page_shift) - 1;
@@ -111,11 +119,11 @@ __global__ __launch_bounds__(256) void paged4_compact_kernel(PagedCompactArgs a)
     if (j < a.total_budget) {
       tok = a.kept[kbase + j];
       const int32_t s = seq_of(a.cu_budget, a.c.n_seqs, j);
-      const int32_t at = int32_t(j - a.cu_budget[s]);
+      const int32_t at = int32_t(j - a.cu_budget[s]), keeps = a.cu_budget[s + 1] - a.cu_budget[s], len = a.c.seq_lens[s];
       const int32_t entry = at >> a.c.page_shift;
       const int32_t page = entry < a.c.max_pages ? a.c.page_table[int64_t(s) * a.c.max_pages + entry] : -1;
       row_at[r] = at & in_page;
-      if (page >= 0 && page < a.c.n_pages) page_at[r] = page4(a.c, unit, page);
+      if (page >= 0 && page < a.c.n_pages && !stays_parked(a.c, s, len, keeps)) page_at[r] = page4(a.c, unit, page);
     }
     const bool ok = tok >= 0 && tok < a.total_tokens;
     const int64_t src = (ubase + (ok ? tok : 0)) * kHeadDim + part * 8;

@@ -293,7 +293,8 @@ def check_compression(cache: PagedCache, p, k, v) -> None:
 
 
 def paged_compact(cache: PagedCache, p, k, v, kept, per_layer: bool = False, stream=None) -> None:
-    """The kept rows of the compression (problem p) into cache's pages; cache.seq_lens become the budgets."""
+    """The kept rows of the compression (problem p) into cache's pages; cache.seq_lens become the budgets.  A sequence that
+    paged_grow has parked stays so, with nothing stored for it, unless it is empty and holds pages for all of its rows."""
     _check_source(cache, p, k, v)
     lists = cache.n_layers if per_layer else cache.n_layers * cache.n_kv_heads
     if (kept.dtype != torch.int32 or not kept.is_contiguous() or kept.device != cache.device
