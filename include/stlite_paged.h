@@ -33,8 +33,9 @@
  * is stored gets for each block the least power of two of which 7 times reaches the
  * block's greatest magnitude, cut to 2^-120 .. 2^125 (fp16: 2^-14 .. 2^13), and each value
  * the nearest code, ties to the even one, beyond 6 to 6.  A block with an infinity or NaN
- * gets scale byte 255: all of its values are NaN.  The same calls store and read such a
- * pool; what they compute, they compute of the values that the codes stand for.
+ * gets scale byte 255: all of its values are NaN.  (Any other byte is read as what it says,
+ * its values rounded to the 16-bit type, beyond that to infinity.)  The same calls store and
+ * read such a pool; what they compute, they compute of the values that the codes stand for.
  *
  * Lengths live on the device, so that a captured graph follows them: seq_lens[s]
  * counts the tokens of sequence s INCLUDING the new ones of this call.  The new

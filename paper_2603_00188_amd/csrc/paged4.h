@@ -100,4 +100,17 @@ __device__ inline void values_of(uint32_t codes, float scale, uint32_t (&w)[4]) 
   w[3] = Four<T>::template values<3>(codes, scale);
 }
 
+// Eight codes without those whose values are not finite under a scale byte above kMost (any
+// other: all of them stay): 4 and 6 one above it, from 2 on two above, from 1 on, from 1/2 on;
+// of 255 none stays.
+template <typename T>
+__device__ inline uint32_t finite_codes(uint32_t codes, uint32_t byte) {
+  const uint32_t b0 = codes, b1 = codes >> 1, b2 = codes >> 2;
+  uint32_t odd = byte > uint32_t(Four<T>::kMost) ? b2 & b1 : 0u;  // (bit 4 i: code i)
+  if (byte > uint32_t(Four<T>::kMost) + 1) odd = b2;
+  if (Four<T>::kMost < 252 && byte > uint32_t(Four<T>::kMost) + 2) odd = byte > uint32_t(Four<T>::kMost) + 3 ? b2 | b1 | b0 : b2 | b1;
+  if (byte == 255u) odd = ~0u;
+  return codes & ~((odd & 0x11111111u) * 15u);
+}
+
 }  // namespace stlite

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
 #pragma unroll
       for (int db = 0; db < 8; ++db) o[ng][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    bool odd = false;  // blocks that some rows do not see were NaN
+    bool odd = false;  // keys that some rows do not see had values that are not finite
 
     auto step = [&](int32_t j0, uint32_t at) {
       uint64_t none = 0;  // lanes whose run's page is none
@@ -284,13 +284,24 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
         // behind the last tile.
         if (ends) {
           asm volatile("");
+          auto byte = [&](int i) { return vs[i >> 2][i & 3] >> (8 * (col >> 2)) & 255u; };
+          uint32_t most = 0;  // scale byte of keys that some rows see
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int r = 2 * h + (i >> 2);
-            const uint32_t byte = vs[i >> 2][i & 3] >> (8 * (col >> 2)) & 255u;
-            const bool in = key(r, i & 3) < end(r), partly = key(r, i & 3) >= sees_first && byte > uint32_t(Four<T>::kMost);
-            odd |= in && partly;
-            if (!in || partly) vscale[i] = 1.0f;
+            const int32_t j = key(2 * h + (i >> 2), i & 3);
+            if (j >= end(2 * h + (i >> 2))) vscale[i] = 1.0f;
+            else if (j >= sees_first) most = max(most, byte(i));
+          }
+          if (__ballot(most > uint32_t(Four<T>::kMost))) {
+            odd = true;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int32_t j = key(2 * h + (i >> 2), i & 3);
+              if (j < end(2 * h + (i >> 2)) && j >= sees_first) {
+                vc[i] = finite_codes<T>(vc[i], byte(i));
+                if (byte(i) == 255u) vscale[i] = 1.0f;
+              }
+            }
           }
         }
 #pragma unroll
@@ -336,20 +347,27 @@ __global__ __launch_bounds__(kWaves * 64 * HALVES, 2) void paged4_few_kernel(Pag
       if (i + kDepth - 1 < steps) fetch(i + kDepth - 1);  // in place of tile i - 1, whose values have been used
       step(first + i * (kKeys * kWaves), ring + (i & (kDepth - 1)) * kSlot);
     }
-    if (__ballot(odd)) {
+    if (odd) {
       for (int32_t j = max(k0, sees_first); j < k1; ++j) {
         if ((j - k0) / kKeys % kWaves != wave) continue;
         const int32_t page = table[j >> c.page_shift];
         if (uint32_t(page) >= uint32_t(c.n_pages)) continue;
-        const uint32_t byte = (unit_at + v_off + uint64_t(page) * page_bytes + scales_at + (j & in_page) * 4)[col >> 2];
+        const uint8_t* const at = unit_at + v_off + uint64_t(page) * page_bytes;
+        const uint32_t byte = (at + scales_at + (j & in_page) * 4)[col >> 2];
+        uint32_t w[4];
+        values_of<T>(*reinterpret_cast<const uint32_t*>(at + (j & in_page) * kCodes4 + col * 4), scale_of(byte), w);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) w[d] &= (E::not_finite(w[d]) >> 15) * 0xffffu;  // the others count already
 #pragma unroll
         for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int32_t seen = __shfl(sees[ng], 4 * quad + r);
-            const float e = byte > uint32_t(Four<T>::kMost) && j < seen ? __builtin_nanf("") : 0.0f;
+            const uint32_t seen = j < __shfl(sees[ng], 4 * quad + r) ? ~0u : 0u;
 #pragma unroll
-            for (int db = 0; db < 8; ++db) o[ng][db][r] += e;
+            for (int d = 0; d < 4; ++d) {
+              o[ng][2 * d][r] += elem_lo<T>(w[d] & seen);
+              o[ng][2 * d + 1][r] += elem_hi<T>(w[d] & seen);
+            }
           }
       }
     }

@@ -521,8 +521,8 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       return m;
     };
     // FOUR: that part, once it has landed, into the 16-bit tile.  0 * NaN is no zero: in a
-    // tile where some queries do not see every key, blocks of values that are not finite are
-    // cleared, and reach the queries that see them behind the last tile.
+    // tile where some queries do not see every key, values that are not finite are cleared,
+    // and reach the queries that see them behind the last tile.
     auto convert4 = [&](int32_t t, uint32_t b) {
       wait_vmcnt<2 * (kAhead4 - 1)>();
       const uint32_t at = raw_lds + ((t - t0) & (kAhead4 - 1)) * kRaw4;
@@ -532,8 +532,9 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
         const bool odd = byte > uint32_t(Four<T>::kMost);
         if (__ballot(odd)) {
           if (odd) {
-            e = u32x4_t{0u, 0u, 0u, 0u};
-            byte = Four<T>::kLeast;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = finite_codes<T>(e[j], byte);
+            byte = byte == 255u ? Four<T>::kLeast : byte;
           }
           odd_lo = min(odd_lo, t);
           odd_hi = t;
@@ -733,11 +734,21 @@ __global__ __launch_bounds__(kExtWaves * 64, 2) void paged_extend_kernel(PagedAt
       if constexpr (FOUR) {
         const uint8_t* p = reinterpret_cast<const uint8_t*>(c.v) + page4(c, unit, pages.page(key >> c.page_shift));
         const uint32_t scales = *reinterpret_cast<const uint32_t*>(p + (in_page + 1) * kCodes4 + (key & in_page) * 4);
+        p += (key & in_page) * kCodes4;
 #pragma unroll
         for (int db = 0; db < 4; ++db) {
-          const float x = (scales >> (8 * db) & 255u) > uint32_t(Four<T>::kMost) && key <= limit ? __builtin_nanf("") : 0.0f;
+          const uint32_t byte = scales >> (8 * db) & 255u;
+          if (byte <= uint32_t(Four<T>::kMost)) continue;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] += x;
+          for (int g = 0; g < 4; ++g) {
+            const uint32_t codes = *reinterpret_cast<const uint16_t*>(p + 16 * db + 4 * g + 2 * h);
+            const uint32_t w[2] = {Four<T>::template values<0>(codes, scale_of(byte)), Four<T>::template values<1>(codes, scale_of(byte))};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t bits = w[j >> 1] >> (16 * (j & 1)) & 0xffffu;
+              o[db][4 * g + j] += E::not_finite(bits) && key <= limit ? elem_lo<T>(bits) : 0.0f;
+            }
+          }
         }
         continue;
       }
