@@ -61,6 +61,7 @@ struct PagedAppendArgs {
   int32_t interleaved;
   int32_t axis1, axis2;  // pairs >= axis1 go by the second position, >= axis2 by the third
   double turns[64];      // theta^(-i/64) / (2 pi): turns of pair i per position
+  double low[64];        // what they lack of it (a 4-bit pool's)
 };
 
 // Attention runs as a flat range of places, cut into equal shares.  The queries of

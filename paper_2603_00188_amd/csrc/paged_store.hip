@@ -340,8 +340,9 @@ __device__ __forceinline__ void store4(const PagedAppendArgs& a, bool key, int l
 //
 // FOUR: keys and values are stored in 4 bits.  Which code a key gets turns on the side of
 // a border that it lies on, so it is formed in 64 bits, which this card multiplies and adds
-// at the rate of single 32-bit operations, and the token's sines too; on the way to
-// codes it passes through fp32 rounded to odd, which keeps the side.
+// at the rate of single 32-bit operations, and the token's sines too, of turns to 105 bits
+// (their product with a position of 2^31 is off by 10^-16 of a turn then, not 10^-8); on the
+// way to codes it passes through fp32 rounded to odd, which keeps the side.
 template <typename T, int WAVES, bool FOUR>
 __global__ __launch_bounds__(256, FOUR ? 4 : 1) void paged_append_kernel(PagedAppendArgs a) {
   constexpr int kTok = 4 / WAVES;  // tokens per work-group
@@ -374,10 +375,10 @@ __global__ __launch_bounds__(256, FOUR ? 4 : 1) void paged_append_kernel(PagedAp
   if (live && part * 8 + sub < rows) load(part * 8 + sub);
   if (a.positions && live && part == 0) {
     const int axis = (lane >= a.axis1) + (lane >= a.axis2);
-    const double turn = double(a.positions[axis * c.total_new + tok]) * a.turns[lane];
+    const double at = double(a.positions[axis * c.total_new + tok]), turn = at * a.turns[lane];
     if constexpr (FOUR) {
       double sn, cs;
-      sincospi(2.0 * (turn - rint(turn)), &sn, &cs);
+      sincospi(2.0 * fma(at, a.low[lane], fma(at, a.turns[lane], -rint(turn))), &sn, &cs);
       sm_cs64[tl][lane] = make_double2(cs, sn);
       sm_cs[tl][lane] = make_float2(float(cs), float(sn));
     } else {
