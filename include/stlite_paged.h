@@ -129,9 +129,10 @@ typedef struct stlite_rope {
 /*
  * Checks every host-visible field of `c`.  h_page_table and h_seq_lens (host,
  * both nullable) are the values that the device arrays hold: with h_seq_lens,
- * every length must lie in [n_s, max_len]; with both, every page of a sequence's
- * tokens must lie in [0, n_pages), and a page that new tokens are stored in must
- * belong to no other sequence.
+ * every length must lie in [n_s, max_len] or be negative (parked, see
+ * stlite_paged_grow); with both, every page of a sequence's tokens must lie in
+ * [0, n_pages), and a page that new tokens are stored in must belong to no other
+ * sequence, a parked one's tokens included.
  */
 stlite_status stlite_paged_validate(const stlite_paged* c, const int32_t* h_page_table,
                                     const int32_t* h_seq_lens);

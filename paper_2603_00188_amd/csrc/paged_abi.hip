@@ -372,6 +372,7 @@ stlite_status stlite_paged_validate(const stlite_paged* c, const int32_t* h_page
   if (!h_seq_lens) return ok();
   for (int32_t s = 0; s < c->n_seqs; ++s) {
     const int32_t n = c->h_cu_new[s + 1] - c->h_cu_new[s];
+    if (h_seq_lens[s] < 0) continue;  // parked
     if (h_seq_lens[s] < n || h_seq_lens[s] > c->max_len)
       return fail(STLITE_ERR_INVALID_ARG, "sequence %d has length %d, outside [%d new tokens, max_len = %d]", s,
                   h_seq_lens[s], n, c->max_len);
@@ -384,18 +385,22 @@ stlite_status stlite_paged_validate(const stlite_paged* c, const int32_t* h_page
     return fail(STLITE_ERR_INVALID_ARG, "no host memory for %d pages", c->n_pages);
   }
   for (int32_t s = 0; s < c->n_seqs; ++s) {
-    const int32_t used = int32_t(ceil_div(h_seq_lens[s], c->page_size));
+    const bool parked = h_seq_lens[s] < 0;  // its tokens' pages are its own, but nothing reads them
+    const int32_t len = parked ? std::min(~h_seq_lens[s], c->max_len) : h_seq_lens[s];
+    const int32_t used = int32_t(ceil_div(len, c->page_size));
     for (int32_t e = 0; e < used; ++e) {
       const int32_t page = h_page_table[int64_t(s) * c->max_pages + e];
-      if (page < 0 || page >= c->n_pages)
+      if (page < 0 || page >= c->n_pages) {
+        if (parked) continue;
         return fail(STLITE_ERR_INVALID_ARG, "sequence %d: page_table entry %d is %d, outside [0, %d)", s, e, page,
                     c->n_pages);
+      }
       ++holders[size_t(page)];
     }
   }
   for (int32_t s = 0; s < c->n_seqs; ++s) {
     const int32_t n = c->h_cu_new[s + 1] - c->h_cu_new[s];
-    if (n == 0) continue;
+    if (n == 0 || h_seq_lens[s] < 0) continue;
     const int32_t first = (h_seq_lens[s] - n) / c->page_size, used = int32_t(ceil_div(h_seq_lens[s], c->page_size));
     for (int32_t e = first; e < used; ++e)
       if (holders[size_t(h_page_table[int64_t(s) * c->max_pages + e])] > 1)

@@ -1,7 +1,17 @@
 """CPU: parked sequences in the oracle of the pages, and in what the host checks."""
 from __future__ import annotations
 
+import os
+
+import numpy as np
+import pytest
+
 from oracle import serving as OS
+from paper_2603_00188_amd import paged as P
+from paper_2603_00188_amd import stlite as S
+from tests.test_paged_host import Fake, _err
+
+needs_lib = pytest.mark.skipif(not os.path.exists(S.LIB_PATH), reason="library not built")
 
 
 def test_compaction_by_hand():
@@ -20,3 +30,37 @@ def test_compaction_by_hand():
     # a table that no call has grown: a length of -1 is as good as 0
     q = OS.Pool([[0, 1, -1, 3]], [-1], [0], [], 16, 64)
     assert q.compact([50]) == [True] and q.lens == [50]
+
+
+@needs_lib
+def test_validate_takes_parked_sequences():
+    """They are idle slots, whatever the batch has for them; their tokens' pages are still their own."""
+    lib = S.load()
+    f = Fake(counts=(0, 1, 3), page_size=16, n_pages=6, max_pages=3, max_len=40)
+
+    def check(table, lens):
+        t, n = np.asarray(table, np.int32), np.asarray(lens, np.int32)
+        return lib.stlite_paged_validate(f.ref, t.ctypes.data, n.ctypes.data)
+
+    table = [[0, 1, 2], [5, 4, -1]]
+    for lens in ([40, ~0], [40, ~32], [~0, 32], [~40, 32], [~5, ~5], [17, ~40], [17, ~(2 ** 31 - 1)]):
+        assert check(table, lens) == S.OK, lens
+    assert lib.stlite_paged_validate(f.ref, None, np.asarray([~3, 32], np.int32).ctypes.data) == S.OK
+    # a page of a parked sequence's tokens is none for another's new ones; behind its tokens it may be
+    shared = [[0, 1, 2], [1, 4, -1]]
+    assert check(shared, [17, ~16]) == S.ERR_INVALID_ARG and "holds twice" in _err()
+    assert check(shared, [17, ~0]) == S.OK and check([[0, 1, 2], [5, 1, -1]], [17, ~16]) == S.OK
+    assert check(shared, [16, ~16]) == S.OK  # read alone
+    # the others are checked as ever
+    assert check(table, [0, ~0]) == S.ERR_INVALID_ARG and check(table, [41, ~0]) == S.ERR_INVALID_ARG
+    assert check([[0, 6, 2], [5, 4, 3]], [17, ~2]) == S.ERR_INVALID_ARG and "outside [0, 6)" in _err()
+    assert check([[0, 1, 2], [6, 4, 3]], [17, ~2]) == S.OK
+
+
+@needs_lib
+def test_binding_validates_parked_sequences():
+    c = P.PagedCache.alloc(1, 2, 2, 2, 40, page_size=16, device="cpu", n_pages=6)
+    b = P.NewTokens([0, 1, 3], device="cpu")
+    c.validate(b, [[0, 1, -1], [2, -1, -1]], [20, ~7])
+    with pytest.raises(RuntimeError, match="new tokens"):
+        c.validate(b, [[0, 1, -1], [2, -1, -1]], [20, 1])
