@@ -236,6 +236,9 @@ typedef struct stlite_free_pages {
  * an idle slot (length 0): nothing of it is read or stored, its new tokens' outputs are 0.
  * It stays parked until a release brings it back.
  * One that needs no page is not held up by those before it.
+ * One with more than max_len new tokens, which no sequence can have, is parked like any other
+ * that does not fit.  The other calls refuse a batch that holds it, with nothing done: the
+ * host, which knows the counts, gives them one without those tokens (n_s = 0).
  *   slots  [total_new], nullable: the row of the pool (page * page_size + row in the page)
  *          of every new token, -1 for a parked sequence's
  */

@@ -88,8 +88,10 @@ stlite_status check_cache(const stlite_paged* c, bool batch, int64_t most_new = 
   for (int32_t s = 0; s < c->n_seqs; ++s) {
     const int64_t n = int64_t(c->h_cu_new[s + 1]) - c->h_cu_new[s];
     if (n < 0 || n > most_new)
-      return fail(STLITE_ERR_INVALID_ARG, "sequence %d has %lld new tokens, outside [0, max_len = %d]", s, (long long)n,
-                  c->max_len);
+      return fail(STLITE_ERR_INVALID_ARG,
+                  n < 0 ? "sequence %d has %lld new tokens, outside [0, max_len = %d]"
+                        : "sequence %d has %lld new tokens, outside [0, max_len = %d]: stlite_paged_grow alone takes so many, and parks it",
+                  s, (long long)n, c->max_len);
   }
   if (c->total_new != c->h_cu_new[c->n_seqs])
     return fail(STLITE_ERR_INVALID_ARG, "total_new %lld != cu_new[n_seqs] %d", (long long)c->total_new,

@@ -420,7 +420,8 @@ class FreePages(_Fixed):
 
 def paged_grow(cache: PagedCache, pages: FreePages, batch: NewTokens, slots=None, stream=None) -> None:
     """Every sequence grows by its new tokens, with pages where it needs them; one that cannot is parked (its length
-    becomes ~len).  slots: int32 [total_new], becomes the new tokens' rows of the pool, -1 where there is none."""
+    becomes ~len).  More than max_len new tokens park their sequence too, but the calls behind this one take no batch that
+    holds them: they get one without (0 new tokens there).  slots: int32 [total_new], becomes the new tokens' rows of the pool, -1 where there is none."""
     if slots is not None:
         _is(slots, "slots", (batch.total,), torch.int32, cache.device)
     with _On(cache.device, stream) as on:

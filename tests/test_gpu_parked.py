@@ -245,3 +245,29 @@ def test_compaction_in_a_graph_meets_parked_sequences(torch_cuda, bits):
             for o, w in zip(outs, want):
                 assert torch.equal(o[:, rows], w[:, rows] if taken[s] else torch.zeros_like(w[:, rows])), (keep, s)
         f.release(keep)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_a_batch_without_what_cannot_be_served(torch_cuda, bits):
+    """More new tokens than max_len park their sequence.  Growing alone takes such a batch; the calls behind it refuse it with
+    nothing done, and take the one without those tokens."""
+    import torch
+    f = Shared(3, 12, 64, bits, seed=6)
+    new = [20, 65, 30]
+    f.grow(new)
+    assert f.o.lens == [20, ~0, 30]
+    b, before = f.batch(new), f.bytes()
+    q, k = f.rows(LAYERS, b.total, HQ), f.rows(LAYERS, b.total, HK)
+    for call in (lambda: f.P.paged_append(f.cache, b, None, k, k), lambda: f.P.paged_attention(f.cache, b, q),
+                 lambda: f.P.paged_read(f.cache, b), lambda: f.cache.workspace(b), lambda: f.cache.validate(b)):
+        with pytest.raises(RuntimeError, match="grow"):
+            call()
+    torch.cuda.synchronize()
+    f.same()
+    assert all(np.array_equal(x, y) for x, y in zip(f.bytes(), before))
+    f.step([0, 0, 0])
+    rest = f.batch([20, 0, 30])
+    k = f.rows(LAYERS, 50, HK)
+    f.P.paged_append(f.cache, rest, None, k, k)
+    assert torch.equal(f.P.paged_read(f.cache, rest)[0], k) or bits == 4
+    f.step([1, 0, 1])

@@ -64,3 +64,12 @@ def test_binding_validates_parked_sequences():
     c.validate(b, [[0, 1, -1], [2, -1, -1]], [20, ~7])
     with pytest.raises(RuntimeError, match="new tokens"):
         c.validate(b, [[0, 1, -1], [2, -1, -1]], [20, 1])
+
+
+@needs_lib
+def test_refusals_name_the_call_that_takes_more_than_max_len():
+    lib = S.load()
+    assert lib.stlite_paged_read(Fake(counts=(0, 1, 82)).ref, None, None, None) == S.ERR_INVALID_ARG
+    assert "81 new tokens" in _err() and "stlite_paged_grow" in _err()
+    assert lib.stlite_paged_read(Fake(counts=(0, 2, 1)).ref, None, None, None) == S.ERR_INVALID_ARG
+    assert "-1 new tokens" in _err() and "grow" not in _err()
