@@ -148,8 +148,9 @@ stlite_status stlite_paged_workspace_size(const stlite_paged* c, size_t* bytes);
  * patterns, which must be of the pool's type (the compression pass knows bf16 alone:
  * its rows belong in a bf16 pool); into a 4-bit pool, their codes.  seq_lens[s] becomes B_s.
  * A parked sequence (stlite_paged_grow) stays parked, and nothing is stored for it; an empty one
- * (-1) that holds pages for all of B_s takes them instead, and is parked no more.  (In a row of
- * the table that no call has grown, -1 with a page in the first entry is as good as 0.)
+ * (-1) that holds pages for all of B_s takes them instead, and is parked no more.  (So the
+ * lengths of a new cache have to be set, to 0.  In a row of the table that no call has grown,
+ * -1 with a page in the first entry is as good as 0.)
  * p and c must agree in n_layers, n_kv_heads and n_seqs, and every B_s must be at most
  * c->max_len; the new tokens (total_new, cu_new, h_cu_new) are not read.  per_layer != 0: one
  * kept list per layer, as in stlite_compact_kv_layer.  A kept index outside

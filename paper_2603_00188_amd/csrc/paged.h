@@ -64,30 +64,32 @@ struct PagedAppendArgs {
   double low[64];        // what they lack of it (a 4-bit pool's)
 };
 
-// Attention runs as a flat range of places, cut into equal shares.  The queries of
-// a (unit, sequence) are cut into items of `tokens` new tokens (all heads of the
-// kv head: tokens * group rows; decode: one token, at most 16 or 32 heads); item i of a
-// sequence with n new tokens behind c cached ones counts c + min((i + 1) tokens,
-// n) keys, what its last token sees, and takes item_cost places before them.  Items
-// lie one after another, units outermost; work-group w takes the keys in [w share,
-// (w + 1) share) of that range.  A share that holds a whole item writes its output; the parts of an item that
-// several shares cut leave (max, sum, O) in the workspace and are joined by a
-// second launch.  The lengths are read on the device only, so the grid does not
-// depend on them.
+// Attention runs as a flat range of places, cut into equal shares.  The queries of a (unit,
+// sequence) are cut into items of `tokens` new tokens (all heads of the kv head: tokens *
+// group rows; the kernels of few rows: one token, or over a 4-bit pool a sequence's few, at
+// most `rows` of their rows, one token's heads in `parts` where they are more); item i of a
+// sequence with n new tokens behind c cached ones counts c + min((i + 1) tokens, n) keys,
+// what its last token sees, and takes item_cost places before them.  Items lie one after
+// another, units outermost; work-group w takes the keys in [w share, (w + 1) share) of that
+// range, but an item of up to `keep` keys is not cut: it is all of the share's that its
+// middle lies in.  A share that holds a whole item writes its output; the parts of an item
+// that several shares cut leave (max, sum, O) in the workspace and are joined by a second
+// launch, which does not go where no item can be cut.  The lengths are read on the device
+// only, so the grid does not depend on them.
 constexpr int32_t kExtRows = 256;  // rows of an item of several tokens
 struct PagedAttnArgs {
   PagedDev c;
   const uint16_t* q;  // [layers][total_new][q_heads][d]
   uint16_t* out;
   float scale2;       // scale * log2(e)
-  int32_t parts;      // head groups of a kv head (decode: `rows` heads each; else 1)
+  int32_t parts;      // head groups of a kv head (few rows: `rows` heads each; else 1)
   int32_t tokens;     // new tokens per item
-  int32_t rows;       // rows of an item's partial (decode 16 or 32, else kExtRows)
+  int32_t rows;       // rows of an item's partial (few rows 16, 32 or, over 4 bits, 64; else kExtRows)
   int32_t shares;     // work-groups
   int32_t min_share;  // places
   int32_t item_cost;  // places that beginning an item takes
-  int32_t keep;       // items of up to so many keys are not cut
-  bool joins;          // items may be cut
+  int32_t keep;       // items of up to so many keys are not cut (a 16-bit pool: 0)
+  bool joins;         // items may be cut
   int32_t join_items;  // joining by item: their number; 0: by boundary
   int32_t join_rows;  // rows of an item per joining work-group
   int32_t join_groups;  // rows that a joining work-group takes at once, 8 or 32

@@ -559,7 +559,9 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, bool four, bool half, h
   // Few (token, layer) pairs: four waves each, for their latency; else a wave each, which
   // forms the angles once.  28 query heads, a wave / four waves each: 1 pair 4.7 / 3.4 us,
   // 448 pairs 6.0 / 4.7, 1024 pairs 6.9 / 5.9, 1792 pairs 9.2 / 10.1, 4096 pairs 14.3 /
-  // 16.3, 87808 pairs 303 / 317.
+  // 16.3, 87808 pairs 303 / 317.  Over 4 bits, where a wave has more to do, 7.3
+  // / 4.7, 8.4 / 6.1, 9.1 / 7.6, 12.1 / 11.3, 18.4 / 22.1, 342 / 487: the same rule, though four
+  // are still ahead at 1792.
   const bool few = a.c.total_new * a.c.n_layers <= 1024;
   // A grid has less than 2^32 threads along x, which 2^26 tokens reach: the rest of them
   // along z.

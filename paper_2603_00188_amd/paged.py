@@ -15,6 +15,11 @@ Sequences that share a pool's pages as they come and go, and that draft tokens, 
     tokens, n = verify_drafts(step, p, drafted, accept, pick, draft=q, cache=cache)  # lengths go back to what is right
     paged_release(cache, pages, lens)                      # sequences that end (0), pages behind the others' ends
 
+and begin with what the compression keeps, once there is room for it
+
+    paged_grow(cache, pages, NewTokens(cu_budget))         # a sequence that finds none is parked, and left out of
+    compress(p, q_win, k, v, out, cache=cache)             # this and every call until a release takes it back
+
 A cache may hold its keys and values in 4 bits: ``PagedCache.alloc(..., bits=4)``, or uint8 tensors.  The same calls
 store and read it; ``paged_read`` gives rows back in 16 bits.
 
@@ -154,6 +159,8 @@ class PagedCache(_Fixed):
 
     With k and v of uint8, [n_layers][n_kv_heads][n_pages][page_size * 68], the pool holds 4 bits (a page's rows of 64
     bytes of codes, then its rows of 4 scale bytes) and ``dtype`` is the 16-bit type of the calls' other tensors.
+
+    ``seq_lens`` is 0 where nothing is stored; what is negative is parked (paged_grow).
 
     The tensors are the cache's for good (a captured graph and the caches of single layers hold them too): other
     lengths or pages are written into them, ``cache.seq_lens.copy_(lens)``."""

@@ -271,3 +271,50 @@ def test_a_batch_without_what_cannot_be_served(torch_cuda, bits):
     f.P.paged_append(f.cache, rest, None, k, k)
     assert torch.equal(f.P.paged_read(f.cache, rest)[0], k) or bits == 4
     f.step([1, 0, 1])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_compress_into_pages_that_are_too_few(torch_cuda, bits):
+    """The whole pass behind growing: who got pages has the kept rows, who did not is parked and nothing else changed."""
+    import torch
+    from paper_2603_00188_amd import paged as P
+    from paper_2603_00188_amd import stlite as S
+    from tests import gpu_harness as H
+    from tests.test_gpu_parity import SMALL
+    case = H.Case(SMALL["ragged"])
+    w, prob = case.w, case.prob
+    res, keep = case.run(), np.diff(case.cu_budget)
+    n_pages = int((-(-keep // PAGE)).sum()) - 1
+    cache = P.PagedCache.alloc(case.n_layers, w.n_q_heads, w.n_kv_heads, prob.n_seqs, int(keep.max()) + 40, page_size=PAGE,
+                               bits=bits, n_pages=n_pages)
+    pages = P.FreePages.of(cache)
+    o = OS.Pool(cache.page_table.tolist(), [0] * prob.n_seqs, [0] * prob.n_seqs, pages.pages.tolist(), PAGE, cache.max_len)
+    P.paged_grow(cache, pages, P.NewTokens(case.cu_budget))
+    o.grow(keep.tolist())
+    S.compress(prob, case.dq, case.dk, case.dv, case.out, alpha=w.alpha, cache=cache)
+    taken = o.compact(keep.tolist())
+    assert 0 < sum(taken) < prob.n_seqs
+    assert cache.seq_lens.tolist() == o.lens and cache.page_table.tolist() == o.table and pages.held.tolist() == o.held
+    table, used = np.array(o.table), []
+    for s in range(prob.n_seqs):
+        if not taken[s]:
+            continue
+        rows = [OP.place(table, s, j, PAGE, n_pages) for j in range(int(keep[s]))]
+        used += rows
+        a, b = case.cu_budget[s:s + 2]
+        for pool, out in ((cache.k, res["k_out"]), (cache.v, res["v_out"])):
+            if bits == 16:
+                assert np.array_equal(_bits(pool).reshape(prob.units, -1, D)[:, rows].view(np.uint16), out[:, a:b])
+                continue
+            x = torch.from_numpy(out[:, a:b].astype(np.int32).astype(np.int16)).view(torch.bfloat16)
+            codes, scales = O4.rows(pool.cpu().numpy().reshape(prob.units, n_pages, -1), PAGE)
+            want = O4.encode(_f64(x), "bf16")
+            r = np.array(rows)
+            assert np.array_equal(codes[:, r // PAGE, r % PAGE], want[0]) and np.array_equal(scales[:, r // PAGE, r % PAGE], want[1])
+    rest = np.setdiff1d(np.arange(n_pages * PAGE), used)
+    for pool in (cache.k, cache.v):
+        if bits == 16:
+            assert not _bits(pool).reshape(prob.units, -1, D)[:, rest].any()
+        else:
+            codes, scales = O4.rows(pool.cpu().numpy().reshape(prob.units, n_pages, -1), PAGE)
+            assert not codes[:, rest // PAGE, rest % PAGE].any() and not scales[:, rest // PAGE, rest % PAGE].any()
